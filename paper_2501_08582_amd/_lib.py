@@ -1,7 +1,8 @@
 """ctypes binding of ``liblors.so`` (argument marshalling only).
 
 Every function here forwards to the C ABI declared in ``include/lors.h`` and
-turns a non-zero status into :class:`LorsError`.  There is no fallback: if the
+``include/lors_train.h`` (the operators around the layer) and turns a non-zero
+status into :class:`LorsError`.  There is no fallback: if the
 library is missing the first call raises.
 """
 from __future__ import annotations
@@ -43,6 +44,19 @@ EXPORTED = (
 )
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
+# include/lors_train.h
+INDEX_I64 = 0
+INDEX_I32 = 1
+NORM_LAYER = 0
+NORM_RMS = 1
+NORM_MAX_COLS = 32768
+
+EXPORTED_TRAIN = (
+    "lors_train_version", "lors_dropout", "lors_norm_forward", "lors_norm_workspace_bytes", "lors_norm_backward",
+    "lors_embedding_forward", "lors_embedding_workspace_bytes", "lors_embedding_backward",
+    "lors_logprob_workspace_bytes", "lors_logprob_forward", "lors_logprob_backward", "lors_preference",
+)
+
 
 class Problem(ctypes.Structure):
     _fields_ = [
@@ -53,6 +67,77 @@ class Problem(ctypes.Structure):
         ("scale", ctypes.c_float),
         ("dtype", ctypes.c_int32),
         ("mask_format", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class Rng(ctypes.Structure):
+    _fields_ = [
+        ("seed", ctypes.c_uint64),
+        ("offset", ctypes.c_uint64),
+        ("state", ctypes.c_void_p),
+    ]
+
+
+class Dropout(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("p", ctypes.c_double),
+        ("rng", Rng),
+        ("dtype", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class Norm(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("eps", ctypes.c_double),
+        ("p", ctypes.c_double),
+        ("rng", Rng),
+        ("dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+        ("kind", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class Embedding(ctypes.Structure):
+    _fields_ = [
+        ("tokens", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("scale", ctypes.c_float),
+        ("dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+        ("index_dtype", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class Logits(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int64),
+        ("length", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("batch_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("index_dtype", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class Preference(ctypes.Structure):
+    _fields_ = [
+        ("pairs", ctypes.c_int64),
+        ("length", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("beta", ctypes.c_double),
+        ("smoothing", ctypes.c_double),
+        ("index_dtype", ctypes.c_int32),
         ("flags", ctypes.c_uint32),
     ]
 
@@ -92,6 +177,18 @@ def _declare(lib) -> None:
                                  [P, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
         "lors_round_bf16": (ctypes.c_int, [_vp, _i64, _vp, _vp, _i64, _vp, _vp]),
         "lors_backward_noalloc": (ctypes.c_int, [P, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+        "lors_train_version": (ctypes.c_int, []),
+        "lors_dropout": (ctypes.c_int, [ctypes.POINTER(Dropout)] + [_vp] * 4),
+        "lors_norm_forward": (ctypes.c_int, [ctypes.POINTER(Norm)] + [_vp] * 9),
+        "lors_norm_workspace_bytes": (_sz, [ctypes.POINTER(Norm)]),
+        "lors_norm_backward": (ctypes.c_int, [ctypes.POINTER(Norm)] + [_vp] * 11 + [_sz, _vp]),
+        "lors_embedding_forward": (ctypes.c_int, [ctypes.POINTER(Embedding)] + [_vp] * 4),
+        "lors_embedding_workspace_bytes": (_sz, [ctypes.POINTER(Embedding)]),
+        "lors_embedding_backward": (ctypes.c_int, [ctypes.POINTER(Embedding)] + [_vp] * 4 + [_sz, _vp]),
+        "lors_logprob_workspace_bytes": (_sz, [ctypes.POINTER(Logits)]),
+        "lors_logprob_forward": (ctypes.c_int, [ctypes.POINTER(Logits)] + [_vp] * 5 + [_sz, _vp]),
+        "lors_logprob_backward": (ctypes.c_int, [ctypes.POINTER(Logits), _vp, _i64] + [_vp] * 6),
+        "lors_preference": (ctypes.c_int, [ctypes.POINTER(Preference)] + [_vp] * 7),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -182,3 +279,48 @@ def backward_noalloc(p: Problem, dY, X, W, M, B, A, dX, dB, dA, dbias, stream) -
 
 def round_bf16(a, na, a_out, b, nb, b_out, stream) -> int:
     return lib().lors_round_bf16(a, int(na), a_out, b, int(nb), b_out, stream)
+
+
+def dropout(p: Dropout, X, residual, Y, stream) -> int:
+    return lib().lors_dropout(ctypes.byref(p), X, residual, Y, stream)
+
+
+def norm_forward(p: Norm, X, residual, weight, bias, Y, Z, mean, rstd, stream) -> int:
+    return lib().lors_norm_forward(ctypes.byref(p), X, residual, weight, bias, Y, Z, mean, rstd, stream)
+
+
+def norm_workspace_bytes(p: Norm) -> int:
+    return lib().lors_norm_workspace_bytes(ctypes.byref(p))
+
+
+def norm_backward(p: Norm, dY, dZ, Z, weight, mean, rstd, dX, dresidual, dweight, dbias, ws, ws_bytes, stream) -> int:
+    return lib().lors_norm_backward(ctypes.byref(p), dY, dZ, Z, weight, mean, rstd, dX, dresidual, dweight, dbias, ws,
+                                    ws_bytes, stream)
+
+
+def embedding_forward(p: Embedding, ids, E, Y, stream) -> int:
+    return lib().lors_embedding_forward(ctypes.byref(p), ids, E, Y, stream)
+
+
+def embedding_workspace_bytes(p: Embedding) -> int:
+    return lib().lors_embedding_workspace_bytes(ctypes.byref(p))
+
+
+def embedding_backward(p: Embedding, ids, dY, dE, ws, ws_bytes, stream) -> int:
+    return lib().lors_embedding_backward(ctypes.byref(p), ids, dY, dE, ws, ws_bytes, stream)
+
+
+def logprob_workspace_bytes(p: Logits) -> int:
+    return lib().lors_logprob_workspace_bytes(ctypes.byref(p))
+
+
+def logprob_forward(p: Logits, logits, targets, logp, lse, ws, ws_bytes, stream) -> int:
+    return lib().lors_logprob_forward(ctypes.byref(p), logits, targets, logp, lse, ws, ws_bytes, stream)
+
+
+def logprob_backward(p: Logits, dlogp, span, upstream, logits, targets, lse, dlogits, stream) -> int:
+    return lib().lors_logprob_backward(ctypes.byref(p), dlogp, span, upstream, logits, targets, lse, dlogits, stream)
+
+
+def preference(p: Preference, logp, ref, targets, loss, reward, dseq, stream) -> int:
+    return lib().lors_preference(ctypes.byref(p), logp, ref, targets, loss, reward, dseq, stream)

@@ -21,7 +21,8 @@ LIB = os.path.join(PKG, "liblors.so")
 
 ARCH = "gfx950"
 SOURCES = ["abi.cpp", "fwd_bf16.hip", "fwd_thin_bf16.hip", "fwd_few_bf16.hip", "fwd24_bf16.hip", "dx_bf16.hip", "dx_thin_bf16.hip",
-           "g_bf16.hip", "ste_bf16.hip", "f32_path.hip", "misc.hip"]
+           "g_bf16.hip", "ste_bf16.hip", "f32_path.hip", "misc.hip",
+           "train_abi.cpp", "norm.hip", "dropout.hip", "embedding.hip", "preference.hip"]
 
 # Packed-fp32 VALU forms are disabled for all device code (their wrong-result
 # hazard is not worth the VALU throughput on a matrix-core bound path); the

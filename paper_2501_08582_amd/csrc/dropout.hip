@@ -1,0 +1,80 @@
+// Dropout from the counter-based generator: y = keep ? factor x : 0 (+ residual).
+// The mask is a function of (seed, offset, row, column), so the gradient is the
+// same pass over dY and nothing is stored.
+#include "train_common.hpp"
+
+namespace lors {
+namespace train {
+namespace {
+
+constexpr int NT = 256;
+constexpr int kAhead = 2;  // units a thread has in flight
+
+template <typename T>
+__global__ __launch_bounds__(NT) void dropout_kernel(int64_t rows, uint32_t cols, uint32_t units, DropArgs drop,
+                                                     const T* __restrict__ X, const T* __restrict__ residual,
+                                                     T* __restrict__ Y) {
+    const Dropper d(drop);
+    // Units in row-major order, a grid's worth apart: one division, then steps.
+    const uint32_t stride = gridDim.x * NT;
+    const uint32_t step_rows = stride / units, step_units = stride - step_rows * units;
+    const uint32_t t = blockIdx.x * NT + threadIdx.x;
+    int64_t n = t / units;
+    uint32_t g = t - (uint32_t)n * units;
+    while (n < rows) {
+        int64_t at[kAhead];
+        uint32_t row[kAhead], unit[kAhead];
+        int left[kAhead];
+        Raw<T> x[kAhead], r[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            at[i] = n * cols + (int64_t)g * kUnit;
+            row[i] = (uint32_t)n;
+            unit[i] = g;
+            left[i] = n < rows ? (int)min(cols - g * kUnit, (uint32_t)kUnit) : 0;
+            if (left[i] > 0) {
+                x[i] = load_unit(X + at[i], left[i]);
+                if (residual != nullptr) r[i] = load_unit(residual + at[i], left[i]);
+            }
+            n += step_rows;
+            g += step_units;
+            if (g >= units) {
+                g -= units;
+                ++n;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (left[i] <= 0) break;
+            F8 f = widen(x[i]);
+            d.apply(f, row[i], unit[i]);
+            if (residual != nullptr) {
+                const F8 q = widen(r[i]);
+#pragma unroll
+                for (int e = 0; e < kUnit; ++e) f.v[e] += q.v[e];
+            }
+            store_unit(Y + at[i], narrow<T>(f), left[i]);
+        }
+    }
+}
+
+template <typename T>
+hipError_t launch(const DropoutArgs& a, hipStream_t s) {
+    const uint32_t units = (uint32_t)((a.cols + kUnit - 1) / kUnit);
+    // rows and units are below 2^31 and 2^28: their product fits
+    const int64_t blocks = (a.rows * units + NT - 1) / NT;
+    const int64_t most = 16 * (int64_t)256;
+    hipLaunchKernelGGL(dropout_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(NT), 0, s, a.rows,
+                       (uint32_t)a.cols, units, a.drop, (const T*)a.X, (const T*)a.residual, (T*)a.Y);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_dropout(const DropoutArgs& a, bool bf16, hipStream_t s) {
+    if (a.rows == 0) return hipSuccess;
+    return bf16 ? launch<__bf16>(a, s) : launch<float>(a, s);
+}
+
+}  // namespace train
+}  // namespace lors

@@ -1,0 +1,480 @@
+// Scaled embedding lookup, and the gradient of its table.
+//
+// The gradient needs, for every row of the table, the tokens that took it: the
+// tokens are sorted by id first, by counting for short batches and by digits for
+// long ones.  Then every row of the gradient is written once, its zeros and its
+// sums alike, and each sum runs over the tokens in their order, so that the
+// result does not depend on which workgroup is faster.
+#include <algorithm>
+
+#include "train_common.hpp"
+
+namespace lors {
+namespace train {
+namespace {
+
+constexpr int NT = 256;
+
+// A token's id as the sort sees it: ids that stand for no token come last, as
+// `vocab`.
+template <bool I64>
+__device__ __forceinline__ uint32_t id_of(const void* ids, int64_t t, uint32_t vocab) {
+    if constexpr (I64) {
+        const uint64_t v = ((const uint64_t*)ids)[t];
+        return v < vocab ? (uint32_t)v : vocab;
+    } else {
+        const uint32_t v = ((const uint32_t*)ids)[t];
+        return v < vocab ? v : vocab;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// lookup
+// ---------------------------------------------------------------------------
+constexpr int kAhead = 4;  // units a thread has in flight
+
+template <typename T, bool I64>
+__global__ __launch_bounds__(NT) void lookup_kernel(int64_t tokens, uint32_t vocab, uint32_t cols, uint32_t units,
+                                                    float scale, const void* __restrict__ ids,
+                                                    const T* __restrict__ E, T* __restrict__ Y) {
+    // units in row-major order, a grid's worth apart: one division, then steps
+    const uint32_t stride = gridDim.x * NT;
+    const uint32_t step_rows = stride / units, step_units = stride - step_rows * units;
+    const uint32_t t = blockIdx.x * NT + threadIdx.x;
+    int64_t n = t / units;
+    uint32_t g = t - (uint32_t)n * units;
+    while (n < tokens) {
+        int64_t at[kAhead];
+        uint32_t id[kAhead], col[kAhead];
+        int left[kAhead];
+        Raw<T> x[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            col[i] = g * kUnit;
+            at[i] = n * cols + col[i];
+            left[i] = n < tokens ? (int)min(cols - col[i], (uint32_t)kUnit) : 0;
+            id[i] = n < tokens ? id_of<I64>(ids, n, vocab) : vocab;
+            n += step_rows;
+            g += step_units;
+            if (g >= units) {
+                g -= units;
+                ++n;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            x[i] = Raw<T>{};
+            if (id[i] < vocab) x[i] = load_unit(E + (int64_t)id[i] * cols + col[i], left[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (left[i] <= 0) break;
+            F8 f = widen(x[i]);
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) f.v[e] *= scale;
+            if (id[i] >= vocab) f = F8{};
+            store_unit(Y + at[i], narrow<T>(f), left[i]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// tokens sorted by (id, token): pairs {id, token}
+// ---------------------------------------------------------------------------
+
+// By counting: a token's place is the number of tokens that come before it.  A
+// workgroup places 64 tokens, one per lane; its waves share the comparisons,
+// each taking a run of the ids out of LDS.
+constexpr int kRankWaves = 16;
+constexpr int kRankChunk = 8192;                    // ids in LDS at a time
+constexpr int kRankRun = kRankChunk / kRankWaves;   // of them for each wave
+
+template <bool I64>
+__global__ __launch_bounds__(64 * kRankWaves) void rank_kernel(int tokens, uint32_t vocab, const void* __restrict__ ids,
+                                                               uint2* __restrict__ sorted) {
+    __shared__ uint32_t key[kRankChunk];
+    __shared__ int count[kRankWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int i0 = blockIdx.x * 64, i = i0 + lane;
+    const uint32_t mine = i < tokens ? id_of<I64>(ids, i, vocab) : vocab;
+    int before = 0;
+    for (int j0 = 0; j0 < tokens; j0 += kRankChunk) {
+        const int here = min(tokens - j0, kRankChunk);
+        const int runs = (here + kRankRun - 1) / kRankRun;  // the last one is filled up with ids above all
+        __syncthreads();
+        for (int j = threadIdx.x; j < runs * kRankRun; j += 64 * kRankWaves)
+            key[j] = j < here ? id_of<I64>(ids, j0 + j, vocab) : ~0u;
+        __syncthreads();
+        if (wave >= runs) continue;
+        const uint32_t* k = key + wave * kRankRun;
+        const int ja = j0 + wave * kRankRun;  // runs and groups of 64 tokens are aligned to themselves
+        if (ja + kRankRun <= i0) {
+#pragma unroll 8
+            for (int j = 0; j < kRankRun; ++j) before += k[j] <= mine;
+        } else if (ja >= i0 + 64) {
+#pragma unroll 8
+            for (int j = 0; j < kRankRun; ++j) before += k[j] < mine;
+        } else {
+            for (int j = 0; j < kRankRun; ++j) before += k[j] < mine || (k[j] == mine && ja + j < i);
+        }
+    }
+    count[wave][lane] = before;
+    __syncthreads();
+    if (wave != 0 || i >= tokens) return;
+    int place = 0;
+#pragma unroll
+    for (int w = 0; w < kRankWaves; ++w) place += count[w][lane];
+    sorted[place] = uint2{mine, (uint32_t)i};
+}
+
+// By digits of 9 bits, the lowest first.  A workgroup takes a tile of tokens: a
+// first launch counts each tile's digits, a second one places its tokens behind
+// those of lower digits and of earlier tiles, in their order.
+constexpr int kDigitBits = 9;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kSortThreads = kDigits;  // one thread per digit where tiles are joined
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kPerLane = 8;
+constexpr int kTile = kSortThreads * kPerLane;
+
+// Pair i of the tile (in token order: a wave's tokens are consecutive); ids of
+// all ones past the end.
+template <bool FIRST, bool I64>
+__device__ __forceinline__ uint2 pair_at(int64_t i, int64_t tokens, uint32_t vocab, const void* ids,
+                                         const uint2* in) {
+    if (i >= tokens) return uint2{~0u, ~0u};
+    if constexpr (FIRST) return uint2{id_of<I64>(ids, i, vocab), (uint32_t)i};
+    else return in[i];
+}
+
+template <bool FIRST, bool I64>
+__global__ __launch_bounds__(kSortThreads) void digit_count_kernel(int64_t tokens, uint32_t vocab, int shift,
+                                                                   const void* __restrict__ ids,
+                                                                   const uint2* __restrict__ in,
+                                                                   uint32_t* __restrict__ counts) {
+    __shared__ uint32_t count[kDigits];
+    count[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kPerLane; ++q) {
+        const int64_t i = (int64_t)blockIdx.x * kTile + q * kSortThreads + threadIdx.x;
+        if (i < tokens) atomicAdd(&count[(pair_at<FIRST, I64>(i, tokens, vocab, ids, in).x >> shift) & (kDigits - 1)], 1u);
+    }
+    __syncthreads();
+    counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
+}
+
+template <bool FIRST, bool I64>
+__global__ __launch_bounds__(kSortThreads) void digit_place_kernel(int64_t tokens, uint32_t vocab, int shift,
+                                                                   const void* __restrict__ ids,
+                                                                   const uint2* __restrict__ in,
+                                                                   const uint32_t* __restrict__ counts,
+                                                                   uint2* __restrict__ out) {
+    __shared__ uint32_t place[kSortWaves][kDigits];
+    __shared__ uint32_t wave_total[kSortWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t first = (int64_t)blockIdx.x * kTile + wave * (kTile / kSortWaves);
+    uint2 pair[kPerLane];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) place[w][threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kPerLane; ++q) {
+        const int64_t i = first + q * 64 + lane;
+        pair[q] = pair_at<FIRST, I64>(i, tokens, vocab, ids, in);
+        if (i < tokens) atomicAdd(&place[wave][(pair[q].x >> shift) & (kDigits - 1)], 1u);
+    }
+    // this thread's digit: its tokens in all tiles, and in earlier ones
+    uint32_t all = 0, earlier = 0;
+    for (uint32_t b = 0; b < gridDim.x; ++b) {
+        const uint32_t c = counts[(int64_t)b * kDigits + threadIdx.x];
+        all += c;
+        if (b < blockIdx.x) earlier += c;
+    }
+    uint32_t run = all;  // inclusive sum over the lower digits of the wave
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t up = __shfl_up(run, d);
+        if (lane >= d) run += up;
+    }
+    if (lane == 63) wave_total[wave] = run;
+    __syncthreads();
+    uint32_t at = run - all + earlier;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w)
+        if (w < wave) at += wave_total[w];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        const uint32_t c = place[w][threadIdx.x];
+        place[w][threadIdx.x] = at;
+        at += c;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kPerLane; ++q) {
+        const bool real = first + q * 64 + lane < tokens;
+        const uint32_t digit = (pair[q].x >> shift) & (kDigits - 1);
+        uint64_t same = __ballot(real);
+#pragma unroll
+        for (int b = 0; b < kDigitBits; ++b) {
+            const uint64_t set = __ballot((digit >> b) & 1u);
+            same &= (digit >> b) & 1u ? set : ~set;
+        }
+        const int before = __popcll(same & ((1ull << lane) - 1));
+        uint32_t base = 0;
+        if (real && before == 0) base = atomicAdd(&place[wave][digit], (uint32_t)__popcll(same));
+        base = __shfl(base, real ? __ffsll((unsigned long long)same) - 1 : 0);
+        if (real) out[base + before] = pair[q];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// the gradient's rows
+// ---------------------------------------------------------------------------
+
+// Columns go to groups of TL lanes, a unit each; a group of a whole wave keeps
+// what all its lanes agree on in scalar registers.
+template <int TL>
+__device__ __forceinline__ uint32_t uniform(uint32_t v) {
+    if constexpr (TL == 64) return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+    else return v;
+}
+
+// The first position whose id is at least v.  A wave looks at 64 positions at a
+// time (every lane has to take part), a smaller group halves.
+template <int TL>
+__device__ __forceinline__ uint32_t lower_bound(const uint2* __restrict__ sorted, uint32_t tokens, uint32_t v) {
+    uint32_t lo = 0, hi = tokens;
+    while (lo < hi) {
+        if constexpr (TL == 64) {
+            const uint32_t step = (hi - lo + 63) / 64;
+            const uint32_t probe = lo + ((threadIdx.x & 63) + 1) * step - 1;
+            const uint32_t below = __popcll(__ballot(probe < hi && sorted[min(probe, hi - 1)].x < v));
+            lo = uniform<TL>(min(lo + below * step, hi));
+            hi = uniform<TL>(min(hi, lo + step - 1));
+        } else {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (sorted[mid].x < v) lo = mid + 1;
+            else hi = mid;
+        }
+    }
+    return lo;
+}
+
+constexpr uint32_t kChunk = 32;  // sorted positions of a partial sum
+constexpr uint32_t kRows = 8;    // rows of the table per group
+template <typename T>
+constexpr int kBatch = sizeof(T) == 2 ? 16 : 8;  // rows of dY in flight
+
+// acc += the dY units of tokens sorted[pos .. pos + n), n <= kBatch, in order.
+template <typename T>
+__device__ __forceinline__ void add_tokens(F8& acc, const uint2 (&pair)[kBatch<T>], int n, const T* __restrict__ dY,
+                                           int64_t cols, int64_t col, int left) {
+    Raw<T> r[kBatch<T>];
+#pragma unroll
+    for (int i = 0; i < kBatch<T>; ++i)
+        if (i < n) r[i] = load_unit(dY + (int64_t)pair[i].y * cols + col, left);
+#pragma unroll
+    for (int i = 0; i < kBatch<T>; ++i)
+        if (i < n) {
+            const F8 f = widen(r[i]);
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) acc.v[e] += f.v[e];
+        }
+}
+
+// Sums of the chunks that belong to one id as a whole.
+template <typename T, int TL>
+__global__ __launch_bounds__(NT) void chunk_kernel(uint32_t chunks, uint32_t vocab, int64_t cols, uint32_t tiles,
+                                                   const uint2* __restrict__ sorted, const T* __restrict__ dY,
+                                                   float* __restrict__ part) {
+    const uint32_t group = block_id() * (NT / TL) + uniform<TL>(threadIdx.x / TL);
+    const uint32_t chunk = group / tiles;
+    if (chunk >= chunks) return;
+    const int64_t col = ((int64_t)(group - chunk * tiles) * TL + threadIdx.x % TL) * kUnit;
+    const int left = (int)min(cols - col, (int64_t)kUnit);
+    const uint2* s = sorted + (int64_t)chunk * kChunk;
+    if (left <= 0 || s[0].x != s[kChunk - 1].x || s[0].x >= vocab) return;
+    F8 acc = {};
+    for (uint32_t p = 0; p < kChunk; p += kBatch<T>) {
+        uint2 pair[kBatch<T>];
+#pragma unroll
+        for (int i = 0; i < kBatch<T>; ++i) pair[i] = s[p + i];
+        add_tokens<T>(acc, pair, kBatch<T>, dY, cols, col, left);
+    }
+    store_unit(part + chunk * cols + col, narrow<float>(acc), left);
+}
+
+template <typename T, typename G, int TL>
+__global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t vocab, int64_t cols, uint32_t tiles,
+                                                  float scale, const uint2* __restrict__ sorted,
+                                                  const T* __restrict__ dY, const float* __restrict__ part,
+                                                  G* __restrict__ dE) {
+    const uint32_t group = block_id() * (NT / TL) + uniform<TL>(threadIdx.x / TL);
+    const uint32_t v0 = group / tiles * kRows;
+    if (v0 >= vocab) return;
+    int64_t col = ((int64_t)(group % tiles) * TL + threadIdx.x % TL) * kUnit;
+    // lanes past the row stay (the search needs them): they read its first unit
+    const bool real = col < cols;
+    if (!real) col = 0;
+    const int left = (int)min(cols - col, (int64_t)kUnit);
+    uint32_t pos = lower_bound<TL>(sorted, tokens, v0);
+    uint32_t next = pos < tokens ? uniform<TL>(sorted[pos].x) : ~0u;
+    for (uint32_t v = v0; v < min(v0 + kRows, vocab); ++v) {
+        F8 acc = {};
+        while (next == v) {
+            if (pos % kChunk == 0 && tokens - pos >= kChunk && sorted[pos + kChunk - 1].x == v) {
+                // whole chunks of a frequent token: their sums are there
+                const uint32_t n = (lower_bound<TL>(sorted, tokens, v + 1) - pos) / kChunk;
+                const float* p = part + (int64_t)(pos / kChunk) * cols + col;
+#pragma unroll 8
+                for (uint32_t i = 0; i < n; ++i) {
+                    const F8 f = widen(load_unit(p + i * cols, left));
+#pragma unroll
+                    for (int e = 0; e < kUnit; ++e) acc.v[e] += f.v[e];
+                }
+                pos += n * kChunk;
+            } else {
+                // up to the next chunk: the tokens of v come first
+                const int room = (int)min(min(kChunk - pos % kChunk, tokens - pos), (uint32_t)kBatch<T>);
+                uint2 pair[kBatch<T>];
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < kBatch<T>; ++i) {
+                    pair[i] = i < room ? sorted[pos + i] : uint2{~0u, 0u};
+                    n += pair[i].x == v;
+                }
+                add_tokens<T>(acc, pair, n, dY, cols, col, left);
+                pos += n;
+            }
+            next = pos < tokens ? uniform<TL>(sorted[pos].x) : ~0u;
+        }
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e) acc.v[e] *= scale;
+        if (real) store_unit(dE + (int64_t)v * cols + col, narrow<G>(acc), left);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+constexpr int64_t kRankMost = 16384;  // tokens that are sorted by counting
+
+int digit_passes(int64_t vocab) {
+    int bits = 1;
+    while ((vocab >> bits) != 0) ++bits;  // the ids go up to `vocab`
+    return (bits + kDigitBits - 1) / kDigitBits;
+}
+
+// The workspace: two arrays of pairs, the digits' counts of every tile, the
+// partial sums.
+struct Layout {
+    size_t sorted, other, counts, part, bytes;
+};
+Layout layout_of(int64_t tokens, int64_t cols) {
+    Layout w{};
+    const size_t pairs = up256((size_t)tokens * sizeof(uint2));
+    w.other = pairs;
+    w.counts = tokens > kRankMost ? 2 * pairs : pairs;
+    w.part = w.counts + (tokens > kRankMost ? (size_t)((tokens + kTile - 1) / kTile) * kDigits * 4 : 0);
+    w.bytes = w.part + up256((size_t)(tokens / kChunk) * cols * 4);
+    return w;
+}
+
+template <bool FIRST, bool I64>
+void digit_pass(const EmbeddingArgs& a, int shift, const uint2* in, uint32_t* counts, uint2* out, hipStream_t s) {
+    const dim3 grid((unsigned)((a.tokens + kTile - 1) / kTile)), block(kSortThreads);
+    hipLaunchKernelGGL((digit_count_kernel<FIRST, I64>), grid, block, 0, s, a.tokens, (uint32_t)a.vocab, shift, a.ids,
+                       in, counts);
+    hipLaunchKernelGGL((digit_place_kernel<FIRST, I64>), grid, block, 0, s, a.tokens, (uint32_t)a.vocab, shift, a.ids,
+                       in, counts, out);
+}
+
+// The sorted pairs, in one of the two arrays.
+template <bool I64>
+const uint2* sort(const EmbeddingArgs& a, const Layout& w, hipStream_t s) {
+    uint8_t* ws = (uint8_t*)a.workspace;
+    uint2* to = (uint2*)(ws + w.sorted);
+    if (a.tokens <= kRankMost) {
+        hipLaunchKernelGGL(rank_kernel<I64>, dim3((unsigned)((a.tokens + 63) / 64)), dim3(64 * kRankWaves), 0, s,
+                           (int)a.tokens, (uint32_t)a.vocab, a.ids, to);
+        return to;
+    }
+    uint2* other = (uint2*)(ws + w.other);
+    uint32_t* counts = (uint32_t*)(ws + w.counts);
+    const int passes = digit_passes(a.vocab);
+    digit_pass<true, I64>(a, 0, nullptr, counts, to, s);
+    for (int p = 1; p < passes; ++p) {
+        digit_pass<false, I64>(a, p * kDigitBits, to, counts, other, s);
+        uint2* t = to;
+        to = other;
+        other = t;
+    }
+    return to;
+}
+
+template <typename T, typename G, int TL>
+hipError_t sums(const EmbeddingArgs& a, const uint2* sorted, float* part, hipStream_t s) {
+    // fewer groups than 2^32: checked where the call is
+    const uint32_t tiles = (uint32_t)((a.cols + TL * kUnit - 1) / (TL * kUnit));
+    const uint32_t chunks = (uint32_t)(a.tokens / kChunk);
+    const int64_t per = NT / TL;
+    const int64_t chunk_blocks = ((int64_t)chunks * tiles + per - 1) / per;
+    const int64_t row_blocks = ((a.vocab + kRows - 1) / kRows * tiles + per - 1) / per;
+    if (chunks > 0)
+        hipLaunchKernelGGL((chunk_kernel<T, TL>), grid_of(chunk_blocks), dim3(NT), 0, s, chunks,
+                           (uint32_t)a.vocab, a.cols, tiles, sorted, (const T*)a.dY, part);
+    hipLaunchKernelGGL((rows_kernel<T, G, TL>), grid_of(row_blocks), dim3(NT), 0, s, (uint32_t)a.tokens,
+                       (uint32_t)a.vocab, a.cols, tiles, a.scale, sorted, (const T*)a.dY, part, (G*)a.dE);
+    return hipGetLastError();
+}
+
+template <typename T, typename G>
+hipError_t backward(const EmbeddingArgs& a, hipStream_t s) {
+    const Layout w = layout_of(a.tokens, a.cols);
+    const uint2* sorted = nullptr;
+    if (a.tokens > 0) sorted = a.index64 ? sort<true>(a, w, s) : sort<false>(a, w, s);
+    float* part = (float*)((uint8_t*)a.workspace + w.part);
+    const int64_t units = (a.cols + kUnit - 1) / kUnit;
+    if (units <= 8) return sums<T, G, 8>(a, sorted, part, s);
+    if (units <= 16) return sums<T, G, 16>(a, sorted, part, s);
+    return sums<T, G, 64>(a, sorted, part, s);
+}
+
+template <typename T>
+hipError_t forward(const EmbeddingArgs& a, hipStream_t s) {
+    const uint32_t units = (uint32_t)((a.cols + kUnit - 1) / kUnit);
+    const int64_t blocks = (a.tokens * units + NT - 1) / NT, most = 16 * (int64_t)256;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    if (a.index64)
+        hipLaunchKernelGGL((lookup_kernel<T, true>), grid, dim3(NT), 0, s, a.tokens, (uint32_t)a.vocab,
+                           (uint32_t)a.cols, units, a.scale, a.ids, (const T*)a.E, (T*)a.Y);
+    else
+        hipLaunchKernelGGL((lookup_kernel<T, false>), grid, dim3(NT), 0, s, a.tokens, (uint32_t)a.vocab,
+                           (uint32_t)a.cols, units, a.scale, a.ids, (const T*)a.E, (T*)a.Y);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool embedding_groups_fit(int64_t tokens, int64_t vocab, int64_t cols) {
+    const int64_t rows = std::max((vocab + kRows - 1) / kRows, tokens / kChunk);
+    return (cols + 64 * kUnit - 1) / (64 * kUnit) * rows < (int64_t)1 << 31;  // narrower groups have one tile
+}
+
+size_t embedding_workspace_bytes(int64_t tokens, int64_t, int64_t cols) { return layout_of(tokens, cols).bytes; }
+
+hipError_t launch_embedding_forward(const EmbeddingArgs& a, bool bf16, hipStream_t s) {
+    if (a.tokens == 0) return hipSuccess;
+    return bf16 ? forward<__bf16>(a, s) : forward<float>(a, s);
+}
+
+hipError_t launch_embedding_backward(const EmbeddingArgs& a, bool bf16, hipStream_t s) {
+    if (bf16) return a.grad_bf16 ? backward<__bf16, __bf16>(a, s) : backward<__bf16, float>(a, s);
+    return a.grad_bf16 ? backward<float, __bf16>(a, s) : backward<float, float>(a, s);
+}
+
+}  // namespace train
+}  // namespace lors

@@ -1,0 +1,396 @@
+// Log-probabilities of target tokens, the paired preference loss over them, and
+// the gradient of the logits.
+//
+// The logits are what costs: the forward reads each row once, keeping a running
+// maximum and the sum of exponentials below it, and the backward reads it again
+// and writes the gradient.  Rows whose target does not count are not read.
+#include <algorithm>
+
+#include "train_common.hpp"
+
+namespace lors {
+namespace train {
+namespace {
+
+constexpr int NT = 256;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kNone = -__builtin_inff();
+
+template <bool I64>
+__device__ __forceinline__ uint32_t target_of(const void* targets, int64_t n, uint32_t vocab) {
+    if constexpr (I64) {
+        const uint64_t v = ((const uint64_t*)targets)[n];
+        return v < vocab ? (uint32_t)v : ~0u;
+    } else {
+        const uint32_t v = ((const uint32_t*)targets)[n];
+        return v < vocab ? v : ~0u;
+    }
+}
+
+// 2^x by the hardware's instruction: results below 2^-126 are 0, which is far
+// below what a term of a sum next to 1 or a probability is rounded to.
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The sum of exp(x - top) over what was seen, with top the largest of it.
+struct Running {
+    float top = kNone, sum = 0.f;
+
+    template <int N>
+    __device__ __forceinline__ void add(const F8 (&x)[N]) {
+        float m = x[0].v[0];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) m = fmaxf(m, x[i].v[e]);
+        if (m > top) {
+            sum = top == kNone ? 0.f : sum * exp2_hw((top - m) * kLog2e);
+            top = m;
+        }
+        const float ref = top == kNone ? 0.f : top;  // all -Inf so far: they add nothing
+        float s[kUnit] = {};
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) s[e] += exp2_hw((x[i].v[e] - ref) * kLog2e);
+        sum += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+    }
+
+    __device__ __forceinline__ void rescale(float to) {
+        sum = top == kNone ? sum : sum * exp2_hw((top - to) * kLog2e);  // a NaN sum stays
+        top = to;
+    }
+};
+
+// A row of logits in memory, and its last unit past the whole ones.
+template <typename T>
+__device__ __forceinline__ F8 logits_unit(const T* row, uint32_t u, uint32_t vocab) {
+    const int left = (int)min(vocab - u * kUnit, (uint32_t)kUnit);
+    F8 f = widen(load_unit(row + (int64_t)u * kUnit, left));
+#pragma unroll
+    for (int e = 1; e < kUnit; ++e)
+        if (e >= left) f.v[e] = kNone;
+    return f;
+}
+
+// The row's results: `top` and `sum` apart, because a sum of them loses the logarithm
+// next to a large `top` (a row whose entries are all the type's lowest value).
+__device__ __forceinline__ void finish(float x, Running r, int64_t n, float* logp, float2* stats) {
+    logp[n] = (float)((double)x - (double)r.top - log((double)r.sum));
+    if (stats != nullptr) stats[n] = float2{r.top, r.sum};
+}
+
+__device__ __forceinline__ void finish_uncounted(int64_t n, float* logp, float2* stats) {
+    logp[n] = 0.f;
+    if (stats != nullptr) stats[n] = float2{0.f, 0.f};
+}
+
+struct Rows {
+    uint32_t count, length, vocab;
+    int64_t batch_stride, row_stride;
+    __device__ __forceinline__ int64_t offset(uint32_t n) const {
+        const uint32_t b = n / length;
+        return b * batch_stride + (n - b * length) * row_stride;
+    }
+};
+
+// Row n of `splits` workgroups' share each; with splits > 1 their (top, sum) go to
+// `part` and logprob_join_kernel finishes.
+template <typename T, bool I64>
+__global__ __launch_bounds__(NT) void logprob_fwd_kernel(Rows rows, uint32_t splits, const T* __restrict__ logits,
+                                                         const void* __restrict__ targets, float* __restrict__ logp,
+                                                         float2* __restrict__ stats, float2* __restrict__ part) {
+    __shared__ float2 waves[NT / 64];
+    const uint32_t n = block_id() / splits, split = block_id() - n * splits;
+    if (n >= rows.count) return;
+    const uint32_t target = target_of<I64>(targets, n, rows.vocab);
+    if (target == ~0u) {
+        if (threadIdx.x == 0 && splits == 1) finish_uncounted(n, logp, stats);
+        return;
+    }
+    const T* row = logits + rows.offset(n);
+    const uint32_t units = (rows.vocab + kUnit - 1) / kUnit, per = (units + splits - 1) / splits;
+    const uint32_t begin = min(split * per, units), end = min(begin + per, units);
+    const uint32_t whole = min(end, rows.vocab / kUnit);
+    Running r;
+    uint32_t u = begin + threadIdx.x;
+    constexpr int kBatch = 4;
+    for (; u + (kBatch - 1) * NT < whole; u += kBatch * NT) {
+        Raw<T> raw[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) raw[i] = load_whole(row + (int64_t)(u + i * NT) * kUnit);
+        F8 x[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) x[i] = widen(raw[i]);
+        r.add(x);
+    }
+    for (; u < end; u += NT) {
+        const F8 x[1] = {logits_unit(row, u, rows.vocab)};
+        r.add(x);
+    }
+    // lanes, then waves
+    r.rescale(over_lanes<64>(r.top, Max()));
+    r.sum = over_lanes<64>(r.sum, Add());
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = float2{r.top, r.sum};
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    float top = kNone;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, waves[w].x);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        Running q{waves[w].x, waves[w].y};
+        q.rescale(top);
+        sum += q.sum;
+    }
+    r.top = top;
+    r.sum = sum;
+    if (splits > 1) part[block_id()] = float2{top, sum};
+    else finish((float)row[target], r, n, logp, stats);
+}
+
+// One wave per row joins its splits.
+template <typename T, bool I64>
+__global__ __launch_bounds__(64) void logprob_join_kernel(Rows rows, uint32_t splits, const T* __restrict__ logits,
+                                                          const void* __restrict__ targets,
+                                                          const float2* __restrict__ part, float* __restrict__ logp,
+                                                          float2* __restrict__ stats) {
+    const uint32_t n = block_id();
+    if (n >= rows.count) return;
+    const uint32_t target = target_of<I64>(targets, n, rows.vocab);
+    if (target == ~0u) {
+        if (threadIdx.x == 0) finish_uncounted(n, logp, stats);
+        return;
+    }
+    Running r;
+    for (uint32_t i = threadIdx.x; i < splits; i += 64) {
+        const float2 p = part[(int64_t)n * splits + i];
+        Running q{p.x, p.y};
+        const float top = fmaxf(r.top, q.top);
+        r.rescale(top);
+        q.rescale(top);
+        r.sum += q.sum;
+    }
+    r.rescale(over_lanes<64>(r.top, Max()));
+    r.sum = over_lanes<64>(r.sum, Add());
+    if (threadIdx.x == 0) finish((float)logits[rows.offset(n) + target], r, n, logp, stats);
+}
+
+// dlogits = c (onehot - exp(x - top) / sum); a workgroup takes `kPart` units of a row.
+constexpr int kPart = 4;
+template <typename T, bool I64>
+__global__ __launch_bounds__(NT) void logprob_bwd_kernel(Rows rows, uint32_t parts, uint32_t span,
+                                                         const float* __restrict__ dlogp,
+                                                         const float* __restrict__ upstream,
+                                                         const T* __restrict__ logits, const void* __restrict__ targets,
+                                                         const float2* __restrict__ stats, T* __restrict__ dlogits) {
+    const uint32_t n = block_id() / parts, first = (block_id() - n * parts) * (kPart * NT) + threadIdx.x;
+    if (n >= rows.count) return;
+    const uint32_t target = target_of<I64>(targets, n, rows.vocab);
+    const uint32_t units = (rows.vocab + kUnit - 1) / kUnit;
+    T* out = dlogits + (int64_t)n * rows.vocab;
+    if (target == ~0u) {
+#pragma unroll
+        for (int i = 0; i < kPart; ++i) {
+            const uint32_t u = first + i * NT;
+            if (u < units)
+                store_unit(out + (int64_t)u * kUnit, Raw<T>{}, (int)min(rows.vocab - u * kUnit, (uint32_t)kUnit));
+        }
+        return;
+    }
+    const T* row = logits + rows.offset(n);
+    const float c = dlogp[n / span] * (upstream != nullptr ? *upstream : 1.f);
+    const float2 st = stats[n];
+    const float top = st.x, down = -c / st.y;
+    Raw<T> x[kPart];
+#pragma unroll
+    for (int i = 0; i < kPart; ++i) {
+        const uint32_t u = first + i * NT;
+        if (u < units) x[i] = load_unit(row + (int64_t)u * kUnit, (int)min(rows.vocab - u * kUnit, (uint32_t)kUnit));
+    }
+#pragma unroll
+    for (int i = 0; i < kPart; ++i) {
+        const uint32_t u = first + i * NT;
+        if (u >= units) break;
+        F8 f = widen(x[i]);
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e) {
+            f.v[e] = down * exp2_hw((f.v[e] - top) * kLog2e);
+            if (u * kUnit + e == target) f.v[e] += c;
+        }
+        store_unit(out + (int64_t)u * kUnit, narrow<T>(f), (int)min(rows.vocab - u * kUnit, (uint32_t)kUnit));
+    }
+}
+
+// ---------------------------------------------------------------------------
+// the loss over pairs of sequences
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ double log_sigmoid(double x) { return fmin(x, 0.0) - log1p(exp(-fabs(x))); }
+
+__device__ __forceinline__ double pair_loss(double margin, double e) {
+    const double l = -(1.0 - e) * log_sigmoid(margin);
+    return e == 0.0 ? l : l - e * log_sigmoid(-margin);
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// With ONE, a single workgroup takes all pairs, a wave each in turn, and the mean
+// as well; otherwise a workgroup takes a pair and preference_mean_kernel the mean.
+constexpr int kWaves = 16;
+template <bool I64, bool ONE>
+__global__ __launch_bounds__(64 * kWaves) void preference_kernel(int64_t pairs, int64_t length, uint32_t vocab,
+                                                                 double beta, double e, const float* __restrict__ logp,
+                                                                 const float* __restrict__ ref,
+                                                                 const void* __restrict__ targets,
+                                                                 float* __restrict__ loss, float* __restrict__ reward,
+                                                                 float* __restrict__ dseq) {
+    __shared__ double lds[2][kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t begin = ONE ? lane : threadIdx.x, step = ONE ? 64 : 64 * kWaves;
+    double total = 0.0;
+    for (int64_t i = ONE ? wave : blockIdx.x; i < pairs; i += ONE ? kWaves : gridDim.x) {
+        if constexpr (!ONE) __syncthreads();
+        double sum[2];
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const int64_t base = (side * pairs + i) * length;
+            double s = 0.0;
+#pragma unroll 4
+            for (int64_t t = begin; t < length; t += step) {
+                const bool counts = target_of<I64>(targets, base + t, vocab) != ~0u;
+                const double d = (double)logp[base + t] - (ref != nullptr ? (double)ref[base + t] : 0.0);
+                if (counts) s += d;
+            }
+            sum[side] = wave_sum(s);
+        }
+        if constexpr (!ONE) {
+            if (lane == 0) {
+                lds[0][wave] = sum[0];
+                lds[1][wave] = sum[1];
+            }
+            __syncthreads();
+            sum[0] = sum[1] = 0.0;
+            for (int w = 0; w < kWaves; ++w) {
+                sum[0] += lds[0][w];
+                sum[1] += lds[1][w];
+            }
+        }
+        const double won = beta * sum[0], lost = beta * sum[1], margin = won - lost;
+        if (ONE ? lane == 0 : threadIdx.x == 0) {
+            reward[i] = (float)won;
+            reward[pairs + i] = (float)lost;
+            const double d = beta / (double)pairs *
+                             (e * exp(log_sigmoid(margin)) - (1.0 - e) * exp(log_sigmoid(-margin)));
+            dseq[i] = (float)d;
+            dseq[pairs + i] = (float)-d;
+            total += pair_loss(margin, e);
+        }
+    }
+    if constexpr (ONE) {
+        if (lane == 0) lds[0][wave] = total;
+        __syncthreads();
+        if (threadIdx.x != 0) return;
+        total = 0.0;
+        for (int w = 0; w < kWaves; ++w) total += lds[0][w];
+        *loss = (float)(total / (double)pairs);
+    }
+}
+
+__global__ __launch_bounds__(64 * kWaves) void preference_mean_kernel(int64_t pairs, double e,
+                                                                      const float* __restrict__ reward,
+                                                                      float* __restrict__ loss) {
+    __shared__ double lds[kWaves];
+    double total = 0.0;
+    for (int64_t i = threadIdx.x; i < pairs; i += 64 * kWaves)
+        total += pair_loss((double)reward[i] - (double)reward[pairs + i], e);
+    total = wave_sum(total);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = total;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    total = 0.0;
+    for (int w = 0; w < kWaves; ++w) total += lds[w];
+    *loss = (float)(total / (double)pairs);
+}
+
+constexpr int64_t kOneMost = 16384;  // tokens of both sides that one workgroup sums
+
+// Workgroups per row: one where the rows fill the chip, else as many as do, each
+// of a batch of every thread at least.
+uint32_t splits_of(int64_t rows, int64_t vocab) {
+    const int64_t most = (vocab + 8 * NT * 4 - 1) / (8 * NT * 4), want = (1024 + rows - 1) / (rows > 0 ? rows : 1);
+    return (uint32_t)(want < most ? want : most);
+}
+
+Rows rows_of(const LogprobArgs& a) {
+    return Rows{(uint32_t)(a.batch * a.length), (uint32_t)a.length, (uint32_t)a.vocab, a.batch_stride, a.row_stride};
+}
+
+template <typename T, bool I64>
+hipError_t forward(const LogprobArgs& a, hipStream_t s) {
+    const int64_t rows = a.batch * a.length;
+    const uint32_t splits = splits_of(rows, a.vocab);
+    hipLaunchKernelGGL((logprob_fwd_kernel<T, I64>), grid_of(rows * splits), dim3(NT), 0, s, rows_of(a),
+                       splits, (const T*)a.logits, a.targets, a.logp, (float2*)a.stats, (float2*)a.workspace);
+    if (splits > 1)
+        hipLaunchKernelGGL((logprob_join_kernel<T, I64>), grid_of(rows), dim3(64), 0, s, rows_of(a), splits,
+                           (const T*)a.logits, a.targets, (const float2*)a.workspace, a.logp, (float2*)a.stats);
+    return hipGetLastError();
+}
+
+template <typename T, bool I64>
+hipError_t backward(const LogprobArgs& a, hipStream_t s) {
+    const int64_t rows = a.batch * a.length;
+    const uint32_t parts = (uint32_t)((a.vocab + kUnit * kPart * NT - 1) / (kUnit * kPart * NT));
+    hipLaunchKernelGGL((logprob_bwd_kernel<T, I64>), grid_of(rows * parts), dim3(NT), 0, s, rows_of(a), parts,
+                       (uint32_t)a.span, a.dlogp, a.upstream, (const T*)a.logits, a.targets, (const float2*)a.stats, (T*)a.dlogits);
+    return hipGetLastError();
+}
+
+template <bool I64>
+hipError_t preference(const PreferenceArgs& a, hipStream_t s) {
+    if (2 * a.pairs * a.length <= kOneMost && a.pairs <= kOneMost) {
+        hipLaunchKernelGGL((preference_kernel<I64, true>), dim3(1), dim3(64 * kWaves), 0, s, a.pairs, a.length,
+                           (uint32_t)a.vocab, a.beta, a.smoothing, a.logp, a.ref, a.targets, a.loss, a.reward, a.dseq);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((preference_kernel<I64, false>), dim3((unsigned)std::min<int64_t>(a.pairs, 65536)), dim3(64 * kWaves), 0, s, a.pairs,
+                       a.length, (uint32_t)a.vocab, a.beta, a.smoothing, a.logp, a.ref, a.targets, a.loss, a.reward,
+                       a.dseq);
+    hipLaunchKernelGGL(preference_mean_kernel, dim3(1), dim3(64 * kWaves), 0, s, a.pairs, a.smoothing, a.reward,
+                       a.loss);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool logprob_grids_fit(int64_t rows, int64_t vocab) {
+    return rows * ((vocab + kUnit * kPart * NT - 1) / (kUnit * kPart * NT)) < (int64_t)1 << 31;
+}
+
+size_t logprob_workspace_bytes(int64_t rows, int64_t vocab) {
+    const uint32_t splits = rows > 0 ? splits_of(rows, vocab) : 1;
+    return splits > 1 ? (size_t)(rows * splits * sizeof(float2)) : 0;
+}
+
+hipError_t launch_logprob_forward(const LogprobArgs& a, bool bf16, hipStream_t s) {
+    if (a.batch * a.length == 0) return hipSuccess;
+    if (bf16) return a.index64 ? forward<__bf16, true>(a, s) : forward<__bf16, false>(a, s);
+    return a.index64 ? forward<float, true>(a, s) : forward<float, false>(a, s);
+}
+
+hipError_t launch_logprob_backward(const LogprobArgs& a, bool bf16, hipStream_t s) {
+    if (a.batch * a.length == 0) return hipSuccess;
+    if (bf16) return a.index64 ? backward<__bf16, true>(a, s) : backward<__bf16, false>(a, s);
+    return a.index64 ? backward<float, true>(a, s) : backward<float, false>(a, s);
+}
+
+hipError_t launch_preference(const PreferenceArgs& a, hipStream_t s) {
+    return a.index64 ? preference<true>(a, s) : preference<false>(a, s);
+}
+
+}  // namespace train
+}  // namespace lors
