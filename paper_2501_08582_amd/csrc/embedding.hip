@@ -6,6 +6,7 @@
 // sums alike, and each sum runs over the tokens in their order, so that the
 // result does not depend on which workgroup is faster.
 #include <algorithm>
+#include <utility>
 
 #include "train_common.hpp"
 
@@ -83,39 +84,42 @@ __global__ __launch_bounds__(NT) void lookup_kernel(int64_t tokens, uint32_t voc
 // ---------------------------------------------------------------------------
 
 // By counting: a token's place is the number of tokens that come before it.  A
-// workgroup places 64 tokens, one per lane; its waves share the comparisons,
-// each taking a run of the ids out of LDS.
+// workgroup places 64 tokens, one per lane.  Its waves share the comparisons: each
+// takes a run of the ids, 64 in a register, and hands them to all lanes one at a
+// time through a scalar.  Three instructions a comparison of 64 tokens, no memory.
 constexpr int kRankWaves = 16;
-constexpr int kRankChunk = 8192;                    // ids in LDS at a time
-constexpr int kRankRun = kRankChunk / kRankWaves;   // of them for each wave
 
 template <bool I64>
 __global__ __launch_bounds__(64 * kRankWaves) void rank_kernel(int tokens, uint32_t vocab, const void* __restrict__ ids,
                                                                uint2* __restrict__ sorted) {
-    __shared__ uint32_t key[kRankChunk];
     __shared__ int count[kRankWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int i0 = blockIdx.x * 64, i = i0 + lane;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = blockIdx.x, i = group * 64 + lane;
     const uint32_t mine = i < tokens ? id_of<I64>(ids, i, vocab) : vocab;
     int before = 0;
-    for (int j0 = 0; j0 < tokens; j0 += kRankChunk) {
-        const int here = min(tokens - j0, kRankChunk);
-        const int runs = (here + kRankRun - 1) / kRankRun;  // the last one is filled up with ids above all
-        __syncthreads();
-        for (int j = threadIdx.x; j < runs * kRankRun; j += 64 * kRankWaves)
-            key[j] = j < here ? id_of<I64>(ids, j0 + j, vocab) : ~0u;
-        __syncthreads();
-        if (wave >= runs) continue;
-        const uint32_t* k = key + wave * kRankRun;
-        const int ja = j0 + wave * kRankRun;  // runs and groups of 64 tokens are aligned to themselves
-        if (ja + kRankRun <= i0) {
-#pragma unroll 8
-            for (int j = 0; j < kRankRun; ++j) before += k[j] <= mine;
-        } else if (ja >= i0 + 64) {
-#pragma unroll 8
-            for (int j = 0; j < kRankRun; ++j) before += k[j] < mine;
+    const int groups = (tokens + 63) / 64;
+    const int begin = groups * wave / kRankWaves, end = groups * (wave + 1) / kRankWaves;
+    auto ids_of = [&](int g) {  // ids above all past the last token
+        const int j = g * 64 + lane;
+        return g < end && j < tokens ? id_of<I64>(ids, j, vocab) : ~0u;
+    };
+    uint32_t next = ids_of(begin);
+    for (int g = begin; g < end; ++g) {
+        const uint32_t keys = next;
+        next = ids_of(g + 1);
+        // earlier tokens of the same id come before, later ones do not
+        if (g < group) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j) before += (uint32_t)__builtin_amdgcn_readlane((int)keys, j) <= mine;
+        } else if (g > group) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j) before += (uint32_t)__builtin_amdgcn_readlane((int)keys, j) < mine;
         } else {
-            for (int j = 0; j < kRankRun; ++j) before += k[j] < mine || (k[j] == mine && ja + j < i);
+#pragma unroll
+            for (int j = 0; j < 64; ++j) {
+                const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)keys, j);
+                before += k < mine || (k == mine && j < lane);
+            }
         }
     }
     count[wave][lane] = before;
@@ -127,27 +131,28 @@ __global__ __launch_bounds__(64 * kRankWaves) void rank_kernel(int tokens, uint3
     sorted[place] = uint2{mine, (uint32_t)i};
 }
 
-// By digits of 9 bits, the lowest first.  A workgroup takes a tile of tokens: a
-// first launch counts each tile's digits, a second one places its tokens behind
-// those of lower digits and of earlier tiles, in their order.
+// By digits of 9 bits, the lowest first.  A workgroup takes a tile of tokens and
+// places them behind those of lower digits and of earlier tiles, in their order.
+// For that it needs the digits of all tiles: of a short batch it counts them
+// itself, of a long one they are counted by a launch before.
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = kDigits;  // one thread per digit where tiles are joined
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kPerLane = 8;
-constexpr int kTile = kSortThreads * kPerLane;
 
-// Pair i of the tile (in token order: a wave's tokens are consecutive); ids of
-// all ones past the end.
+// A tile is Q tokens a thread; its last one is short.
+template <int Q>
+constexpr int kTile = kSortThreads * Q;
+
+// Token i's pair: from the ids for the first digit, then from the pairs `in`.
 template <bool FIRST, bool I64>
-__device__ __forceinline__ uint2 pair_at(int64_t i, int64_t tokens, uint32_t vocab, const void* ids,
-                                         const uint2* in) {
-    if (i >= tokens) return uint2{~0u, ~0u};
+__device__ __forceinline__ uint2 pair_of(int64_t i, uint32_t vocab, const void* ids, const uint2* in) {
     if constexpr (FIRST) return uint2{id_of<I64>(ids, i, vocab), (uint32_t)i};
     else return in[i];
 }
+__device__ __forceinline__ uint32_t digit_of(uint2 pair, int shift) { return (pair.x >> shift) & (kDigits - 1); }
 
-template <bool FIRST, bool I64>
+template <int Q, bool FIRST, bool I64>
 __global__ __launch_bounds__(kSortThreads) void digit_count_kernel(int64_t tokens, uint32_t vocab, int shift,
                                                                    const void* __restrict__ ids,
                                                                    const uint2* __restrict__ in,
@@ -156,15 +161,16 @@ __global__ __launch_bounds__(kSortThreads) void digit_count_kernel(int64_t token
     count[threadIdx.x] = 0;
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < kPerLane; ++q) {
-        const int64_t i = (int64_t)blockIdx.x * kTile + q * kSortThreads + threadIdx.x;
-        if (i < tokens) atomicAdd(&count[(pair_at<FIRST, I64>(i, tokens, vocab, ids, in).x >> shift) & (kDigits - 1)], 1u);
+    for (int q = 0; q < Q; ++q) {
+        const int64_t i = (int64_t)blockIdx.x * kTile<Q> + q * kSortThreads + threadIdx.x;
+        if (i < tokens) atomicAdd(&count[digit_of(pair_of<FIRST, I64>(i, vocab, ids, in), shift)], 1u);
     }
     __syncthreads();
     counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
 }
 
-template <bool FIRST, bool I64>
+// SELF: counts is not there.
+template <int Q, bool SELF, bool FIRST, bool I64>
 __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(int64_t tokens, uint32_t vocab, int shift,
                                                                    const void* __restrict__ ids,
                                                                    const uint2* __restrict__ in,
@@ -173,24 +179,39 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(int64_t token
     __shared__ uint32_t place[kSortWaves][kDigits];
     __shared__ uint32_t wave_total[kSortWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = (int64_t)blockIdx.x * kTile + wave * (kTile / kSortWaves);
-    uint2 pair[kPerLane];
+    const int64_t tile = (int64_t)blockIdx.x * kTile<Q>;
+    const int64_t first = tile + wave * (kTile<Q> / kSortWaves);  // a wave's tokens are consecutive
+    uint2 pair[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int64_t i = first + q * 64 + lane;
+        pair[q] = i < tokens ? pair_of<FIRST, I64>(i, vocab, ids, in) : uint2{~0u, ~0u};
+    }
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) place[w][threadIdx.x] = 0;
-    __syncthreads();
+    uint32_t all = 0, earlier = 0;  // of this thread's digit: the tokens in all tiles, and in earlier ones
+    if constexpr (SELF) {
+        __shared__ uint32_t others[2][kDigits];  // in earlier tiles, in this one and later ones
+        others[0][threadIdx.x] = others[1][threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll 8
+        for (int64_t i = threadIdx.x; i < tokens; i += kSortThreads)
+            atomicAdd(&others[i >= tile][digit_of(pair_of<FIRST, I64>(i, vocab, ids, in), shift)], 1u);
+        __syncthreads();
+        earlier = others[0][threadIdx.x];
+        all = earlier + others[1][threadIdx.x];
+    } else {
+#pragma unroll 4
+        for (uint32_t b = 0; b < gridDim.x; ++b) {
+            const uint32_t c = counts[(int64_t)b * kDigits + threadIdx.x];
+            all += c;
+            if (b < blockIdx.x) earlier += c;
+        }
+        __syncthreads();
+    }
 #pragma unroll
-    for (int q = 0; q < kPerLane; ++q) {
-        const int64_t i = first + q * 64 + lane;
-        pair[q] = pair_at<FIRST, I64>(i, tokens, vocab, ids, in);
-        if (i < tokens) atomicAdd(&place[wave][(pair[q].x >> shift) & (kDigits - 1)], 1u);
-    }
-    // this thread's digit: its tokens in all tiles, and in earlier ones
-    uint32_t all = 0, earlier = 0;
-    for (uint32_t b = 0; b < gridDim.x; ++b) {
-        const uint32_t c = counts[(int64_t)b * kDigits + threadIdx.x];
-        all += c;
-        if (b < blockIdx.x) earlier += c;
-    }
+    for (int q = 0; q < Q; ++q)
+        if (first + q * 64 + lane < tokens) atomicAdd(&place[wave][digit_of(pair[q], shift)], 1u);
     uint32_t run = all;  // inclusive sum over the lower digits of the wave
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -211,9 +232,9 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(int64_t token
     }
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < kPerLane; ++q) {
+    for (int q = 0; q < Q; ++q) {
         const bool real = first + q * 64 + lane < tokens;
-        const uint32_t digit = (pair[q].x >> shift) & (kDigits - 1);
+        const uint32_t digit = digit_of(pair[q], shift);
         uint64_t same = __ballot(real);
 #pragma unroll
         for (int b = 0; b < kDigitBits; ++b) {
@@ -294,14 +315,14 @@ __global__ __launch_bounds__(NT) void chunk_kernel(uint32_t chunks, uint32_t voc
     const int64_t col = ((int64_t)(group - chunk * tiles) * TL + threadIdx.x % TL) * kUnit;
     const int left = (int)min(cols - col, (int64_t)kUnit);
     const uint2* s = sorted + (int64_t)chunk * kChunk;
-    if (left <= 0 || s[0].x != s[kChunk - 1].x || s[0].x >= vocab) return;
-    F8 acc = {};
-    for (uint32_t p = 0; p < kChunk; p += kBatch<T>) {
-        uint2 pair[kBatch<T>];
+    uint2 pair[kChunk / kBatch<T>][kBatch<T>];  // all at once: a chunk is two waits on memory
 #pragma unroll
-        for (int i = 0; i < kBatch<T>; ++i) pair[i] = s[p + i];
-        add_tokens<T>(acc, pair, kBatch<T>, dY, cols, col, left);
-    }
+    for (uint32_t i = 0; i < kChunk; ++i) pair[i / kBatch<T>][i % kBatch<T>] = s[i];
+    const uint32_t id = pair[0][0].x;
+    if (left <= 0 || id != pair[kChunk / kBatch<T> - 1][kBatch<T> - 1].x || id >= vocab) return;
+    F8 acc = {};
+#pragma unroll
+    for (uint32_t b = 0; b < kChunk / kBatch<T>; ++b) add_tokens<T>(acc, pair[b], kBatch<T>, dY, cols, col, left);
     store_unit(part + chunk * cols + col, narrow<float>(acc), left);
 }
 
@@ -360,7 +381,9 @@ __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t voca
 // ---------------------------------------------------------------------------
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-constexpr int64_t kRankMost = 16384;  // tokens that are sorted by counting
+constexpr int64_t kRankMost = 4096;     // tokens that are sorted by counting
+constexpr int64_t kSelfMost = 8192;    // tokens whose digits every workgroup counts
+constexpr int64_t kShortMost = 65536;  // tokens that are sorted in short tiles
 
 int digit_passes(int64_t vocab) {
     int bits = 1;
@@ -368,31 +391,49 @@ int digit_passes(int64_t vocab) {
     return (bits + kDigitBits - 1) / kDigitBits;
 }
 
-// The workspace: two arrays of pairs, the digits' counts of every tile, the
-// partial sums.
+int64_t tiles_of(int64_t tokens) {
+    const int64_t tile = tokens <= kShortMost ? kTile<2> : kTile<8>;
+    return (tokens + tile - 1) / tile;
+}
+
+// The workspace: two arrays of pairs, the digits' counts of every tile, the partial
+// sums.
 struct Layout {
     size_t sorted, other, counts, part, bytes;
 };
 Layout layout_of(int64_t tokens, int64_t cols) {
     Layout w{};
     const size_t pairs = up256((size_t)tokens * sizeof(uint2));
+    const bool digits = tokens > kRankMost;
     w.other = pairs;
-    w.counts = tokens > kRankMost ? 2 * pairs : pairs;
-    w.part = w.counts + (tokens > kRankMost ? (size_t)((tokens + kTile - 1) / kTile) * kDigits * 4 : 0);
+    w.counts = digits ? 2 * pairs : pairs;
+    w.part = w.counts + (tokens > kSelfMost ? (size_t)tiles_of(tokens) * kDigits * 4 : 0);
     w.bytes = w.part + up256((size_t)(tokens / kChunk) * cols * 4);
     return w;
 }
 
-template <bool FIRST, bool I64>
+template <int Q, bool SELF, bool FIRST, bool I64>
 void digit_pass(const EmbeddingArgs& a, int shift, const uint2* in, uint32_t* counts, uint2* out, hipStream_t s) {
-    const dim3 grid((unsigned)((a.tokens + kTile - 1) / kTile)), block(kSortThreads);
-    hipLaunchKernelGGL((digit_count_kernel<FIRST, I64>), grid, block, 0, s, a.tokens, (uint32_t)a.vocab, shift, a.ids,
-                       in, counts);
-    hipLaunchKernelGGL((digit_place_kernel<FIRST, I64>), grid, block, 0, s, a.tokens, (uint32_t)a.vocab, shift, a.ids,
-                       in, counts, out);
+    const dim3 grid((unsigned)tiles_of(a.tokens)), block(kSortThreads);
+    if constexpr (!SELF)
+        hipLaunchKernelGGL((digit_count_kernel<Q, FIRST, I64>), grid, block, 0, s, a.tokens, (uint32_t)a.vocab, shift,
+                           a.ids, in, counts);
+    hipLaunchKernelGGL((digit_place_kernel<Q, SELF, FIRST, I64>), grid, block, 0, s, a.tokens, (uint32_t)a.vocab,
+                       shift, a.ids, in, counts, out);
 }
 
 // The sorted pairs, in one of the two arrays.
+template <int Q, bool SELF, bool I64>
+const uint2* sort_digits(const EmbeddingArgs& a, uint2* to, uint2* other, uint32_t* counts, hipStream_t s) {
+    const int passes = digit_passes(a.vocab);
+    digit_pass<Q, SELF, true, I64>(a, 0, nullptr, counts, to, s);
+    for (int p = 1; p < passes; ++p) {
+        digit_pass<Q, SELF, false, I64>(a, p * kDigitBits, to, counts, other, s);
+        std::swap(to, other);
+    }
+    return to;
+}
+
 template <bool I64>
 const uint2* sort(const EmbeddingArgs& a, const Layout& w, hipStream_t s) {
     uint8_t* ws = (uint8_t*)a.workspace;
@@ -404,15 +445,9 @@ const uint2* sort(const EmbeddingArgs& a, const Layout& w, hipStream_t s) {
     }
     uint2* other = (uint2*)(ws + w.other);
     uint32_t* counts = (uint32_t*)(ws + w.counts);
-    const int passes = digit_passes(a.vocab);
-    digit_pass<true, I64>(a, 0, nullptr, counts, to, s);
-    for (int p = 1; p < passes; ++p) {
-        digit_pass<false, I64>(a, p * kDigitBits, to, counts, other, s);
-        uint2* t = to;
-        to = other;
-        other = t;
-    }
-    return to;
+    if (a.tokens <= kSelfMost) return sort_digits<2, true, I64>(a, to, other, counts, s);
+    return a.tokens <= kShortMost ? sort_digits<2, false, I64>(a, to, other, counts, s)
+                                  : sort_digits<8, false, I64>(a, to, other, counts, s);
 }
 
 template <typename T, typename G, int TL>
