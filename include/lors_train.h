@@ -145,7 +145,7 @@ typedef enum lors_index_dtype {
 
 /*
  * tokens >= 0, vocab >= 1, cols >= 1, each < 2^31, scale finite; otherwise
- * LORS_ERR_SHAPE; the backward takes ceil(cols / 512) . max(vocab / 8, tokens / 32) < 2^31,
+ * LORS_ERR_SHAPE; the backward takes ceil(cols / 256) . max(vocab / 8, tokens / 32) < 2^31,
  * otherwise LORS_ERR_UNSUPPORTED.  Ids outside 0 .. vocab - 1 stand for no token (padding): their
  * row of Y is zero and they have no part in the gradient.
  * grad_dtype: the type of dE.
@@ -182,7 +182,7 @@ lors_status_t lors_embedding_backward(const lors_embedding_t* p, const void* ids
  * token t of sequence b is element b . batch_stride + t . row_stride + v.  Targets,
  * log-probabilities and the like are batch x length, contiguous.
  * batch, length >= 0, batch . length < 2^31, 1 <= vocab < 2^31, strides >= 0;
- * otherwise LORS_ERR_SHAPE.  (batch . length) . ceil(vocab / 8192) < 2^31, otherwise
+ * otherwise LORS_ERR_SHAPE.  (batch . length) . ceil(vocab / 4096) < 2^31, otherwise
  * LORS_ERR_UNSUPPORTED.
  * A target outside 0 .. vocab - 1 (a prompt's or padding's, -100) does not count:
  * its log-probability and gradient are 0, and its row of logits is not read.

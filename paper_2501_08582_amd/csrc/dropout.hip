@@ -14,6 +14,7 @@ template <typename T>
 __global__ __launch_bounds__(NT) void dropout_kernel(int64_t rows, uint32_t cols, uint32_t units, DropArgs drop,
                                                      const T* __restrict__ X, const T* __restrict__ residual,
                                                      T* __restrict__ Y) {
+    constexpr int N = kUnit<T>;
     const Dropper d(drop);
     // Units in row-major order, a grid's worth apart: one division, then steps.
     const uint32_t stride = gridDim.x * NT;
@@ -25,13 +26,13 @@ __global__ __launch_bounds__(NT) void dropout_kernel(int64_t rows, uint32_t cols
         int64_t at[kAhead];
         uint32_t row[kAhead], unit[kAhead];
         int left[kAhead];
-        Raw<T> x[kAhead], r[kAhead];
+        Raw<T, N> x[kAhead], r[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            at[i] = n * cols + (int64_t)g * kUnit;
+            at[i] = n * cols + (int64_t)g * N;
             row[i] = (uint32_t)n;
             unit[i] = g;
-            left[i] = n < rows ? (int)min(cols - g * kUnit, (uint32_t)kUnit) : 0;
+            left[i] = n < rows ? (int)min(cols - g * N, (uint32_t)N) : 0;
             if (left[i] > 0) {
                 x[i] = load_unit(X + at[i], left[i]);
                 if (residual != nullptr) r[i] = load_unit(residual + at[i], left[i]);
@@ -46,12 +47,12 @@ __global__ __launch_bounds__(NT) void dropout_kernel(int64_t rows, uint32_t cols
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (left[i] <= 0) break;
-            F8 f = widen(x[i]);
+            F<N> f = widen(x[i]);
             d.apply(f, row[i], unit[i]);
             if (residual != nullptr) {
-                const F8 q = widen(r[i]);
+                const F<N> q = widen(r[i]);
 #pragma unroll
-                for (int e = 0; e < kUnit; ++e) f.v[e] += q.v[e];
+                for (int e = 0; e < N; ++e) f.v[e] += q.v[e];
             }
             store_unit(Y + at[i], narrow<T>(f), left[i]);
         }
@@ -60,8 +61,8 @@ __global__ __launch_bounds__(NT) void dropout_kernel(int64_t rows, uint32_t cols
 
 template <typename T>
 hipError_t launch(const DropoutArgs& a, hipStream_t s) {
-    const uint32_t units = (uint32_t)((a.cols + kUnit - 1) / kUnit);
-    // rows and units are below 2^31 and 2^28: their product fits
+    const uint32_t units = (uint32_t)((a.cols + kUnit<T> - 1) / kUnit<T>);
+    // rows and units are below 2^31 and 2^29: their product fits
     const int64_t blocks = (a.rows * units + NT - 1) / NT;
     const int64_t most = 16 * (int64_t)256;
     hipLaunchKernelGGL(dropout_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(NT), 0, s, a.rows,

@@ -38,6 +38,7 @@ template <typename T, bool I64>
 __global__ __launch_bounds__(NT) void lookup_kernel(int64_t tokens, uint32_t vocab, uint32_t cols, uint32_t units,
                                                     float scale, const void* __restrict__ ids,
                                                     const T* __restrict__ E, T* __restrict__ Y) {
+    constexpr int N = kUnit<T>;
     // units in row-major order, a grid's worth apart: one division, then steps
     const uint32_t stride = gridDim.x * NT;
     const uint32_t step_rows = stride / units, step_units = stride - step_rows * units;
@@ -48,12 +49,12 @@ __global__ __launch_bounds__(NT) void lookup_kernel(int64_t tokens, uint32_t voc
         int64_t at[kAhead];
         uint32_t id[kAhead], col[kAhead];
         int left[kAhead];
-        Raw<T> x[kAhead];
+        Raw<T, N> x[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            col[i] = g * kUnit;
+            col[i] = g * N;
             at[i] = n * cols + col[i];
-            left[i] = n < tokens ? (int)min(cols - col[i], (uint32_t)kUnit) : 0;
+            left[i] = n < tokens ? (int)min(cols - col[i], (uint32_t)N) : 0;
             id[i] = n < tokens ? id_of<I64>(ids, n, vocab) : vocab;
             n += step_rows;
             g += step_units;
@@ -64,16 +65,16 @@ __global__ __launch_bounds__(NT) void lookup_kernel(int64_t tokens, uint32_t voc
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            x[i] = Raw<T>{};
+            x[i] = Raw<T, N>{};
             if (id[i] < vocab) x[i] = load_unit(E + (int64_t)id[i] * cols + col[i], left[i]);
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (left[i] <= 0) break;
-            F8 f = widen(x[i]);
+            F<N> f = widen(x[i]);
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) f.v[e] *= scale;
-            if (id[i] >= vocab) f = F8{};
+            for (int e = 0; e < N; ++e) f.v[e] *= scale;
+            if (id[i] >= vocab) f = F<N>{};
             store_unit(Y + at[i], narrow<T>(f), left[i]);
         }
     }
@@ -287,62 +288,64 @@ constexpr uint32_t kRows = 8;    // rows of the table per group
 template <typename T>
 constexpr int kBatch = sizeof(T) == 2 ? 16 : 8;  // rows of dY in flight
 
-// acc += the dY units of tokens sorted[pos .. pos + n), n <= kBatch, in order.
-template <typename T>
-__device__ __forceinline__ void add_tokens(F8& acc, const uint2 (&pair)[kBatch<T>], int n, const T* __restrict__ dY,
+// acc += the units of dY's tokens pair[0 .. n), n <= kBatch, in order.
+template <typename T, int N>
+__device__ __forceinline__ void add_tokens(F<N>& acc, const uint2 (&pair)[kBatch<T>], int n, const T* __restrict__ dY,
                                            int64_t cols, int64_t col, int left) {
-    Raw<T> r[kBatch<T>];
+    Raw<T, N> r[kBatch<T>];
 #pragma unroll
     for (int i = 0; i < kBatch<T>; ++i)
-        if (i < n) r[i] = load_unit(dY + (int64_t)pair[i].y * cols + col, left);
+        if (i < n) r[i] = load_unit<T, N>(dY + (int64_t)pair[i].y * cols + col, left);
 #pragma unroll
     for (int i = 0; i < kBatch<T>; ++i)
         if (i < n) {
-            const F8 f = widen(r[i]);
+            const F<N> f = widen(r[i]);
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) acc.v[e] += f.v[e];
+            for (int e = 0; e < N; ++e) acc.v[e] += f.v[e];
         }
 }
 
 // Sums of the chunks that belong to one id as a whole.
-template <typename T, int TL>
+template <typename T, int N, int TL>
 __global__ __launch_bounds__(NT) void chunk_kernel(uint32_t chunks, uint32_t vocab, int64_t cols, uint32_t tiles,
                                                    const uint2* __restrict__ sorted, const T* __restrict__ dY,
                                                    float* __restrict__ part) {
     const uint32_t group = block_id() * (NT / TL) + uniform<TL>(threadIdx.x / TL);
     const uint32_t chunk = group / tiles;
     if (chunk >= chunks) return;
-    const int64_t col = ((int64_t)(group - chunk * tiles) * TL + threadIdx.x % TL) * kUnit;
-    const int left = (int)min(cols - col, (int64_t)kUnit);
+    const int64_t col = ((int64_t)(group - chunk * tiles) * TL + threadIdx.x % TL) * N;
+    const int left = (int)min(cols - col, (int64_t)N);
     const uint2* s = sorted + (int64_t)chunk * kChunk;
     uint2 pair[kChunk / kBatch<T>][kBatch<T>];  // all at once: a chunk is two waits on memory
 #pragma unroll
     for (uint32_t i = 0; i < kChunk; ++i) pair[i / kBatch<T>][i % kBatch<T>] = s[i];
     const uint32_t id = pair[0][0].x;
     if (left <= 0 || id != pair[kChunk / kBatch<T> - 1][kBatch<T> - 1].x || id >= vocab) return;
-    F8 acc = {};
+    F<N> acc = {};
 #pragma unroll
-    for (uint32_t b = 0; b < kChunk / kBatch<T>; ++b) add_tokens<T>(acc, pair[b], kBatch<T>, dY, cols, col, left);
+    for (uint32_t b = 0; b < kChunk / kBatch<T>; ++b) add_tokens(acc, pair[b], kBatch<T>, dY, cols, col, left);
     store_unit(part + chunk * cols + col, narrow<float>(acc), left);
 }
 
+// The lanes' units are those of what they write: N elements of G are 16 bytes.
 template <typename T, typename G, int TL>
 __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t vocab, int64_t cols, uint32_t tiles,
                                                   float scale, const uint2* __restrict__ sorted,
                                                   const T* __restrict__ dY, const float* __restrict__ part,
                                                   G* __restrict__ dE) {
+    constexpr int N = kUnit<G>;
     const uint32_t group = block_id() * (NT / TL) + uniform<TL>(threadIdx.x / TL);
     const uint32_t v0 = group / tiles * kRows;
     if (v0 >= vocab) return;
-    int64_t col = ((int64_t)(group % tiles) * TL + threadIdx.x % TL) * kUnit;
+    int64_t col = ((int64_t)(group % tiles) * TL + threadIdx.x % TL) * N;
     // lanes past the row stay (the search needs them): they read its first unit
     const bool real = col < cols;
     if (!real) col = 0;
-    const int left = (int)min(cols - col, (int64_t)kUnit);
+    const int left = (int)min(cols - col, (int64_t)N);
     uint32_t pos = lower_bound<TL>(sorted, tokens, v0);
     uint32_t next = pos < tokens ? uniform<TL>(sorted[pos].x) : ~0u;
     for (uint32_t v = v0; v < min(v0 + kRows, vocab); ++v) {
-        F8 acc = {};
+        F<N> acc = {};
         while (next == v) {
             if (pos % kChunk == 0 && tokens - pos >= kChunk && sorted[pos + kChunk - 1].x == v) {
                 // whole chunks of a frequent token: their sums are there
@@ -350,9 +353,9 @@ __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t voca
                 const float* p = part + (int64_t)(pos / kChunk) * cols + col;
 #pragma unroll 8
                 for (uint32_t i = 0; i < n; ++i) {
-                    const F8 f = widen(load_unit(p + i * cols, left));
+                    const F<N> f = widen(load_unit<float, N>(p + i * cols, left));
 #pragma unroll
-                    for (int e = 0; e < kUnit; ++e) acc.v[e] += f.v[e];
+                    for (int e = 0; e < N; ++e) acc.v[e] += f.v[e];
                 }
                 pos += n * kChunk;
             } else {
@@ -365,14 +368,14 @@ __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t voca
                     pair[i] = i < room ? sorted[pos + i] : uint2{~0u, 0u};
                     n += pair[i].x == v;
                 }
-                add_tokens<T>(acc, pair, n, dY, cols, col, left);
+                add_tokens(acc, pair, n, dY, cols, col, left);
                 pos += n;
             }
             next = pos < tokens ? uniform<TL>(sorted[pos].x) : ~0u;
         }
 #pragma unroll
-        for (int e = 0; e < kUnit; ++e) acc.v[e] *= scale;
-        if (real) store_unit(dE + (int64_t)v * cols + col, narrow<G>(acc), left);
+        for (int e = 0; e < N; ++e) acc.v[e] *= scale;
+        if (real) stream_unit(dE + (int64_t)v * cols + col, narrow<G>(acc), left);
     }
 }
 
@@ -453,13 +456,14 @@ const uint2* sort(const EmbeddingArgs& a, const Layout& w, hipStream_t s) {
 template <typename T, typename G, int TL>
 hipError_t sums(const EmbeddingArgs& a, const uint2* sorted, float* part, hipStream_t s) {
     // fewer groups than 2^32: checked where the call is
-    const uint32_t tiles = (uint32_t)((a.cols + TL * kUnit - 1) / (TL * kUnit));
+    constexpr int N = kUnit<G>;
+    const uint32_t tiles = (uint32_t)((a.cols + TL * N - 1) / (TL * N));
     const uint32_t chunks = (uint32_t)(a.tokens / kChunk);
     const int64_t per = NT / TL;
     const int64_t chunk_blocks = ((int64_t)chunks * tiles + per - 1) / per;
     const int64_t row_blocks = ((a.vocab + kRows - 1) / kRows * tiles + per - 1) / per;
     if (chunks > 0)
-        hipLaunchKernelGGL((chunk_kernel<T, TL>), grid_of(chunk_blocks), dim3(NT), 0, s, chunks,
+        hipLaunchKernelGGL((chunk_kernel<T, N, TL>), grid_of(chunk_blocks), dim3(NT), 0, s, chunks,
                            (uint32_t)a.vocab, a.cols, tiles, sorted, (const T*)a.dY, part);
     hipLaunchKernelGGL((rows_kernel<T, G, TL>), grid_of(row_blocks), dim3(NT), 0, s, (uint32_t)a.tokens,
                        (uint32_t)a.vocab, a.cols, tiles, a.scale, sorted, (const T*)a.dY, part, (G*)a.dE);
@@ -472,7 +476,7 @@ hipError_t backward(const EmbeddingArgs& a, hipStream_t s) {
     const uint2* sorted = nullptr;
     if (a.tokens > 0) sorted = a.index64 ? sort<true>(a, w, s) : sort<false>(a, w, s);
     float* part = (float*)((uint8_t*)a.workspace + w.part);
-    const int64_t units = (a.cols + kUnit - 1) / kUnit;
+    const int64_t units = (a.cols + kUnit<G> - 1) / kUnit<G>;
     if (units <= 8) return sums<T, G, 8>(a, sorted, part, s);
     if (units <= 16) return sums<T, G, 16>(a, sorted, part, s);
     return sums<T, G, 64>(a, sorted, part, s);
@@ -480,7 +484,7 @@ hipError_t backward(const EmbeddingArgs& a, hipStream_t s) {
 
 template <typename T>
 hipError_t forward(const EmbeddingArgs& a, hipStream_t s) {
-    const uint32_t units = (uint32_t)((a.cols + kUnit - 1) / kUnit);
+    const uint32_t units = (uint32_t)((a.cols + kUnit<T> - 1) / kUnit<T>);
     const int64_t blocks = (a.tokens * units + NT - 1) / NT, most = 16 * (int64_t)256;
     const dim3 grid((unsigned)(blocks < most ? blocks : most));
     if (a.index64)
@@ -496,7 +500,7 @@ hipError_t forward(const EmbeddingArgs& a, hipStream_t s) {
 
 bool embedding_groups_fit(int64_t tokens, int64_t vocab, int64_t cols) {
     const int64_t rows = std::max((vocab + kRows - 1) / kRows, tokens / kChunk);
-    return (cols + 64 * kUnit - 1) / (64 * kUnit) * rows < (int64_t)1 << 31;  // narrower groups have one tile
+    return (cols + 255) / 256 * rows < (int64_t)1 << 31;  // tiles of 256 columns at least; narrower groups have one
 }
 
 size_t embedding_workspace_bytes(int64_t tokens, int64_t, int64_t cols) { return layout_of(tokens, cols).bytes; }

@@ -13,7 +13,7 @@ constexpr int kMaxWaves = 1024 / 64;
 
 // The lanes that share a row.  LPR (8 .. 64): that many lanes of a wave; the
 // workgroup of 256 threads takes 256 / LPR rows at once.  LPR = 0: the whole
-// workgroup.  V units per lane; lane i of the row holds units i, i + lanes, ..
+// workgroup.  Lane i of a row holds its units i, i + lanes, ..
 template <int LPR>
 struct RowLanes {
     int lanes, slot, slots, lane;
@@ -32,23 +32,23 @@ struct RowLanes {
     }
 };
 
-// Sums of N values over the lanes of a row, in each of them.  `lds`: kMaxWaves
+// Sums of K values over the lanes of a row, in each of them.  `lds`: kMaxWaves
 // floats per value, which no wave may still read from an earlier call.
-template <int LPR, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[kMaxWaves]) {
+template <int LPR, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float (*lds)[kMaxWaves]) {
     if constexpr (LPR != 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = over_lanes<LPR>(v[i], Add());
+        for (int i = 0; i < K; ++i) v[i] = over_lanes<LPR>(v[i], Add());
     } else {
         const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+        for (int i = 0; i < K; ++i) {
             v[i] = over_lanes<64>(v[i], Add());
             if ((threadIdx.x & 63) == 0) lds[i][wave] = v[i];
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+        for (int i = 0; i < K; ++i) {
             float sum = 0.f;
             for (int w = 0; w < waves; ++w) sum += lds[i][w];
             v[i] = sum;
@@ -57,40 +57,49 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[kMaxWaves])
 }
 
 template <typename T, int LPR, int V, int NT>
-__global__ __launch_bounds__(NT) void norm_fwd_kernel(
-    int64_t rows, int cols, float eps, bool rms, DropArgs drop, const T* __restrict__ X,
-    const T* __restrict__ residual, const T* __restrict__ weight, const T* __restrict__ bias, T* __restrict__ Y,
-    T* __restrict__ Z, float* __restrict__ mean, float* __restrict__ rstd) {
+__global__ __launch_bounds__(NT) void norm_fwd_kernel(int64_t rows, int cols, float eps, bool rms, DropArgs drop,
+                                                      const T* __restrict__ X, const T* __restrict__ residual,
+                                                      const T* __restrict__ weight, const T* __restrict__ bias,
+                                                      T* __restrict__ Y, T* __restrict__ Z, float* __restrict__ mean,
+                                                      float* __restrict__ rstd) {
+    constexpr int N = kUnit<T>;
     __shared__ float lds[2][1][kMaxWaves];
     const RowLanes<LPR> me;
     const int64_t n = (int64_t)block_id() * me.slots + me.slot;
     if (n >= rows) return;  // whole rows: no barrier follows for LPR != 0, and all lanes agree for LPR = 0
+    const Dropper dropper(drop);
     const int64_t base = n * cols;
-    F8 z[V];
+    Raw<T, N> x[V], r[V];
+    F<N> z[V];
     int left[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int c = (me.lane + i * me.lanes) * N;
+        left[i] = min(cols - c, N);
+        if (left[i] <= 0) continue;
+        x[i] = load_unit(X + base + c, left[i]);
+        if (residual != nullptr) r[i] = load_unit(residual + base + c, left[i]);
+    }
     float sum[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int c = (me.lane + i * me.lanes) * kUnit;
-        left[i] = min(cols - c, kUnit);
         if (left[i] <= 0) continue;
-        z[i] = widen(load_unit(X + base + c, left[i]));
-        Raw<T> q;
-        if (residual != nullptr) q = load_unit(residual + base + c, left[i]);
-        if (drop.below != 0) Dropper(drop).apply(z[i], (uint32_t)n, (uint32_t)(c / kUnit));
+        const int c = (me.lane + i * me.lanes) * N;
+        z[i] = widen(x[i]);
+        if (drop.below != 0) dropper.apply(z[i], (uint32_t)n, (uint32_t)(c / N));
         if (residual != nullptr) {
-            const F8 f = widen(q);
+            const F<N> f = widen(r[i]);
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) z[i].v[e] += f.v[e];
+            for (int e = 0; e < N; ++e) z[i].v[e] += f.v[e];
         }
         if (Z != nullptr) {
             // the sum is what the residual stream stores: normalise that
-            const Raw<T> r = narrow<T>(z[i]);
-            store_unit(Z + base + c, r, left[i]);
-            z[i] = widen(r);
+            const Raw<T, N> q = narrow<T>(z[i]);
+            store_unit(Z + base + c, q, left[i]);
+            z[i] = widen(q);
         }
 #pragma unroll
-        for (int e = 0; e < kUnit; ++e) sum[0] += rms ? z[i].v[e] * z[i].v[e] : z[i].v[e];  // 0 past the row
+        for (int e = 0; e < N; ++e) sum[0] += rms ? z[i].v[e] * z[i].v[e] : z[i].v[e];  // 0 past the row
     }
     row_sums<LPR>(sum, lds[0]);
     float mu = 0.f, sq = sum[0];
@@ -101,7 +110,7 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(
         for (int i = 0; i < V; ++i)
             if (left[i] > 0)
 #pragma unroll
-                for (int e = 0; e < kUnit; ++e)
+                for (int e = 0; e < N; ++e)
                     if (e < left[i]) dev[0] += (z[i].v[e] - mu) * (z[i].v[e] - mu);
         row_sums<LPR>(dev, lds[1]);
         sq = dev[0];
@@ -114,132 +123,164 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         if (left[i] <= 0) continue;
-        const int c = (me.lane + i * me.lanes) * kUnit;
-        F8 y;
+        const int c = (me.lane + i * me.lanes) * N;
+        F<N> y;
 #pragma unroll
-        for (int e = 0; e < kUnit; ++e) y.v[e] = (z[i].v[e] - mu) * scale;
+        for (int e = 0; e < N; ++e) y.v[e] = (z[i].v[e] - mu) * scale;
         if (weight != nullptr) {
-            const F8 w = widen(load_unit(weight + c, left[i]));
+            const F<N> w = widen(load_unit(weight + c, left[i]));
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) y.v[e] *= w.v[e];
+            for (int e = 0; e < N; ++e) y.v[e] *= w.v[e];
         }
         if (bias != nullptr) {
-            const F8 b = widen(load_unit(bias + c, left[i]));
+            const F<N> b = widen(load_unit(bias + c, left[i]));
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) y.v[e] += b.v[e];
+            for (int e = 0; e < N; ++e) y.v[e] += b.v[e];
         }
         store_unit(Y + base + c, narrow<T>(y), left[i]);
     }
 }
 
-template <typename T>
-__device__ __forceinline__ Raw<T> ones() {
-    F8 f;
-#pragma unroll
-    for (int e = 0; e < kUnit; ++e) f.v[e] = 1.f;
-    return narrow<T>(f);
-}
-
 // A workgroup's sums, one per column, to `out`: those of its slots are added up
 // in LDS first.
-template <int LPR, int V>
-__device__ __forceinline__ void put_row(const RowLanes<LPR>& me, F8 (&sum)[V], const int (&left)[V],
+template <int LPR, int V, int N>
+__device__ __forceinline__ void put_row(const RowLanes<LPR>& me, F<N> (&sum)[V], const int (&left)[V],
                                         float* __restrict__ out) {
     if constexpr (LPR != 0) {
-        __shared__ float lds[kUnit][256];
+        __shared__ float lds[N][256];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) lds[e][threadIdx.x] = sum[i].v[e];
+            for (int e = 0; e < N; ++e) lds[e][threadIdx.x] = sum[i].v[e];
             __syncthreads();
             if (me.slot == 0)
                 for (int k = 1; k < 256 / LPR; ++k)
 #pragma unroll
-                    for (int e = 0; e < kUnit; ++e) sum[i].v[e] += lds[e][k * LPR + me.lane];
+                    for (int e = 0; e < N; ++e) sum[i].v[e] += lds[e][k * LPR + me.lane];
         }
         if (me.slot != 0) return;
     }
 #pragma unroll
     for (int i = 0; i < V; ++i)
-        if (left[i] > 0) store_unit(out + (me.lane + i * me.lanes) * kUnit, narrow<float>(sum[i]), left[i]);
+        if (left[i] > 0) store_unit(out + (me.lane + i * me.lanes) * N, narrow<float>(sum[i]), left[i]);
 }
 
 // The gradients.  A workgroup takes every gridDim.x-th group of rows and keeps its
 // sums of dweight and dbias in registers; they leave as one partial row per
 // workgroup, which a second launch adds up in a fixed order.
-template <typename T, int LPR, int V, int NT>
-__global__ __launch_bounds__(NT) void norm_bwd_kernel(
-    int64_t rows, int cols, bool rms, DropArgs drop, const T* __restrict__ dY, const T* __restrict__ dZ,
-    const T* __restrict__ Z, const T* __restrict__ weight, const float* __restrict__ mean,
-    const float* __restrict__ rstd, T* __restrict__ dX, T* __restrict__ dresidual, float* __restrict__ part,
-    bool want_dw, bool want_db) {
+// AHEAD: the next row is loaded before this one's sums are joined, so that memory
+// works through the barrier.  Without it (rows so wide that the registers do not
+// hold two) a row's second half reads it again out of the cache.
+template <typename T, int LPR, int V, int NT, bool AHEAD>
+__global__ __launch_bounds__(NT) void norm_bwd_kernel(int64_t rows, int cols, bool rms, DropArgs drop,
+                                                      const T* __restrict__ dY, const T* __restrict__ dZ,
+                                                      const T* __restrict__ Z, const T* __restrict__ weight,
+                                                      const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                      T* __restrict__ dX, T* __restrict__ dresidual,
+                                                      float* __restrict__ part, bool want_dw, bool want_db) {
+    constexpr int N = kUnit<T>;
+    constexpr int H = AHEAD ? V : 1;  // units that are held
     __shared__ float lds[2][2][kMaxWaves];
     const RowLanes<LPR> me;
-    F8 dw[V] = {}, db[V] = {};
-    Raw<T> w[V];
+    const Dropper dropper(drop);
+    const int64_t step = (int64_t)gridDim.x * me.slots;
+    F<N> dw[V] = {}, db[V] = {};
     int left[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int c = (me.lane + i * me.lanes) * kUnit;
-        left[i] = min(cols - c, kUnit);
-        w[i] = ones<T>();
-        if (weight != nullptr && left[i] > 0) w[i] = load_unit(weight + c, left[i]);
-    }
-    int turn = 0;
-    for (int64_t n = (int64_t)blockIdx.x * me.slots + me.slot; n < rows; n += (int64_t)gridDim.x * me.slots) {
-        const int64_t base = n * cols;
-        const float mu = rms ? 0.f : mean[n], scale = rstd[n];
-        Raw<T> z[V], y[V], q[V];
+    for (int i = 0; i < V; ++i) left[i] = min(cols - (me.lane + i * me.lanes) * N, N);
+    auto column = [&](int i) { return (me.lane + i * me.lanes) * N; };
+    auto weights = [&](int i) {
+        if (weight == nullptr || left[i] <= 0) {
+            F<N> one;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = (me.lane + i * me.lanes) * kUnit;
-            if (left[i] <= 0) continue;
-            z[i] = load_unit(Z + base + c, left[i]);
-            y[i] = load_unit(dY + base + c, left[i]);
-            if (dZ != nullptr) q[i] = load_unit(dZ + base + c, left[i]);
+            for (int e = 0; e < N; ++e) one.v[e] = 1.f;
+            return narrow<T>(one);
         }
+        return load_unit(weight + column(i), left[i]);
+    };
+    struct Row {
+        Raw<T, N> z[H], y[H], q[H];
+        float mu, scale;
+    };
+    auto load = [&](Row& r, int h, int i, int64_t n) {
+        const int64_t at = n * cols + column(i);
+        if (left[i] <= 0) return;
+        r.z[h] = load_unit(Z + at, left[i]);
+        r.y[h] = load_unit(dY + at, left[i]);
+        if (dZ != nullptr) r.q[h] = load_unit(dZ + at, left[i]);
+    };
+    auto load_row = [&](Row& r, int64_t n) {
+        r.mu = rms ? 0.f : mean[n];
+        r.scale = rstd[n];
+        if constexpr (AHEAD)
+#pragma unroll
+            for (int i = 0; i < V; ++i) load(r, i, i, n);
+    };
+    Raw<T, N> w[H];
+    if constexpr (AHEAD)
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] = weights(i);
+    Row now, next;
+    int64_t n = (int64_t)blockIdx.x * me.slots + me.slot;
+    if (n < rows) load_row(now, n);
+    for (int turn = 0; n < rows; turn ^= 1) {
+        if (AHEAD && n + step < rows) load_row(next, n + step);
         float sums[2] = {0.f, 0.f};  // of g, and of g h
 #pragma unroll
         for (int i = 0; i < V; ++i) {
+            const int h = AHEAD ? i : 0;
+            if constexpr (!AHEAD) {
+                __builtin_amdgcn_sched_barrier(0);  // one unit after the other: the registers hold no more
+                load(now, 0, i, n);
+                w[0] = weights(i);
+            }
             if (left[i] <= 0) continue;
-            const F8 fz = widen(z[i]), fy = widen(y[i]), fw = widen(w[i]);
+            const F<N> fz = widen(now.z[h]), fy = widen(now.y[h]), fw = widen(w[h]);
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) {
-                const float h = (fz.v[e] - mu) * scale, g = fy.v[e] * fw.v[e];  // dY is 0 past the row
+            for (int e = 0; e < N; ++e) {
+                const float hat = (fz.v[e] - now.mu) * now.scale, g = fy.v[e] * fw.v[e];  // dY is 0 past the row
                 sums[0] += g;
-                sums[1] += g * h;
-                dw[i].v[e] += fy.v[e] * h;
+                sums[1] += g * hat;
+                dw[i].v[e] += fy.v[e] * hat;
                 db[i].v[e] += fy.v[e];
             }
         }
         row_sums<LPR>(sums, lds[turn]);
-        turn ^= 1;
         const float m1 = rms ? 0.f : sums[0] / (float)cols, m2 = sums[1] / (float)cols;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
+            const int h = AHEAD ? i : 0;
+            if constexpr (!AHEAD) {
+                __builtin_amdgcn_sched_barrier(0);  // one unit after the other: the registers hold no more
+                load(now, 0, i, n);
+                w[0] = weights(i);
+            }
             if (left[i] <= 0) continue;
-            const int c = (me.lane + i * me.lanes) * kUnit;
-            const F8 fz = widen(z[i]), fy = widen(y[i]), fw = widen(w[i]);
-            F8 d;
+            const int64_t at = n * cols + column(i);
+            const F<N> fz = widen(now.z[h]), fy = widen(now.y[h]), fw = widen(w[h]);
+            F<N> d;
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) {
-                const float h = (fz.v[e] - mu) * scale, g = fy.v[e] * fw.v[e];
-                d.v[e] = scale * (g - m1 - h * m2);
+            for (int e = 0; e < N; ++e) {
+                const float hat = (fz.v[e] - now.mu) * now.scale, g = fy.v[e] * fw.v[e];
+                d.v[e] = now.scale * (g - m1 - hat * m2);
             }
             if (dZ != nullptr) {
-                const F8 f = widen(q[i]);
+                const F<N> f = widen(now.q[h]);
 #pragma unroll
-                for (int e = 0; e < kUnit; ++e) d.v[e] += f.v[e];
+                for (int e = 0; e < N; ++e) d.v[e] += f.v[e];
             }
-            if (dresidual != nullptr) store_unit(dresidual + base + c, narrow<T>(d), left[i]);
-            if (drop.below != 0) Dropper(drop).apply(d, (uint32_t)n, (uint32_t)(c / kUnit));
-            store_unit(dX + base + c, narrow<T>(d), left[i]);
+            if (dresidual != nullptr) store_unit(dresidual + at, narrow<T>(d), left[i]);
+            if (drop.below != 0) dropper.apply(d, (uint32_t)n, (uint32_t)(column(i) / N));
+            store_unit(dX + at, narrow<T>(d), left[i]);
         }
+        n += step;
+        if constexpr (AHEAD) now = next;
+        else if (n < rows) load_row(now, n);
     }
     // one row of dweight per workgroup, then as many of dbias
-    if (want_dw) put_row<LPR, V>(me, dw, left, part + (int64_t)blockIdx.x * cols);
-    if (want_db) put_row<LPR, V>(me, db, left, part + (int64_t)((want_dw ? gridDim.x : 0) + blockIdx.x) * cols);
+    if (want_dw) put_row(me, dw, left, part + (int64_t)blockIdx.x * cols);
+    if (want_db) put_row(me, db, left, part + (int64_t)((want_dw ? gridDim.x : 0) + blockIdx.x) * cols);
 }
 
 // The sum of a column over the partial rows: 64 columns per workgroup, a part of
@@ -251,11 +292,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void norm_join_kernel(const float*
     __shared__ float lds[kJoinWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = blockIdx.x * 64 + lane;
-    const float* p = part + (int64_t)blockIdx.y * prows * cols + c;
+    const float* p = part + (int64_t)blockIdx.y * prows * cols + min(c, cols - 1);
     void* out = dweight == nullptr || blockIdx.y == 1 ? dbias : dweight;
     float sum = 0.f;
-    if (c < cols)
-        for (int r = wave; r < prows; r += kJoinWaves) sum += p[(int64_t)r * cols];
+#pragma unroll 8
+    for (int r = wave; r < prows; r += kJoinWaves) sum += p[(int64_t)r * cols];
     lds[wave][lane] = sum;
     __syncthreads();
     if (wave != 0 || c >= cols) return;
@@ -273,14 +314,15 @@ struct Plan {
     int lpr, v, most, threads;
 };
 
-Plan plan_of(int64_t cols) {
-    const int units = (int)((cols + kUnit - 1) / kUnit);
+Plan plan_of(int64_t cols, bool bf16) {
+    const int per = bf16 ? kUnit<__bf16> : kUnit<float>;
+    const int units = (int)((cols + per - 1) / per);
     if (units <= 8) return {8, 1, 256, 256};
     if (units <= 16) return {16, 1, 256, 256};
     if (units <= 32) return {32, 1, 256, 256};
     if (units <= 64) return {64, 1, 256, 256};
     if (units <= 128) return {64, 2, 256, 256};
-    const int v = units <= 1024 ? 2 : 4;
+    const int v = units <= 1024 ? 2 : units <= 4096 ? 4 : 8;
     return {0, v, units <= 2048 ? 512 : 1024, ((units + v - 1) / v + 63) / 64 * 64};
 }
 
@@ -299,8 +341,8 @@ struct Held {
     static constexpr int lpr = LPR, v = V, nt = NT;
 };
 
-template <typename F>
-hipError_t with_plan(const Plan& p, F&& f) {
+template <typename T, typename Fn>
+hipError_t with_plan(const Plan& p, Fn&& f) {
     switch (p.lpr) {
         case 8: return f(Held<8, 1, 256>());
         case 16: return f(Held<16, 1, 256>());
@@ -309,32 +351,34 @@ hipError_t with_plan(const Plan& p, F&& f) {
         default: break;
     }
     if (p.v == 2) return f(Held<0, 2, 512>());
+    if constexpr (sizeof(T) == 4)
+        if (p.v == 8) return f(Held<0, 8, 1024>());
     return p.most == 512 ? f(Held<0, 4, 512>()) : f(Held<0, 4, 1024>());
 }
 
 template <typename T>
 hipError_t forward(const NormArgs& a, hipStream_t s) {
-    const Plan p = plan_of(a.cols);
-    return with_plan(p, [&](auto h) {
+    const Plan p = plan_of(a.cols, sizeof(T) == 2);
+    return with_plan<T>(p, [&](auto h) {
         using H = decltype(h);
         const int64_t rpg = rows_per_group(p);
-        hipLaunchKernelGGL((norm_fwd_kernel<T, H::lpr, H::v, H::nt>),
-                           grid_of((a.rows + rpg - 1) / rpg), dim3(p.threads), 0, s, a.rows, (int)a.cols,
-                           a.eps, a.rms, a.drop, (const T*)a.X, (const T*)a.residual, (const T*)a.weight,
-                           (const T*)a.bias, (T*)a.Y, (T*)a.Z, a.mean, a.rstd);
+        hipLaunchKernelGGL((norm_fwd_kernel<T, H::lpr, H::v, H::nt>), grid_of((a.rows + rpg - 1) / rpg),
+                           dim3(p.threads), 0, s, a.rows, (int)a.cols, a.eps, a.rms, a.drop, (const T*)a.X,
+                           (const T*)a.residual, (const T*)a.weight, (const T*)a.bias, (T*)a.Y, (T*)a.Z, a.mean,
+                           a.rstd);
         return hipGetLastError();
     });
 }
 
 template <typename T>
 hipError_t backward(const NormArgs& a, hipStream_t s) {
-    const Plan p = plan_of(a.cols);
+    const Plan p = plan_of(a.cols, sizeof(T) == 2);
     const int64_t groups = backward_groups(a.rows, p);
     const bool dw = a.dweight != nullptr, db = a.dbias != nullptr;
     if (groups > 0) {
-        const hipError_t e = with_plan(p, [&](auto h) {
+        const hipError_t e = with_plan<T>(p, [&](auto h) {
             using H = decltype(h);
-            hipLaunchKernelGGL((norm_bwd_kernel<T, H::lpr, H::v, H::nt>), dim3((unsigned)groups),
+            hipLaunchKernelGGL((norm_bwd_kernel<T, H::lpr, H::v, H::nt, H::v * kUnit<T> <= 16>), dim3((unsigned)groups),
                                dim3(p.threads), 0, s, a.rows, (int)a.cols, a.rms, a.drop, (const T*)a.dY,
                                (const T*)a.dZ, (const T*)a.Z, (const T*)a.weight, a.mean, a.rstd, (T*)a.dX,
                                (T*)a.dresidual, a.part, dw, db);
@@ -345,19 +389,18 @@ hipError_t backward(const NormArgs& a, hipStream_t s) {
     if (!dw && !db) return hipSuccess;
     const dim3 grid((unsigned)((a.cols + 63) / 64), dw && db ? 2 : 1);
     if (a.grad_bf16)
-        hipLaunchKernelGGL(norm_join_kernel<true>, grid, dim3(64 * kJoinWaves), 0, s, a.part, (int)groups, (int)a.cols,
-                           a.dweight, a.dbias);
+        hipLaunchKernelGGL(norm_join_kernel<true>, grid, dim3(64 * kJoinWaves), 0, s, a.part, (int)groups,
+                           (int)a.cols, a.dweight, a.dbias);
     else
-        hipLaunchKernelGGL(norm_join_kernel<false>, grid, dim3(64 * kJoinWaves), 0, s, a.part, (int)groups, (int)a.cols,
-                           a.dweight, a.dbias);
+        hipLaunchKernelGGL(norm_join_kernel<false>, grid, dim3(64 * kJoinWaves), 0, s, a.part, (int)groups,
+                           (int)a.cols, a.dweight, a.dbias);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t norm_workspace_bytes(int64_t rows, int64_t cols) {
-    const Plan p = plan_of(cols);
-    return (size_t)(2 * 4 * backward_groups(rows, p) * cols);
+size_t norm_workspace_bytes(int64_t rows, int64_t cols, bool bf16) {
+    return (size_t)(2 * 4 * backward_groups(rows, plan_of(cols, bf16)) * cols);
 }
 
 hipError_t launch_norm_forward(const NormArgs& a, bool bf16, hipStream_t s) {

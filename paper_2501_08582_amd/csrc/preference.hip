@@ -35,24 +35,25 @@ __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2
 struct Running {
     float top = kNone, sum = 0.f;
 
-    template <int N>
-    __device__ __forceinline__ void add(const F8 (&x)[N]) {
+    template <int B, int N>
+    __device__ __forceinline__ void add(const F<N> (&x)[B]) {
         float m = x[0].v[0];
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int i = 0; i < B; ++i)
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) m = fmaxf(m, x[i].v[e]);
+            for (int e = 0; e < N; ++e) m = fmaxf(m, x[i].v[e]);
         if (m > top) {
             sum = top == kNone ? 0.f : sum * exp2_hw((top - m) * kLog2e);
             top = m;
         }
         const float ref = top == kNone ? 0.f : top;  // all -Inf so far: they add nothing
-        float s[kUnit] = {};
+        float s[N] = {};
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int i = 0; i < B; ++i)
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) s[e] += exp2_hw((x[i].v[e] - ref) * kLog2e);
-        sum += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+            for (int e = 0; e < N; ++e) s[e] += exp2_hw((x[i].v[e] - ref) * kLog2e);
+        sum += (s[0] + s[1]) + (s[2] + s[3]);
+        if constexpr (N == 8) sum += (s[4] + s[5]) + (s[6] + s[7]);
     }
 
     __device__ __forceinline__ void rescale(float to) {
@@ -63,11 +64,12 @@ struct Running {
 
 // A row of logits in memory, and its last unit past the whole ones.
 template <typename T>
-__device__ __forceinline__ F8 logits_unit(const T* row, uint32_t u, uint32_t vocab) {
-    const int left = (int)min(vocab - u * kUnit, (uint32_t)kUnit);
-    F8 f = widen(load_unit(row + (int64_t)u * kUnit, left));
+__device__ __forceinline__ F<kUnit<T>> logits_unit(const T* row, uint32_t u, uint32_t vocab) {
+    constexpr int N = kUnit<T>;
+    const int left = (int)min(vocab - u * N, (uint32_t)N);
+    F<N> f = widen(load_unit(row + (int64_t)u * N, left));
 #pragma unroll
-    for (int e = 1; e < kUnit; ++e)
+    for (int e = 1; e < N; ++e)
         if (e >= left) f.v[e] = kNone;
     return f;
 }
@@ -99,6 +101,7 @@ template <typename T, bool I64>
 __global__ __launch_bounds__(NT) void logprob_fwd_kernel(Rows rows, uint32_t splits, const T* __restrict__ logits,
                                                          const void* __restrict__ targets, float* __restrict__ logp,
                                                          float2* __restrict__ stats, float2* __restrict__ part) {
+    constexpr int N = kUnit<T>;
     __shared__ float2 waves[NT / 64];
     const uint32_t n = block_id() / splits, split = block_id() - n * splits;
     if (n >= rows.count) return;
@@ -108,23 +111,23 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(Rows rows, uint32_t spl
         return;
     }
     const T* row = logits + rows.offset(n);
-    const uint32_t units = (rows.vocab + kUnit - 1) / kUnit, per = (units + splits - 1) / splits;
+    const uint32_t units = (rows.vocab + N - 1) / N, per = (units + splits - 1) / splits;
     const uint32_t begin = min(split * per, units), end = min(begin + per, units);
-    const uint32_t whole = min(end, rows.vocab / kUnit);
+    const uint32_t whole = min(end, rows.vocab / N);
     Running r;
     uint32_t u = begin + threadIdx.x;
     constexpr int kBatch = 4;
     for (; u + (kBatch - 1) * NT < whole; u += kBatch * NT) {
-        Raw<T> raw[kBatch];
+        Raw<T, N> raw[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) raw[i] = load_whole(row + (int64_t)(u + i * NT) * kUnit);
-        F8 x[kBatch];
+        for (int i = 0; i < kBatch; ++i) raw[i] = load_whole<T, N>(row + (int64_t)(u + i * NT) * N);
+        F<N> x[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) x[i] = widen(raw[i]);
         r.add(x);
     }
     for (; u < end; u += NT) {
-        const F8 x[1] = {logits_unit(row, u, rows.vocab)};
+        const F<N> x[1] = {logits_unit(row, u, rows.vocab)};
         r.add(x);
     }
     // lanes, then waves
@@ -184,17 +187,18 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(Rows rows, uint32_t par
                                                          const float* __restrict__ upstream,
                                                          const T* __restrict__ logits, const void* __restrict__ targets,
                                                          const float2* __restrict__ stats, T* __restrict__ dlogits) {
+    constexpr int N = kUnit<T>;
     const uint32_t n = block_id() / parts, first = (block_id() - n * parts) * (kPart * NT) + threadIdx.x;
     if (n >= rows.count) return;
     const uint32_t target = target_of<I64>(targets, n, rows.vocab);
-    const uint32_t units = (rows.vocab + kUnit - 1) / kUnit;
+    const uint32_t units = (rows.vocab + N - 1) / N;
     T* out = dlogits + (int64_t)n * rows.vocab;
     if (target == ~0u) {
 #pragma unroll
         for (int i = 0; i < kPart; ++i) {
             const uint32_t u = first + i * NT;
             if (u < units)
-                store_unit(out + (int64_t)u * kUnit, Raw<T>{}, (int)min(rows.vocab - u * kUnit, (uint32_t)kUnit));
+                stream_unit(out + (int64_t)u * N, Raw<T, N>{}, (int)min(rows.vocab - u * N, (uint32_t)N));
         }
         return;
     }
@@ -202,23 +206,23 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(Rows rows, uint32_t par
     const float c = dlogp[n / span] * (upstream != nullptr ? *upstream : 1.f);
     const float2 st = stats[n];
     const float top = st.x, down = -c / st.y;
-    Raw<T> x[kPart];
+    Raw<T, N> x[kPart];
 #pragma unroll
     for (int i = 0; i < kPart; ++i) {
         const uint32_t u = first + i * NT;
-        if (u < units) x[i] = load_unit(row + (int64_t)u * kUnit, (int)min(rows.vocab - u * kUnit, (uint32_t)kUnit));
+        if (u < units) x[i] = load_unit(row + (int64_t)u * N, (int)min(rows.vocab - u * N, (uint32_t)N));
     }
 #pragma unroll
     for (int i = 0; i < kPart; ++i) {
         const uint32_t u = first + i * NT;
         if (u >= units) break;
-        F8 f = widen(x[i]);
+        F<N> f = widen(x[i]);
 #pragma unroll
-        for (int e = 0; e < kUnit; ++e) {
+        for (int e = 0; e < N; ++e) {
             f.v[e] = down * exp2_hw((f.v[e] - top) * kLog2e);
-            if (u * kUnit + e == target) f.v[e] += c;
+            if (u * N + e == target) f.v[e] += c;
         }
-        store_unit(out + (int64_t)u * kUnit, narrow<T>(f), (int)min(rows.vocab - u * kUnit, (uint32_t)kUnit));
+        stream_unit(out + (int64_t)u * N, narrow<T>(f), (int)min(rows.vocab - u * N, (uint32_t)N));
     }
 }
 
@@ -316,12 +320,13 @@ __global__ __launch_bounds__(64 * kWaves) void preference_mean_kernel(int64_t pa
     *loss = (float)(total / (double)pairs);
 }
 
+constexpr int64_t kPartCols = 4096;  // the fewest entries of a row that a workgroup takes
 constexpr int64_t kOneMost = 16384;  // tokens of both sides that one workgroup sums
 
 // Workgroups per row: one where the rows fill the chip, else as many as do, each
 // of a batch of every thread at least.
 uint32_t splits_of(int64_t rows, int64_t vocab) {
-    const int64_t most = (vocab + 8 * NT * 4 - 1) / (8 * NT * 4), want = (1024 + rows - 1) / (rows > 0 ? rows : 1);
+    const int64_t most = (vocab + kPartCols - 1) / kPartCols, want = (1024 + rows - 1) / (rows > 0 ? rows : 1);
     return (uint32_t)(want < most ? want : most);
 }
 
@@ -344,7 +349,8 @@ hipError_t forward(const LogprobArgs& a, hipStream_t s) {
 template <typename T, bool I64>
 hipError_t backward(const LogprobArgs& a, hipStream_t s) {
     const int64_t rows = a.batch * a.length;
-    const uint32_t parts = (uint32_t)((a.vocab + kUnit * kPart * NT - 1) / (kUnit * kPart * NT));
+    constexpr int64_t cols = kUnit<T> * kPart * NT;
+    const uint32_t parts = (uint32_t)((a.vocab + cols - 1) / cols);
     hipLaunchKernelGGL((logprob_bwd_kernel<T, I64>), grid_of(rows * parts), dim3(NT), 0, s, rows_of(a), parts,
                        (uint32_t)a.span, a.dlogp, a.upstream, (const T*)a.logits, a.targets, (const float2*)a.stats, (T*)a.dlogits);
     return hipGetLastError();
@@ -368,7 +374,7 @@ hipError_t preference(const PreferenceArgs& a, hipStream_t s) {
 }  // namespace
 
 bool logprob_grids_fit(int64_t rows, int64_t vocab) {
-    return rows * ((vocab + kUnit * kPart * NT - 1) / (kUnit * kPart * NT)) < (int64_t)1 << 31;
+    return rows * ((vocab + kPartCols - 1) / kPartCols) < (int64_t)1 << 31;
 }
 
 size_t logprob_workspace_bytes(int64_t rows, int64_t vocab) {

@@ -161,7 +161,7 @@ lors_status_t lors_norm_forward(const lors_norm_t* p, const void* X, const void*
 
 size_t lors_norm_workspace_bytes(const lors_norm_t* p) {
     if (p == nullptr || check_norm(p) != LORS_OK) return static_cast<size_t>(-1);
-    return lt::norm_workspace_bytes(p->rows, p->cols);
+    return lt::norm_workspace_bytes(p->rows, p->cols, p->dtype == LORS_DTYPE_BF16);
 }
 
 lors_status_t lors_norm_backward(const lors_norm_t* p, const void* dY, const void* dZ, const void* Z,
@@ -176,7 +176,7 @@ lors_status_t lors_norm_backward(const lors_norm_t* p, const void* dY, const voi
     if (p->kind == LORS_NORM_RMS) mean = nullptr;
     const int64_t es = elt_size(p->dtype), n = p->rows * p->cols * es, w = p->cols * es;
     const int64_t gs = elt_size(p->grad_dtype), g = p->cols * gs;
-    const size_t need = dweight != nullptr || dbias != nullptr ? lt::norm_workspace_bytes(p->rows, p->cols) : 0;
+    const size_t need = dweight != nullptr || dbias != nullptr ? lt::norm_workspace_bytes(p->rows, p->cols, p->dtype == LORS_DTYPE_BF16) : 0;
     st = check_arrays({{dY, n, es}, {dZ, n, es}, {Z, n, es}, {weight, w, es}, {mean, 4 * p->rows, 4},
                        {rstd, 4 * p->rows, 4}, state_of(p->rng)},
                       {{dX, n, es}, {dresidual, n, es}, {dweight, g, gs}, {dbias, g, gs},

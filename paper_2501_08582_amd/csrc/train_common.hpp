@@ -1,4 +1,4 @@
-// Device-side building blocks of the operators around the layer: units of eight
+// Device-side building blocks of the operators around the layer: units of
 // elements, the counter-based generator, reductions over a wave.
 #pragma once
 
@@ -14,108 +14,98 @@ namespace train {
 // Number of the workgroup in a grid_of().
 __device__ __forceinline__ uint32_t block_id() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
-// Eight consecutive elements of a row: one 16-byte vector of bf16, two of fp32.
-// Every kernel here works in such units: they are what the generator's blocks
-// cover, and rows of odd widths only differ in their last one.
-constexpr int kUnit = 8;
-
-struct F8 {
-    float v[kUnit];
-};
-
-// A unit as it is stored.  A row of an odd width starts at any multiple of the
-// element's size; the loads and stores below are written for that alignment,
-// and gfx950 executes them as 16-byte accesses at any address.
+// Consecutive elements of a row that a lane takes at a time: one 16-byte vector.
+// Every kernel here works in such units, so that the lanes of a wave access one
+// run of memory whatever the type; rows of odd widths only differ in their last
+// unit.
 template <typename T>
-struct Raw;
-template <>
-struct Raw<__bf16> {
-    u32x4 a;
-};
-template <>
-struct Raw<float> {
-    u32x4 a, b;
+constexpr int kUnit = 16 / sizeof(T);
+
+template <int N>
+struct F {
+    float v[N];
 };
 
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
+// N elements as they are stored.  A row of an odd width starts at any multiple of
+// the element's size: the loads and stores below are written for that alignment,
+// and gfx950 executes them as whole vectors at any address.
+template <typename T, int N>
+struct Raw {
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+};
+template <typename T, int N>
+struct alignas(sizeof(T)) Packed {
+    T v[N];
+};
 
-__device__ __forceinline__ Raw<__bf16> load_whole(const __bf16* p) { return {*(const u32x4_any*)p}; }
-__device__ __forceinline__ Raw<float> load_whole(const float* p) {
-    return {*(const u32x4_any4*)p, *(const u32x4_any4*)(p + 4)};
+template <typename T, int N>
+__device__ __forceinline__ Raw<T, N> load_whole(const T* p) {
+    return __builtin_bit_cast(Raw<T, N>, *(const Packed<T, N>*)p);
 }
 
-__device__ __forceinline__ F8 widen(Raw<__bf16> r) {
-    F8 f;
+template <typename T, int N>
+__device__ __forceinline__ F<N> widen(const Raw<T, N>& r) {
+    F<N> f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        f.v[2 * e] = __uint_as_float(r.a[e] << 16);
-        f.v[2 * e + 1] = __uint_as_float(r.a[e] & 0xFFFF0000u);
-    }
-    return f;
-}
-__device__ __forceinline__ F8 widen(Raw<float> r) {
-    F8 f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        f.v[e] = __uint_as_float(r.a[e]);
-        f.v[4 + e] = __uint_as_float(r.b[e]);
+    for (int e = 0; e < N; ++e) {
+        if constexpr (sizeof(T) == 2) f.v[e] = __uint_as_float(e & 1 ? r.w[e >> 1] & 0xFFFF0000u : r.w[e >> 1] << 16);
+        else f.v[e] = __uint_as_float(r.w[e]);
     }
     return f;
 }
 
-// The first n (1 .. 8) elements at p, the others 0.
-template <typename T>
-__device__ __forceinline__ Raw<T> load_unit(const T* p, int n) {
-    if (n >= kUnit) return load_whole(p);
-    Raw<T> r{};
-    if constexpr (sizeof(T) == 2) {
+template <typename T, int N>
+__device__ __forceinline__ Raw<T, N> narrow(const F<N>& f) {
+    Raw<T, N> r;
 #pragma unroll
-        for (int e = 0; e < kUnit - 1; ++e)
-            if (e < n) r.a[e >> 1] |= (uint32_t)((const uint16_t*)p)[e] << (16 * (e & 1));
-    } else {
-#pragma unroll
-        for (int e = 0; e < kUnit - 1; ++e)
-            if (e < n) (e < 4 ? r.a : r.b)[e & 3] = __float_as_uint(p[e]);
+    for (int i = 0; i < Raw<T, N>::kWords; ++i) {
+        if constexpr (sizeof(T) == 2) r.w[i] = pack_bf16x2(f.v[2 * i], f.v[2 * i + 1]);
+        else r.w[i] = __float_as_uint(f.v[i]);
     }
     return r;
 }
 
-template <typename T>
-__device__ __forceinline__ Raw<T> narrow(const F8& f) {
-    if constexpr (sizeof(T) == 2) {
-        return {u32x4{pack_bf16x2(f.v[0], f.v[1]), pack_bf16x2(f.v[2], f.v[3]), pack_bf16x2(f.v[4], f.v[5]),
-                      pack_bf16x2(f.v[6], f.v[7])}};
-    } else {
-        Raw<float> r;
+// The first n (1 .. N) elements at p, the others 0.
+template <typename T, int N>
+__device__ __forceinline__ Raw<T, N> load_unit(const T* p, int n) {
+    if (n >= N) return load_whole<T, N>(p);
+    Raw<T, N> r{};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            r.a[e] = __float_as_uint(f.v[e]);
-            r.b[e] = __float_as_uint(f.v[4 + e]);
+    for (int e = 0; e < N - 1; ++e)
+        if (e < n) {
+            if constexpr (sizeof(T) == 2) r.w[e >> 1] |= (uint32_t)((const uint16_t*)p)[e] << (16 * (e & 1));
+            else r.w[e] = ((const uint32_t*)p)[e];
         }
-        return r;
-    }
+    return r;
 }
-
-__device__ __forceinline__ void store_whole(__bf16* p, Raw<__bf16> r) { *(u32x4_any*)p = r.a; }
-__device__ __forceinline__ void store_whole(float* p, Raw<float> r) {
-    *(u32x4_any4*)p = r.a;
-    *(u32x4_any4*)(p + 4) = r.b;
-}
-
 template <typename T>
-__device__ __forceinline__ void store_unit(T* p, Raw<T> r, int n) {
-    if (n >= kUnit) {
-        store_whole(p, r);
-    } else if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int e = 0; e < kUnit - 1; ++e)
-            if (e < n) ((uint16_t*)p)[e] = (uint16_t)u16_at(r.a, e);
-    } else {
-#pragma unroll
-        for (int e = 0; e < kUnit - 1; ++e)
-            if (e < n) p[e] = __uint_as_float((e < 4 ? r.a : r.b)[e & 3]);
+__device__ __forceinline__ Raw<T, kUnit<T>> load_unit(const T* p, int n) {
+    return load_unit<T, kUnit<T>>(p, n);
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_unit(T* p, const Raw<T, N>& r, int n) {
+    if (n >= N) {
+        *(Packed<T, N>*)p = __builtin_bit_cast(Packed<T, N>, r);
+        return;
     }
+#pragma unroll
+    for (int e = 0; e < N - 1; ++e)
+        if (e < n) {
+            if constexpr (sizeof(T) == 2) ((uint16_t*)p)[e] = (uint16_t)(r.w[e >> 1] >> (16 * (e & 1)));
+            else ((uint32_t*)p)[e] = r.w[e];
+        }
+}
+
+// The same past the caches, for results that no cache could hold until they are
+// read.
+template <typename T, int N>
+__device__ __forceinline__ void stream_unit(T* p, const Raw<T, N>& r, int n) {
+    typedef uint32_t words __attribute__((ext_vector_type(Raw<T, N>::kWords)));
+    typedef words words_any __attribute__((aligned(sizeof(T))));
+    if (n >= N) __builtin_nontemporal_store(__builtin_bit_cast(words, r), (words_any*)p);
+    else store_unit<T, N>(p, r, n);
 }
 
 // ---------------------------------------------------------------------------
@@ -157,11 +147,17 @@ struct Dropper {
         factor = d.factor;
     }
 
-    // Unit g of row n, kept elements times the factor.
-    __device__ __forceinline__ void apply(F8& f, uint32_t n, uint32_t g) const {
-        const u32x4 w = philox(g, n, o0, o1, k0, k1);
+    // Unit g of row n, kept elements times the factor.  A block's 16-bit halves are
+    // one unit of bf16 and two of fp32.
+    template <int N>
+    __device__ __forceinline__ void apply(F<N>& f, uint32_t n, uint32_t g) const {
+        const u32x4 w = philox(g / (8 / N), n, o0, o1, k0, k1);
+        const bool upper = N == 4 && (g & 1);
 #pragma unroll
-        for (int e = 0; e < kUnit; ++e) f.v[e] = u16_at(w, e) >= below ? f.v[e] * factor : 0.f;
+        for (int e = 0; e < N; ++e) {
+            const uint32_t bits = upper ? u16_at(w, (e + 4) & 7) : u16_at(w, e);
+            f.v[e] = bits >= below ? f.v[e] * factor : 0.f;
+        }
     }
 };
 

@@ -60,7 +60,7 @@ struct NormArgs {
 };
 hipError_t launch_norm_forward(const NormArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_norm_backward(const NormArgs& a, bool bf16, hipStream_t s);
-size_t norm_workspace_bytes(int64_t rows, int64_t cols);
+size_t norm_workspace_bytes(int64_t rows, int64_t cols, bool bf16);
 
 struct EmbeddingArgs {
     int64_t tokens, vocab, cols;
