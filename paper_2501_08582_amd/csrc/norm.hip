@@ -308,32 +308,56 @@ __global__ __launch_bounds__(64 * kJoinWaves) void norm_join_kernel(const float*
 }
 
 // How a row is held: lanes of a wave per row (0: a workgroup), units per lane, the
-// threads of the workgroup and the most of them that its kernel is built for
-// (which sets the registers each may have).
+// most threads that its kernel is built for (which sets the registers each may
+// have), the threads of the workgroup.
 struct Plan {
     int lpr, v, most, threads;
 };
 
-Plan plan_of(int64_t cols, bool bf16) {
-    const int per = bf16 ? kUnit<__bf16> : kUnit<float>;
-    const int units = (int)((cols + per - 1) / per);
+int64_t units_of(int64_t cols, bool bf16) {
+    const int64_t per = bf16 ? kUnit<__bf16> : kUnit<float>;
+    return (cols + per - 1) / per;
+}
+
+Plan narrow_plan(int64_t units) {
     if (units <= 8) return {8, 1, 256, 256};
     if (units <= 16) return {16, 1, 256, 256};
     if (units <= 32) return {32, 1, 256, 256};
-    if (units <= 64) return {64, 1, 256, 256};
-    if (units <= 128) return {64, 2, 256, 256};
-    const int v = units <= 1024 ? 2 : units <= 4096 ? 4 : 8;
-    return {0, v, units <= 2048 ? 512 : 1024, ((units + v - 1) / v + 63) / 64 * 64};
+    return {64, units <= 64 ? 1 : 2, 256, 256};
+}
+
+Plan wide_plan(int64_t units, int v, int most) {
+    return {0, v, most, (int)((units + v - 1) / v + 63) / 64 * 64};
+}
+
+// The forward holds a row and little else: few waves with two units a lane are
+// faster than many with one (4096 x 5120 bf16 with dropout and residual: 39 us against
+// 42; 14336 wide, four against two units: 47 against 54).
+Plan forward_plan(int64_t units) {
+    if (units <= 128) return narrow_plan(units);
+    if (units <= 1024) return wide_plan(units, 2, 512);
+    return wide_plan(units, units <= 4096 ? 4 : 8, units <= 2048 ? 512 : 1024);
+}
+
+// The backward's sums take 64 bytes a unit beside the rows themselves: one unit a
+// lane as far as it goes leaves room for twice the waves (4096 x 5120 bf16, the same: 59 us
+// against 73; 2000 x 14336, two against four: 94 against 139).
+Plan backward_plan(int64_t units) {
+    if (units <= 128) return narrow_plan(units);
+    if (units <= 640) return wide_plan(units, 1, 640);
+    return wide_plan(units, units <= 1024 ? 1 : units <= 2048 ? 2 : units <= 4096 ? 4 : 8, 1024);
 }
 
 int64_t rows_per_group(const Plan& p) { return p.lpr == 0 ? 1 : p.threads / p.lpr; }
 
-// Workgroups of the backward: enough to fill the chip, no more than there are
-// groups of rows.
+// Workgroups of the backward: what the chip holds of them (two to a CU, one of the
+// largest), all with the same count of turns.
 int64_t backward_groups(int64_t rows, const Plan& p) {
     const int64_t groups = (rows + rows_per_group(p) - 1) / rows_per_group(p);
-    const int64_t most = 512;
-    return groups < most ? groups : most;
+    const int64_t most = p.threads > 640 ? 256 : 512;
+    if (groups <= most) return groups;
+    const int64_t turns = (groups + most - 1) / most;
+    return (groups + turns - 1) / turns;
 }
 
 template <int LPR, int V, int NT>
@@ -341,7 +365,7 @@ struct Held {
     static constexpr int lpr = LPR, v = V, nt = NT;
 };
 
-template <typename T, typename Fn>
+template <typename T, bool FORWARD, typename Fn>
 hipError_t with_plan(const Plan& p, Fn&& f) {
     switch (p.lpr) {
         case 8: return f(Held<8, 1, 256>());
@@ -350,16 +374,22 @@ hipError_t with_plan(const Plan& p, Fn&& f) {
         case 64: return p.v == 1 ? f(Held<64, 1, 256>()) : f(Held<64, 2, 256>());
         default: break;
     }
-    if (p.v == 2) return f(Held<0, 2, 512>());
+    if constexpr (FORWARD) {
+        if (p.v == 2) return f(Held<0, 2, 512>());
+        if (p.v == 4 && p.most == 512) return f(Held<0, 4, 512>());
+    } else {
+        if (p.v == 1) return p.most == 640 ? f(Held<0, 1, 640>()) : f(Held<0, 1, 1024>());
+        if (p.v == 2) return f(Held<0, 2, 1024>());
+    }
     if constexpr (sizeof(T) == 4)
         if (p.v == 8) return f(Held<0, 8, 1024>());
-    return p.most == 512 ? f(Held<0, 4, 512>()) : f(Held<0, 4, 1024>());
+    return f(Held<0, 4, 1024>());
 }
 
 template <typename T>
 hipError_t forward(const NormArgs& a, hipStream_t s) {
-    const Plan p = plan_of(a.cols, sizeof(T) == 2);
-    return with_plan<T>(p, [&](auto h) {
+    const Plan p = forward_plan(units_of(a.cols, sizeof(T) == 2));
+    return with_plan<T, true>(p, [&](auto h) {
         using H = decltype(h);
         const int64_t rpg = rows_per_group(p);
         hipLaunchKernelGGL((norm_fwd_kernel<T, H::lpr, H::v, H::nt>), grid_of((a.rows + rpg - 1) / rpg),
@@ -372,13 +402,13 @@ hipError_t forward(const NormArgs& a, hipStream_t s) {
 
 template <typename T>
 hipError_t backward(const NormArgs& a, hipStream_t s) {
-    const Plan p = plan_of(a.cols, sizeof(T) == 2);
+    const Plan p = backward_plan(units_of(a.cols, sizeof(T) == 2));
     const int64_t groups = backward_groups(a.rows, p);
     const bool dw = a.dweight != nullptr, db = a.dbias != nullptr;
     if (groups > 0) {
-        const hipError_t e = with_plan<T>(p, [&](auto h) {
+        const hipError_t e = with_plan<T, false>(p, [&](auto h) {
             using H = decltype(h);
-            hipLaunchKernelGGL((norm_bwd_kernel<T, H::lpr, H::v, H::nt, H::v * kUnit<T> <= 16>), dim3((unsigned)groups),
+            hipLaunchKernelGGL((norm_bwd_kernel<T, H::lpr, H::v, H::nt, (H::nt == 256 || H::v * kUnit<T> <= 8)>), dim3((unsigned)groups),
                                dim3(p.threads), 0, s, a.rows, (int)a.cols, a.rms, a.drop, (const T*)a.dY,
                                (const T*)a.dZ, (const T*)a.Z, (const T*)a.weight, a.mean, a.rstd, (T*)a.dX,
                                (T*)a.dresidual, a.part, dw, db);
@@ -400,7 +430,7 @@ hipError_t backward(const NormArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t norm_workspace_bytes(int64_t rows, int64_t cols, bool bf16) {
-    return (size_t)(2 * 4 * backward_groups(rows, plan_of(cols, bf16)) * cols);
+    return (size_t)(2 * 4 * backward_groups(rows, backward_plan(units_of(cols, bf16))) * cols);
 }
 
 hipError_t launch_norm_forward(const NormArgs& a, bool bf16, hipStream_t s) {
