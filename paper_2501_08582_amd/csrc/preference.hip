@@ -31,6 +31,19 @@ __device__ __forceinline__ uint32_t target_of(const void* targets, int64_t n, ui
 // below what a term of a sum next to 1 or a probability is rounded to.
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// e^t for t <= 0 where the result is an output of type T.  t log2(e) in fp32 is off by
+// up to 2^-24 of itself, t of -16 by 1e-6 of the result: nothing next to bf16's
+// rounding, more than fp32's, for which the product's remainder is put back.
+constexpr float kLog2eRest = 1.92596299e-8f;  // log2(e) - kLog2e
+template <typename T>
+__device__ __forceinline__ float exp_below(float t) {
+    const float x = t * kLog2e, y = exp2_hw(x);
+    if constexpr (sizeof(T) == 2) return y;
+    const float rest = __builtin_fmaf(t, kLog2e, -x) + t * kLog2eRest;
+    // -Inf, and products past fp32's range, have no remainder: their result is 0
+    return y == 0.f ? 0.f : __builtin_fmaf(y, rest * 0.69314718f, y);
+}
+
 // The sum of exp(x - top) over what was seen, with top the largest of it.
 struct Running {
     float top = kNone, sum = 0.f;
@@ -219,7 +232,7 @@ __global__ __launch_bounds__(NT) void logprob_bwd_kernel(Rows rows, uint32_t par
         F<N> f = widen(x[i]);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            f.v[e] = down * exp2_hw((f.v[e] - top) * kLog2e);
+            f.v[e] = down * exp_below<T>(f.v[e] - top);
             if (u * N + e == target) f.v[e] += c;
         }
         stream_unit(out + (int64_t)u * N, narrow<T>(f), (int)min(rows.vocab - u * N, (uint32_t)N));
@@ -242,65 +255,109 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
-// With ONE, a single workgroup takes all pairs, a wave each in turn, and the mean
-// as well; otherwise a workgroup takes a pair and preference_mean_kernel the mean.
 constexpr int kWaves = 16;
-template <bool I64, bool ONE>
+constexpr int kOnePairs = 512;
+
+// sum[side] += logp - ref over the tokens begin, begin + step, .. < end of both
+// sequences of pair i.
+template <bool I64>
+__device__ __forceinline__ void add_pair(double (&sum)[2], int64_t i, int64_t pairs, int64_t length, uint32_t vocab,
+                                         const float* logp, const float* ref, const void* targets, int64_t begin,
+                                         int64_t end, int step) {
+#pragma unroll 4
+    for (int64_t t = begin; t < end; t += step) {
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const int64_t at = (side * pairs + i) * length + t;
+            const double d = (double)logp[at] - (ref != nullptr ? (double)ref[at] : 0.0);
+            sum[side] += target_of<I64>(targets, at, vocab) != ~0u ? d : 0.0;
+        }
+    }
+}
+
+// The results of pair i from its sums; its loss is returned.
+__device__ __forceinline__ double finish_pair(double won, double lost, int64_t i, int64_t pairs, double beta, double e,
+                                              float* reward, float* dseq) {
+    won *= beta;
+    lost *= beta;
+    const double margin = won - lost;
+    reward[i] = (float)won;
+    reward[pairs + i] = (float)lost;
+    const double d =
+        beta / (double)pairs * (e * exp(log_sigmoid(margin)) - (1.0 - e) * exp(log_sigmoid(-margin)));
+    dseq[i] = (float)d;
+    dseq[pairs + i] = (float)-d;
+    return pair_loss(margin, e);
+}
+
+// Few tokens: one workgroup for all pairs, each cut into `segs` runs of tokens so
+// that every wave has one, then a thread to a pair.
+template <bool I64>
+__global__ __launch_bounds__(64 * kWaves) void preference_one_kernel(int pairs, int64_t length, uint32_t vocab,
+                                                                     double beta, double e, int segs,
+                                                                     const float* __restrict__ logp,
+                                                                     const float* __restrict__ ref,
+                                                                     const void* __restrict__ targets,
+                                                                     float* __restrict__ loss,
+                                                                     float* __restrict__ reward,
+                                                                     float* __restrict__ dseq) {
+    __shared__ double sums[2][kOnePairs];
+    __shared__ double totals[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int item = wave; item < pairs * segs; item += kWaves) {
+        const int i = item / segs, seg = item - i * segs;
+        double s[2] = {0.0, 0.0};
+        add_pair<I64>(s, i, pairs, length, vocab, logp, ref, targets, length * seg / segs + lane,
+                      length * (seg + 1) / segs, 64);
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            s[side] = wave_sum(s[side]);
+            if (lane == 0) sums[side][item] = s[side];
+        }
+    }
+    __syncthreads();
+    double total = 0.0;
+    for (int i = threadIdx.x; i < pairs; i += 64 * kWaves) {
+        double s[2] = {0.0, 0.0};
+        for (int seg = 0; seg < segs; ++seg)
+#pragma unroll
+            for (int side = 0; side < 2; ++side) s[side] += sums[side][i * segs + seg];
+        total += finish_pair(s[0], s[1], i, pairs, beta, e, reward, dseq);
+    }
+    total = wave_sum(total);
+    if (lane == 0) totals[wave] = total;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    total = 0.0;
+    for (int w = 0; w < kWaves; ++w) total += totals[w];
+    *loss = (float)(total / (double)pairs);
+}
+
+// Many: a workgroup to a pair; preference_mean_kernel takes the mean.
+template <bool I64>
 __global__ __launch_bounds__(64 * kWaves) void preference_kernel(int64_t pairs, int64_t length, uint32_t vocab,
                                                                  double beta, double e, const float* __restrict__ logp,
                                                                  const float* __restrict__ ref,
                                                                  const void* __restrict__ targets,
-                                                                 float* __restrict__ loss, float* __restrict__ reward,
+                                                                 float* __restrict__ reward,
                                                                  float* __restrict__ dseq) {
     __shared__ double lds[2][kWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t begin = ONE ? lane : threadIdx.x, step = ONE ? 64 : 64 * kWaves;
-    double total = 0.0;
-    for (int64_t i = ONE ? wave : blockIdx.x; i < pairs; i += ONE ? kWaves : gridDim.x) {
-        if constexpr (!ONE) __syncthreads();
-        double sum[2];
+    for (int64_t i = blockIdx.x; i < pairs; i += gridDim.x) {
+        double s[2] = {0.0, 0.0};
+        add_pair<I64>(s, i, pairs, length, vocab, logp, ref, targets, threadIdx.x, length, 64 * kWaves);
+        __syncthreads();  // the sums of the pair before are read
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-            const int64_t base = (side * pairs + i) * length;
-            double s = 0.0;
-#pragma unroll 4
-            for (int64_t t = begin; t < length; t += step) {
-                const bool counts = target_of<I64>(targets, base + t, vocab) != ~0u;
-                const double d = (double)logp[base + t] - (ref != nullptr ? (double)ref[base + t] : 0.0);
-                if (counts) s += d;
-            }
-            sum[side] = wave_sum(s);
+            s[side] = wave_sum(s[side]);
+            if ((threadIdx.x & 63) == 0) lds[side][threadIdx.x >> 6] = s[side];
         }
-        if constexpr (!ONE) {
-            if (lane == 0) {
-                lds[0][wave] = sum[0];
-                lds[1][wave] = sum[1];
-            }
-            __syncthreads();
-            sum[0] = sum[1] = 0.0;
-            for (int w = 0; w < kWaves; ++w) {
-                sum[0] += lds[0][w];
-                sum[1] += lds[1][w];
-            }
-        }
-        const double won = beta * sum[0], lost = beta * sum[1], margin = won - lost;
-        if (ONE ? lane == 0 : threadIdx.x == 0) {
-            reward[i] = (float)won;
-            reward[pairs + i] = (float)lost;
-            const double d = beta / (double)pairs *
-                             (e * exp(log_sigmoid(margin)) - (1.0 - e) * exp(log_sigmoid(-margin)));
-            dseq[i] = (float)d;
-            dseq[pairs + i] = (float)-d;
-            total += pair_loss(margin, e);
-        }
-    }
-    if constexpr (ONE) {
-        if (lane == 0) lds[0][wave] = total;
         __syncthreads();
-        if (threadIdx.x != 0) return;
-        total = 0.0;
-        for (int w = 0; w < kWaves; ++w) total += lds[0][w];
-        *loss = (float)(total / (double)pairs);
+        if (threadIdx.x != 0) continue;
+        s[0] = s[1] = 0.0;
+        for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+            for (int side = 0; side < 2; ++side) s[side] += lds[side][w];
+        finish_pair(s[0], s[1], i, pairs, beta, e, reward, dseq);
     }
 }
 
@@ -358,13 +415,16 @@ hipError_t backward(const LogprobArgs& a, hipStream_t s) {
 
 template <bool I64>
 hipError_t preference(const PreferenceArgs& a, hipStream_t s) {
-    if (2 * a.pairs * a.length <= kOneMost && a.pairs <= kOneMost) {
-        hipLaunchKernelGGL((preference_kernel<I64, true>), dim3(1), dim3(64 * kWaves), 0, s, a.pairs, a.length,
-                           (uint32_t)a.vocab, a.beta, a.smoothing, a.logp, a.ref, a.targets, a.loss, a.reward, a.dseq);
+    const dim3 block(64 * kWaves);
+    if (2 * a.pairs * a.length <= kOneMost && a.pairs <= kOnePairs) {
+        const int segs = a.pairs >= kWaves ? 1 : kWaves / (int)a.pairs;
+        hipLaunchKernelGGL(preference_one_kernel<I64>, dim3(1), block, 0, s, (int)a.pairs, a.length,
+                           (uint32_t)a.vocab, a.beta, a.smoothing, segs, a.logp, a.ref, a.targets, a.loss, a.reward,
+                           a.dseq);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((preference_kernel<I64, false>), dim3((unsigned)std::min<int64_t>(a.pairs, 65536)), dim3(64 * kWaves), 0, s, a.pairs,
-                       a.length, (uint32_t)a.vocab, a.beta, a.smoothing, a.logp, a.ref, a.targets, a.loss, a.reward,
+    hipLaunchKernelGGL(preference_kernel<I64>, dim3((unsigned)std::min<int64_t>(a.pairs, 65536)), block, 0, s,
+                       a.pairs, a.length, (uint32_t)a.vocab, a.beta, a.smoothing, a.logp, a.ref, a.targets, a.reward,
                        a.dseq);
     hipLaunchKernelGGL(preference_mean_kernel, dim3(1), dim3(64 * kWaves), 0, s, a.pairs, a.smoothing, a.reward,
                        a.loss);
