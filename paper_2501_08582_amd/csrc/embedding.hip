@@ -284,20 +284,19 @@ __device__ __forceinline__ uint32_t lower_bound(const uint2* __restrict__ sorted
 }
 
 constexpr uint32_t kChunk = 32;  // sorted positions of a partial sum
-constexpr uint32_t kRows = 8;    // rows of the table per group
-template <typename T>
-constexpr int kBatch = sizeof(T) == 2 ? 16 : 8;  // rows of dY in flight
+constexpr uint32_t kRows = 4;    // rows of the table per group
+constexpr int kBatch = 8;        // rows of dY in flight
 
 // acc += the units of dY's tokens pair[0 .. n), n <= kBatch, in order.
 template <typename T, int N>
-__device__ __forceinline__ void add_tokens(F<N>& acc, const uint2 (&pair)[kBatch<T>], int n, const T* __restrict__ dY,
+__device__ __forceinline__ void add_tokens(F<N>& acc, const uint2 (&pair)[kBatch], int n, const T* __restrict__ dY,
                                            int64_t cols, int64_t col, int left) {
-    Raw<T, N> r[kBatch<T>];
+    Raw<T, N> r[kBatch];
 #pragma unroll
-    for (int i = 0; i < kBatch<T>; ++i)
+    for (int i = 0; i < kBatch; ++i)
         if (i < n) r[i] = load_unit<T, N>(dY + (int64_t)pair[i].y * cols + col, left);
 #pragma unroll
-    for (int i = 0; i < kBatch<T>; ++i)
+    for (int i = 0; i < kBatch; ++i)
         if (i < n) {
             const F<N> f = widen(r[i]);
 #pragma unroll
@@ -316,14 +315,14 @@ __global__ __launch_bounds__(NT) void chunk_kernel(uint32_t chunks, uint32_t voc
     const int64_t col = ((int64_t)(group - chunk * tiles) * TL + threadIdx.x % TL) * N;
     const int left = (int)min(cols - col, (int64_t)N);
     const uint2* s = sorted + (int64_t)chunk * kChunk;
-    uint2 pair[kChunk / kBatch<T>][kBatch<T>];  // all at once: a chunk is two waits on memory
+    uint2 pair[kChunk / kBatch][kBatch];  // all at once: a chunk is two waits on memory
 #pragma unroll
-    for (uint32_t i = 0; i < kChunk; ++i) pair[i / kBatch<T>][i % kBatch<T>] = s[i];
+    for (uint32_t i = 0; i < kChunk; ++i) pair[i / kBatch][i % kBatch] = s[i];
     const uint32_t id = pair[0][0].x;
-    if (left <= 0 || id != pair[kChunk / kBatch<T> - 1][kBatch<T> - 1].x || id >= vocab) return;
+    if (left <= 0 || id != pair[kChunk / kBatch - 1][kBatch - 1].x || id >= vocab) return;
     F<N> acc = {};
 #pragma unroll
-    for (uint32_t b = 0; b < kChunk / kBatch<T>; ++b) add_tokens(acc, pair[b], kBatch<T>, dY, cols, col, left);
+    for (uint32_t b = 0; b < kChunk / kBatch; ++b) add_tokens(acc, pair[b], kBatch, dY, cols, col, left);
     store_unit(part + chunk * cols + col, narrow<float>(acc), left);
 }
 
@@ -360,11 +359,11 @@ __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t voca
                 pos += n * kChunk;
             } else {
                 // up to the next chunk: the tokens of v come first
-                const int room = (int)min(min(kChunk - pos % kChunk, tokens - pos), (uint32_t)kBatch<T>);
-                uint2 pair[kBatch<T>];
+                const int room = (int)min(min(kChunk - pos % kChunk, tokens - pos), (uint32_t)kBatch);
+                uint2 pair[kBatch];
                 int n = 0;
 #pragma unroll
-                for (int i = 0; i < kBatch<T>; ++i) {
+                for (int i = 0; i < kBatch; ++i) {
                     pair[i] = i < room ? sorted[pos + i] : uint2{~0u, 0u};
                     n += pair[i].x == v;
                 }
