@@ -284,8 +284,13 @@ __device__ __forceinline__ uint32_t lower_bound(const uint2* __restrict__ sorted
 }
 
 constexpr uint32_t kChunk = 32;  // sorted positions of a partial sum
-constexpr uint32_t kRows = 4;    // rows of the table per group
-constexpr int kBatch = 8;        // rows of dY in flight
+// Rows of the table per group, and of dY in flight.  With inputs that change from
+// call to call (lookup and gradient, us): 8 x 8 122 at 8192 tokens into 32768 x 4096, 304
+// at 16384 into 131072 x 4096, 54 at 1501 into 50021 x 771 fp32; 4 rows 129, 308, 50; 16
+// rows 124, 314, 57; 16 in flight 120, 307, 51, but 59 against 52 with 32768 tokens of
+// 32768 ids.
+constexpr uint32_t kRows = 8;
+constexpr int kBatch = 8;
 
 // acc += the units of dY's tokens pair[0 .. n), n <= kBatch, in order.
 template <typename T, int N>
