@@ -22,11 +22,11 @@ def philox_block(counter, key):
     return c
 
 
-def random16(rows, cols, seed, offset):
-    """The 16 random bits of every element."""
+def random16(rows, cols, seed, offset, first=0):
+    """The 16 random bits of every element of rows first .. first + rows - 1."""
     blocks = -(-cols // 8)
     c0 = np.broadcast_to(np.arange(blocks, dtype=np.uint64), (rows, blocks))
-    c1 = np.broadcast_to(np.arange(rows, dtype=np.uint64)[:, None], (rows, blocks))
+    c1 = np.broadcast_to(np.arange(first, first + rows, dtype=np.uint64)[:, None], (rows, blocks))
     c = [c0, c1, np.full((rows, blocks), offset & M32, np.uint64), np.full((rows, blocks), offset >> 32 & M32, np.uint64)]
     k0, k1 = seed & M32, seed >> 32 & M32
     lo, sh = np.uint64(M32), np.uint64(32)

@@ -108,14 +108,14 @@ struct Rows {
     }
 };
 
-// Row n of `splits` workgroups' share each; with splits > 1 their (top, sum) go to
+// A row's `splits` workgroups of W threads take a run of it each; with splits > 1 their (top, sum) go to
 // `part` and logprob_join_kernel finishes.
-template <typename T, bool I64>
-__global__ __launch_bounds__(NT) void logprob_fwd_kernel(Rows rows, uint32_t splits, const T* __restrict__ logits,
+template <typename T, bool I64, int W>
+__global__ __launch_bounds__(W) void logprob_fwd_kernel(Rows rows, uint32_t splits, const T* __restrict__ logits,
                                                          const void* __restrict__ targets, float* __restrict__ logp,
                                                          float2* __restrict__ stats, float2* __restrict__ part) {
     constexpr int N = kUnit<T>;
-    __shared__ float2 waves[NT / 64];
+    __shared__ float2 waves[W / 64];
     const uint32_t n = block_id() / splits, split = block_id() - n * splits;
     if (n >= rows.count) return;
     const uint32_t target = target_of<I64>(targets, n, rows.vocab);
@@ -130,16 +130,16 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(Rows rows, uint32_t spl
     Running r;
     uint32_t u = begin + threadIdx.x;
     constexpr int kBatch = 4;
-    for (; u + (kBatch - 1) * NT < whole; u += kBatch * NT) {
+    for (; u + (kBatch - 1) * W < whole; u += kBatch * W) {
         Raw<T, N> raw[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) raw[i] = load_whole<T, N>(row + (int64_t)(u + i * NT) * N);
+        for (int i = 0; i < kBatch; ++i) raw[i] = load_whole<T, N>(row + (int64_t)(u + i * W) * N);
         F<N> x[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) x[i] = widen(raw[i]);
         r.add(x);
     }
-    for (; u < end; u += NT) {
+    for (; u < end; u += W) {
         const F<N> x[1] = {logits_unit(row, u, rows.vocab)};
         r.add(x);
     }
@@ -151,10 +151,10 @@ __global__ __launch_bounds__(NT) void logprob_fwd_kernel(Rows rows, uint32_t spl
     if (threadIdx.x != 0) return;
     float top = kNone;
 #pragma unroll
-    for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, waves[w].x);
+    for (int w = 0; w < W / 64; ++w) top = fmaxf(top, waves[w].x);
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
+    for (int w = 0; w < W / 64; ++w) {
         Running q{waves[w].x, waves[w].y};
         q.rescale(top);
         sum += q.sum;
@@ -378,13 +378,21 @@ __global__ __launch_bounds__(64 * kWaves) void preference_mean_kernel(int64_t pa
 }
 
 constexpr int64_t kPartCols = 4096;  // the fewest entries of a row that a workgroup takes
+constexpr int64_t kManyRows = 512, kRowBytes = 256 << 10, kFewGroups = 512;
 constexpr int64_t kOneMost = 16384;  // tokens of both sides that one workgroup sums
 
-// Workgroups per row: one where the rows fill the chip, else as many as do, each
-// of a batch of every thread at least.
-uint32_t splits_of(int64_t rows, int64_t vocab) {
-    const int64_t most = (vocab + kPartCols - 1) / kPartCols, want = (1024 + rows - 1) / (rows > 0 ? rows : 1);
-    return (uint32_t)(want < most ? want : most);
+// How the forward takes its rows.  Many rows fill the chip with workgroups of 256
+// threads each.  A few take 1024 threads each, and very long ones of them several
+// workgroups, whose sums a second launch joins.
+struct FwdPlan {
+    int threads;
+    uint32_t splits;
+};
+FwdPlan fwd_plan(int64_t rows, int64_t vocab, bool bf16) {
+    if (rows >= kManyRows) return {NT, 1};
+    const int64_t pieces = vocab * (bf16 ? 2 : 4) / kRowBytes, room = rows > 0 ? kFewGroups / rows : 1;
+    const int64_t splits = pieces < room ? pieces : room;
+    return {1024, (uint32_t)(splits > 1 ? splits : 1)};
 }
 
 Rows rows_of(const LogprobArgs& a) {
@@ -394,9 +402,14 @@ Rows rows_of(const LogprobArgs& a) {
 template <typename T, bool I64>
 hipError_t forward(const LogprobArgs& a, hipStream_t s) {
     const int64_t rows = a.batch * a.length;
-    const uint32_t splits = splits_of(rows, a.vocab);
-    hipLaunchKernelGGL((logprob_fwd_kernel<T, I64>), grid_of(rows * splits), dim3(NT), 0, s, rows_of(a),
-                       splits, (const T*)a.logits, a.targets, a.logp, (float2*)a.stats, (float2*)a.workspace);
+    const FwdPlan p = fwd_plan(rows, a.vocab, sizeof(T) == 2);
+    const uint32_t splits = p.splits;
+    if (p.threads == NT)
+        hipLaunchKernelGGL((logprob_fwd_kernel<T, I64, NT>), grid_of(rows), dim3(NT), 0, s, rows_of(a), splits,
+                           (const T*)a.logits, a.targets, a.logp, (float2*)a.stats, (float2*)a.workspace);
+    else
+        hipLaunchKernelGGL((logprob_fwd_kernel<T, I64, 1024>), grid_of(rows * splits), dim3(1024), 0, s, rows_of(a),
+                           splits, (const T*)a.logits, a.targets, a.logp, (float2*)a.stats, (float2*)a.workspace);
     if (splits > 1)
         hipLaunchKernelGGL((logprob_join_kernel<T, I64>), grid_of(rows), dim3(64), 0, s, rows_of(a), splits,
                            (const T*)a.logits, a.targets, (const float2*)a.workspace, a.logp, (float2*)a.stats);
@@ -437,8 +450,8 @@ bool logprob_grids_fit(int64_t rows, int64_t vocab) {
     return rows * ((vocab + kPartCols - 1) / kPartCols) < (int64_t)1 << 31;
 }
 
-size_t logprob_workspace_bytes(int64_t rows, int64_t vocab) {
-    const uint32_t splits = rows > 0 ? splits_of(rows, vocab) : 1;
+size_t logprob_workspace_bytes(int64_t rows, int64_t vocab, bool bf16) {
+    const uint32_t splits = fwd_plan(rows, vocab, bf16).splits;
     return splits > 1 ? (size_t)(rows * splits * sizeof(float2)) : 0;
 }
 

@@ -314,7 +314,7 @@ static lt::LogprobArgs logprob_args(const lors_logits_t* p, const void* logits, 
 
 size_t lors_logprob_workspace_bytes(const lors_logits_t* p) {
     if (p == nullptr || check_logits(p) != LORS_OK) return static_cast<size_t>(-1);
-    return lt::logprob_workspace_bytes(p->batch * p->length, p->vocab);
+    return lt::logprob_workspace_bytes(p->batch * p->length, p->vocab, p->dtype == LORS_DTYPE_BF16);
 }
 
 lors_status_t lors_logprob_forward(const lors_logits_t* p, const void* logits, const void* targets, float* logp,
@@ -325,7 +325,7 @@ lors_status_t lors_logprob_forward(const lors_logits_t* p, const void* logits, c
     lors_status_t st = check_logits(p);
     if (st != LORS_OK) return st;
     const int64_t n = p->batch * p->length, es = elt_size(p->dtype), is = index_size(p->index_dtype);
-    const size_t need = lt::logprob_workspace_bytes(n, p->vocab);
+    const size_t need = lt::logprob_workspace_bytes(n, p->vocab, p->dtype == LORS_DTYPE_BF16);
     st = check_arrays({{logits, logits_bytes(p), es}, {targets, n * is, is}},
                       {{logp, 4 * n, 4}, {stats, 8 * n, 4}, {workspace, static_cast<int64_t>(need), 16}});
     if (st == LORS_OK) st = check_workspace(workspace, workspace_bytes, need);

@@ -96,7 +96,7 @@ hipError_t launch_logprob_forward(const LogprobArgs& a, bool bf16, hipStream_t s
 hipError_t launch_logprob_backward(const LogprobArgs& a, bool bf16, hipStream_t s);
 // Whether the grids can count their work in 32 bits.
 bool logprob_grids_fit(int64_t rows, int64_t vocab);
-size_t logprob_workspace_bytes(int64_t rows, int64_t vocab);
+size_t logprob_workspace_bytes(int64_t rows, int64_t vocab, bool bf16);
 
 struct PreferenceArgs {
     int64_t pairs, length, vocab;

@@ -64,16 +64,18 @@ def _vector(X: torch.Tensor, what: str, t: Optional[torch.Tensor], dtype=None) -
 
 def _extents(X: torch.Tensor) -> Tuple[int, int]:
     """Rows and columns of X with its leading dimensions flattened to one."""
-    if X.dim() == 0:
-        raise ValueError("expected a tensor of at least one dimension")
+    if X.dim() == 0 or X.shape[-1] == 0:
+        raise ValueError("expected a last dimension of at least one element")
     cols = X.shape[-1]
-    rows = 1
-    for n in X.shape[:-1]:
-        rows *= n
-    return rows, cols
+    return X.numel() // cols, cols
 
 
-def _rng(seed: int, offset: int, state: Optional[torch.Tensor]) -> _lib.Rng:
+_NO_RNG = _lib.Rng(0, 0, None)  # a descriptor takes a copy
+
+
+def _rng(p: float, seed: int, offset: int, state: Optional[torch.Tensor]) -> _lib.Rng:
+    if p == 0.0:
+        return _NO_RNG
     if state is not None and (state.dtype != torch.int64 or state.numel() != 2):
         raise ValueError("rng_state must be two int64")
     return _lib.Rng(int(seed) & _U64, int(offset) & _U64, _ptr(state))
@@ -97,10 +99,10 @@ def dropout(X: torch.Tensor, p: float, seed: int, offset: int = 0, residual: Opt
     rows, cols = _extents(X)
     _like(X, "residual", residual)
     _like(X, "out", out)
-    d = _lib.Dropout(rows, cols, p, _rng(seed, offset, rng_state), _dt(X), 0)
+    d = _lib.Dropout(rows, cols, p, _rng(p, seed, offset, rng_state), _dt(X), 0)
     if out is None:
         out = torch.empty_like(X)
-    if X.numel():
+    if rows:
         _call(dev, "lors_dropout", _lib.dropout, d, X.data_ptr(), _ptr(residual), out.data_ptr())
     return out
 
@@ -143,7 +145,7 @@ def norm_forward(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: O
     _vector(X, "weight", weight)
     _vector(X, "bias", bias)
     k, dt = _kind(kind), _dt(X)
-    d = _lib.Norm(rows, cols, eps, p, _rng(seed, offset, rng_state), dt, dt, k, 0)
+    d = _lib.Norm(rows, cols, eps, p, _rng(p, seed, offset, rng_state), dt, dt, k, 0)
     Y = torch.empty_like(X)
     # p below 2^-17 drops nothing
     Z = torch.empty_like(X) if residual is not None or p >= 2.0**-17 else None
@@ -179,7 +181,7 @@ def norm_backward(dY: torch.Tensor, Z: torch.Tensor, weight: Optional[torch.Tens
         raise ValueError("the layer norm's gradient needs its mean")
     if need_dweight is None:
         need_dweight = weight is not None
-    d = _lib.Norm(rows, cols, 0.0, p, _rng(seed, offset, rng_state), dt, _lib.DTYPE_BF16 if gdt == torch.bfloat16 else
+    d = _lib.Norm(rows, cols, 0.0, p, _rng(p, seed, offset, rng_state), dt, _lib.DTYPE_BF16 if gdt == torch.bfloat16 else
                   _lib.DTYPE_F32, k, 0)
     dX = torch.empty_like(Z)
     dres = torch.empty_like(Z) if need_dresidual and p > 0 else None
@@ -314,7 +316,7 @@ def logprob_forward(logits: torch.Tensor, targets: torch.Tensor) -> Tuple[torch.
     its results are 0 and its logits are not read."""
     d, dev = _logits(logits, targets)
     logp = torch.empty(targets.shape, dtype=torch.float32, device=dev)
-    stats = torch.empty((*targets.shape, 2), dtype=torch.float32, device=dev)
+    stats = logp.new_empty((*targets.shape, 2))
     need = _lib.logprob_workspace_bytes(d)
     ws = _workspace(need, dev)
     _call(dev, "lors_logprob_forward", _lib.logprob_forward, d, _ptr(logits), _ptr(targets), _ptr(logp), _ptr(stats),

@@ -102,8 +102,8 @@ def test_dropout_state_on_the_device():
 # The mean is off by 64 units of |z|, rstd by 34 of itself, h = (z - mean) rstd by
 # both: c = 128 of |w| (max|z| rstd + |h|) covers the result.
 # ---------------------------------------------------------------------------
-NORM_COLS = [1, 2, 7, 8, 9, 63, 64, 65, 127, 128, 129, 255, 257, 511, 512, 513, 1000, 1024, 1025, 2047, 2048, 4096, 5120,
-             8191, 8192, 8193, 16384, 16385, 32767, 32768]
+NORM_COLS = [1, 2, 7, 8, 9, 63, 64, 65, 127, 128, 129, 255, 257, 511, 512, 513, 1000, 1024, 1025, 2047, 2048, 2560, 2561, 4096,
+             4097, 5120, 5121, 8191, 8192, 8193, 16384, 16385, 32767, 32768]
 
 
 def _norm_case(rows, cols, dtype, rms, residual, p, weight, bias, train_too=True):
@@ -163,7 +163,7 @@ def test_norm_widths(cols, dtype):
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 4096), (2, 70), (700, 333), (1100, 2300), (20000, 40), (3000, 64), (1030, 1000),
-                                       (600, 9000)])
+                                       (600, 9000), (1300, 5120), (520, 16400)])
 @pytest.mark.parametrize("rms,residual,p,weight,bias", [(False, True, 0.2, True, True), (False, False, 0.0, False, False),
                                                         (True, True, 0.0, True, False), (True, False, 0.3, False, True)])
 def test_norm_rows_and_options(rows, cols, rms, residual, p, weight, bias):
@@ -228,7 +228,9 @@ def _ids(rng, n, vocab, how):
     (33, 1000, 128, "padded", "f32"), (64, 3, 129, "one", "f32"), (65, 1, 512, "one", "bf16"), (500, 50, 513, "zipf", "f32"),
     (3000, 20011, 771, "zipf", "bf16"), (8192, 1000, 40, "padded", "f32"), (8193, 512, 520, "zipf", "f32"),
     (16384, 300, 24, "zipf", "bf16"), (16385, 300, 24, "zipf", "bf16"), (20000, 70001, 136, "zipf", "f32"),
-    (40961, 300001, 9, "padded", "f32"), (33000, 2, 16, "padded", "f32"), (17000, 512, 8, "one", "f32")])
+    (40961, 300001, 9, "padded", "f32"), (33000, 2, 16, "padded", "f32"), (17000, 512, 8, "one", "f32"),
+    (4096, 600, 72, "zipf", "bf16"), (4097, 600, 72, "zipf", "f32"), (65536, 5000, 8, "zipf", "f32"), (65537, 5000, 8, "padded", "f32"),
+    (70001, 300001, 12, "zipf", "bf16")])
 def test_embedding(n, vocab, cols, how, dtype):
     rng = np.random.default_rng(n + vocab)
     ids = _ids(rng, n, vocab, how)
@@ -307,7 +309,7 @@ def _check_logprobs(logits, targets, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("batch,length,V", [(1, 1, 1), (2, 3, 2), (1, 5, 7), (3, 1, 8), (2, 2, 9), (1, 4, 2047), (2, 3, 8192),
-                                            (1, 1, 131072), (1, 2, 50021), (2, 600, 1003), (4, 300, 8193)])
+                                            (1, 1, 131072), (1, 2, 50021), (2, 600, 1003), (4, 300, 8193), (1, 3, 300001)])
 def test_logprobs(batch, length, V, dtype):
     rng = np.random.default_rng(V + length)
     logits, _ = normal(rng, (batch, length, V), dtype, 3.0)
@@ -589,3 +591,59 @@ def test_refusals():
         train.preference_forward(lp, tt, 9, smoothing=0.6)
     with pytest.raises(_lib.LorsError):
         train.preference_forward(lp[:0], tt[:0], 9)
+
+
+# ---------------------------------------------------------------------------
+# arrays of more than 2^31 elements
+# ---------------------------------------------------------------------------
+def test_dropout_and_norm_past_32_bits():
+    rows, cols, tail = 70001, 32768, 3
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").fill_(1.0)
+    x[-tail:] = torch.randn(tail, cols, device="cuda")
+    y = train.dropout(x, 0.25, SEED, OFFSET)
+    kept = ot.random16(tail, cols, SEED, OFFSET, first=rows - tail) >= ot.threshold(0.25)
+    x64 = f64(x[-tail:])
+    check("y", y[-tail:], np.where(kept, x64 * (65536 / 49152), 0.0), np.abs(x64) * 2, 2)
+    del y
+    got = train.norm_forward(x, residual=x)
+    small = x[-tail:].contiguous()
+    want = train.norm_forward(small, residual=small)
+    assert all(torch.equal(g[-tail:], w) for g, w in zip(got, want))
+    y, z, mean, rstd = got
+    dx = train.norm_backward(x, z, None, mean, rstd)[0]
+    assert torch.equal(dx[-tail:], train.norm_backward(small, want[1], None, want[2], want[3])[0])
+
+
+def test_embedding_past_32_bits():
+    vocab, cols = 600001, 4096
+    table = torch.zeros(vocab, cols, dtype=torch.bfloat16, device="cuda")
+    ids = torch.tensor([vocab - 1, 5, vocab - 2, vocab - 1], device="cuda")
+    table[vocab - 2:] = torch.randn(2, cols, device="cuda")
+    y = train.embedding_forward(ids, table)
+    assert torch.equal(y[0], table[-1]) and torch.equal(y[2], table[-2]) and not y[1].any()
+    table.fill_(3.0)
+    dy = torch.randn(4, cols, device="cuda").bfloat16()
+    dE = train.embedding_backward(dy, ids, vocab)
+    assert torch.equal(dE[-2], dy[2]) and torch.equal(dE[5], dy[1])
+    assert torch.equal(dE[-1], (dy[0].float() + dy[3].float()).bfloat16())
+    dE[-2:] = 0
+    dE[5] = 0
+    assert all(not part.any() for part in dE.split(100000))
+
+
+def test_logprobs_past_32_bits():
+    rows, V, tail = 17001, 131072, 5
+    x = torch.zeros(rows, V, dtype=torch.bfloat16, device="cuda")
+    x[-tail:] = torch.randn(tail, V, device="cuda") * 3
+    t = torch.full((rows,), -100, device="cuda")
+    t[-tail:] = torch.tensor([0, 7, V - 1, V - 2, 12345], device="cuda")
+    logp, stats = train.logprob_forward(x, t)
+    dx = train.logprob_backward(torch.ones(rows, device="cuda"), x, t, stats)
+    x64, t64 = f64(x[-tail:]), t[-tail:].cpu().numpy()
+    rp, top, total = ot.logprobs(x64, t64)
+    c = _sum_roundings(x64)
+    check("logp", logp[-tail:], rp, c, 1)
+    ref = ot.logprobs_backward(np.ones(tail), x64, t64)
+    p = np.exp(x64 - top[:, None]) / total[:, None]
+    check("dlogits", dx[-tail:], ref, p * (c[:, None] + 3 * (top[:, None] - x64) + 6) + np.abs(ref) + 2.0**-100, 2)
+    assert not logp[:-tail].any() and all(not part.any() for part in dx[:-tail].split(4000))

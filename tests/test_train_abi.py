@@ -234,7 +234,7 @@ def test_workspace(lib):
     # log-probabilities: none where the rows fill the chip
     assert _lib.logprob_workspace_bytes(logits(batch=2, length=4096, vocab=100000, batch_stride=0, row_stride=100000)) == 0
     assert _lib.logprob_workspace_bytes(logits(batch=0)) == 0
-    few = logits(batch=1, length=4, vocab=131072, row_stride=131072)
+    few = logits(batch=1, length=4, vocab=300000, row_stride=300000)
     need = _lib.logprob_workspace_bytes(few)
     assert need > 0 and need % 8 == 0
     assert call_logprob_forward(few, ptrs(4), BASE + 30 * GAP, need - 1) == _lib.ERR_WORKSPACE
