@@ -6,6 +6,7 @@ the C ABI in ``include/lors.h`` and ``include/lors_train.h``).  Python modules:
 ``ops``    PyTorch-facing calls and the autograd op (imports torch)
 ``train``  the operators around the layer in a fine-tuning step: norm, dropout,
            embedding, preference loss (imports torch)
+``finetune``  preference fine-tuning of a small sparse model with all of them
 ``_lib``   ctypes binding of the C ABI
 ``synth``  seeded synthetic inputs shaped like the paper's Llama projections
 ``costs``  flop / byte accounting
