@@ -124,12 +124,13 @@ __global__ __launch_bounds__(W) void logprob_fwd_kernel(Rows rows, uint32_t spli
         return;
     }
     const T* row = logits + rows.offset(n);
+    const float picked = (float)row[target];  // ahead: nothing waits for it at the end
     const uint32_t units = (rows.vocab + N - 1) / N, per = (units + splits - 1) / splits;
     const uint32_t begin = min(split * per, units), end = min(begin + per, units);
     const uint32_t whole = min(end, rows.vocab / N);
     Running r;
     uint32_t u = begin + threadIdx.x;
-    constexpr int kBatch = 4;
+    constexpr int kBatch = W == 1024 ? 8 : 4;  // units in flight: a row of few is bound by the wait for them
     for (; u + (kBatch - 1) * W < whole; u += kBatch * W) {
         Raw<T, N> raw[kBatch];
 #pragma unroll
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(W) void logprob_fwd_kernel(Rows rows, uint32_t spli
     r.top = top;
     r.sum = sum;
     if (splits > 1) part[block_id()] = float2{top, sum};
-    else finish((float)row[target], r, n, logp, stats);
+    else finish(picked, r, n, logp, stats);
 }
 
 // One wave per row joins its splits.
