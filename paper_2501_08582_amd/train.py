@@ -70,6 +70,11 @@ def _extents(X: torch.Tensor) -> Tuple[int, int]:
     return X.numel() // cols, cols
 
 
+def _drops(p: float) -> bool:
+    """Whether p, rounded to 2^-16 as the library does, drops anything."""
+    return not p * 65536.0 + 0.5 < 1.0
+
+
 _NO_RNG = _lib.Rng(0, 0, None)  # a descriptor takes a copy
 
 
@@ -147,8 +152,7 @@ def norm_forward(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: O
     k, dt = _kind(kind), _dt(X)
     d = _lib.Norm(rows, cols, eps, p, _rng(p, seed, offset, rng_state), dt, dt, k, 0)
     Y = torch.empty_like(X)
-    # p below 2^-17 drops nothing
-    Z = torch.empty_like(X) if residual is not None or p >= 2.0**-17 else None
+    Z = torch.empty_like(X) if residual is not None or _drops(p) else None
     rstd = torch.empty(X.shape[:-1], dtype=torch.float32, device=dev) if need_stats else None
     mean = torch.empty_like(rstd) if need_stats and k == _lib.NORM_LAYER else None
     if rows:
@@ -184,7 +188,7 @@ def norm_backward(dY: torch.Tensor, Z: torch.Tensor, weight: Optional[torch.Tens
     d = _lib.Norm(rows, cols, 0.0, p, _rng(p, seed, offset, rng_state), dt, _lib.DTYPE_BF16 if gdt == torch.bfloat16 else
                   _lib.DTYPE_F32, k, 0)
     dX = torch.empty_like(Z)
-    dres = torch.empty_like(Z) if need_dresidual and p > 0 else None
+    dres = torch.empty_like(Z) if need_dresidual and _drops(p) else None
     dweight = torch.empty(cols, dtype=gdt, device=dev) if need_dweight else None
     dbias = torch.empty(cols, dtype=gdt, device=dev) if need_dbias else None
     need = _lib.norm_workspace_bytes(d) if need_dweight or need_dbias else 0

@@ -183,6 +183,19 @@ def test_norm_equals_dropout_then_norm():
         assert torch.equal(u[0], y) and torch.equal(u[1], z)
 
 
+def test_norm_without_a_dropped_element():
+    """p that rounds to no drop at 2^-16, on both sides of the first that does."""
+    x = torch.randn(5, 300, device="cuda")
+    for p in (0.0, 1e-9, 2.0**-17 * (1 - 2.0**-40), np.nextafter(2.0**-17, 0), 2.0**-17, 2.0**-16):
+        y, z, mean, rstd = train.norm_forward(x, p=p, seed=1)
+        if ot.threshold(p) == 0:
+            assert z is x
+        else:
+            assert z is not x and torch.equal(z, train.dropout(x, p, 1))
+        dx, dres, _, _ = train.norm_backward(x, z, None, mean, rstd, p=p, seed=1, need_dresidual=True)
+        assert (dres is dx) == (ot.threshold(p) == 0)
+
+
 def test_norm_repeats_its_bits():
     x, w, dy = torch.randn(3000, 640, device="cuda"), torch.randn(640, device="cuda"), torch.randn(3000, 640, device="cuda")
     _, z, mean, rstd = train.norm_forward(x, w)
