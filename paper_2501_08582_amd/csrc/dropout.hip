@@ -1,6 +1,13 @@
 // Dropout from the counter-based generator: y = keep ? factor x : 0 (+ residual).
 // The mask is a function of (seed, offset, row, column), so the gradient is the
 // same pass over dY and nothing is stored.
+//
+// Bound by memory as long as the generator keeps up: a block of Philox is 20
+// products of 32 x 32 -> 64 bits (a quarter of the rate of other instructions) and
+// about 60 more.  With 32 bits an element a block would cover four and, by that count,
+// take 1.7 times as long as reading and writing four bf16; with 16 bits it covers
+// eight, and p is resolved to 2^-16.  8192 x 14336 bf16: 94 us, 5.0 TB/s (a copy reaches 5.1);
+// 777 x 1003 fp32: 4 us.
 #include "train_common.hpp"
 
 namespace lors {
@@ -10,6 +17,7 @@ namespace {
 constexpr int NT = 256;
 constexpr int kAhead = 2;  // units a thread has in flight
 
+// A grid of 16 workgroups a CU walks the units, two of them ahead of the generator.
 template <typename T>
 __global__ __launch_bounds__(NT) void dropout_kernel(int64_t rows, uint32_t cols, uint32_t units, DropArgs drop,
                                                      const T* __restrict__ X, const T* __restrict__ residual,

@@ -3,7 +3,14 @@
 //
 // The logits are what costs: the forward reads each row once, keeping a running
 // maximum and the sum of exponentials below it, and the backward reads it again
-// and writes the gradient.  Rows whose target does not count are not read.
+// and writes the gradient.  Rows whose target does not count are not read.  (The
+// loss of a pair needs all its tokens before the first gradient, so two reads it
+// is.)
+//   logp = x[target] - top - log(sum),  dx = c (onehot - exp(x - top) / sum)
+//
+// Bound by memory: 8192 x 65536 bf16, 86 % of the rows counted: forward 154 us (0.92 GB,
+// 6.0 TB/s), backward 345 us (0.92 GB read, 1.07 written, 5.8 TB/s).  1028 x 50021 fp32:
+// 35 and 59 us.
 #include <algorithm>
 
 #include "train_common.hpp"
@@ -108,6 +115,9 @@ struct Rows {
     }
 };
 
+// An element takes a conversion, half a maximum, a difference, a product, an
+// exponential (a quarter of the rate) and a sum: by that count two thirds of the time
+// that the two bytes of a bf16 take.
 // A row's `splits` workgroups of W threads take a run of it each; with splits > 1 their (top, sum) go to
 // `part` and logprob_join_kernel finishes.
 template <typename T, bool I64, int W>
@@ -384,7 +394,9 @@ constexpr int64_t kOneMost = 16384;  // tokens of both sides that one workgroup 
 
 // How the forward takes its rows.  Many rows fill the chip with workgroups of 256
 // threads each.  A few take 1024 threads each, and very long ones of them several
-// workgroups, whose sums a second launch joins.
+// workgroups, whose sums a second launch joins: 4 x 131072 bf16 9.2 us so, against
+// 3.2 and 2.8 in 64 workgroups and a join -- but a call of two launches costs its
+// caller 16.4 us, of one 11.4.
 struct FwdPlan {
     int threads;
     uint32_t splits;
