@@ -24,7 +24,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import _lib
-from .ops import _call, _dev, _dt, _ptr
+from .ops import _dev, _dt, _ptr
 
 LAYER = "layer"
 RMS = "rms"
@@ -33,6 +33,31 @@ _KIND = {LAYER: _lib.NORM_LAYER, RMS: _lib.NORM_RMS}
 _INDEX = {torch.int64: _lib.INDEX_I64, torch.int32: _lib.INDEX_I32}
 _U64 = 2**64 - 1
 _INVALID = 2**64 - 1
+_current = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _call(dev: torch.device, where: str, fn, *args) -> None:
+    """``ops._call`` for calls whose kernels take a few microseconds: the caller's
+    tensors are on the GPU, so its runtime is up."""
+    index = dev.index
+    if _current() == index:
+        status = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _raw_stream(index))
+    if status:
+        _lib.check(status, where)
+
+
+def _place(X: torch.Tensor, *ts: Optional[torch.Tensor]) -> torch.device:
+    """The device of X, on which the others have to be as well, all contiguous."""
+    index = X.get_device()
+    fine = index >= 0 and X.is_contiguous()
+    for t in ts:
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
+            fine = False
+    return X.device if fine else _dev(X, *ts)  # which says what is wrong
 
 
 def _kind(kind) -> int:
@@ -100,7 +125,7 @@ def dropout(X: torch.Tensor, p: float, seed: int, offset: int = 0, residual: Opt
     """dropout(X) (+ residual).  ``p`` is applied as the nearest multiple of 2^-16,
     and kept elements are divided by 1 minus that.  The gradient of X is the same call on
     dY without the residual (``dropout_add`` does that under autograd)."""
-    dev = _dev(X, residual, rng_state, out)
+    dev = _place(X, residual, rng_state, out)
     rows, cols = _extents(X)
     _like(X, "residual", residual)
     _like(X, "out", out)
@@ -144,7 +169,7 @@ def norm_forward(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: O
     residual and dropout), Y its norm over the last dimension: ``layer``, (Z - mean) rstd
     weight + bias, or ``rms``, Z rstd weight + bias.  mean (None for ``rms``) and rstd are what
     ``norm_backward`` needs; ``need_stats=False`` leaves them out."""
-    dev = _dev(X, weight, bias, residual, rng_state)
+    dev = _place(X, weight, bias, residual, rng_state)
     rows, cols = _extents(X)
     _like(X, "residual", residual)
     _vector(X, "weight", weight)
@@ -170,7 +195,7 @@ def norm_backward(dY: torch.Tensor, Z: torch.Tensor, weight: Optional[torch.Tens
     elsewhere, its gradient ``dZ`` from there.  dweight (by default where there is a
     weight) and dbias are in ``grad_dtype``, by default Z's.  Without dropout dresidual
     is dX."""
-    dev = _dev(dY, Z, weight, mean, rstd, dZ, rng_state)
+    dev = _place(dY, Z, weight, mean, rstd, dZ, rng_state)
     rows, cols = _extents(Z)
     _like(Z, "dY, dZ", dY, dZ)
     _vector(Z, "weight", weight)
@@ -239,13 +264,13 @@ def _embedding(ids, vocab, cols, scale, dtype, grad_dtype) -> _lib.Embedding:
 def embedding_forward(ids: torch.Tensor, E: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
     """scale * E[ids], with a trailing dimension of E's width.  Ids outside the table
     (padding, e.g. -1) give rows of zeros."""
-    dev = _dev(ids, E)
+    dev = _place(ids, E)
     if E.dim() != 2:
         raise ValueError("the table must be vocab x width")
     vocab, cols = E.shape
     dt = _dt(E)
     d = _embedding(ids, vocab, cols, scale, dt, dt)
-    Y = torch.empty((*ids.shape, cols), dtype=E.dtype, device=dev)
+    Y = E.new_empty((*ids.shape, cols))
     _call(dev, "lors_embedding_forward", _lib.embedding_forward, d, _ptr(ids), _ptr(E), _ptr(Y))
     return Y
 
@@ -254,7 +279,7 @@ def embedding_backward(dY: torch.Tensor, ids: torch.Tensor, vocab: int, scale: f
                        grad_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """The gradient of the whole table (vocab x width) in ``grad_dtype``, by default
     dY's: sums in fp32 over the tokens in their order, rounded once."""
-    dev = _dev(dY, ids)
+    dev = _place(dY, ids)
     rows, cols = _extents(dY)
     if rows != ids.numel():
         raise ValueError(f"dY has {rows} rows for {ids.numel()} ids")
@@ -299,7 +324,7 @@ def _logits(logits: torch.Tensor, targets: torch.Tensor):
         raise ValueError("logits must be (batch x) length x vocab, targets (batch x) length")
     if logits.stride(-1) != 1 and logits.shape[-1] > 1:
         raise ValueError("logits must be contiguous in their last dimension")
-    dev = _dev(targets)
+    dev = _place(targets)
     if dev != logits.device:
         raise ValueError("all tensors must be on the same device")
     batch, bs = (1, 0) if logits.dim() == 2 else (logits.shape[0], logits.stride(0))
@@ -334,7 +359,7 @@ def logprob_backward(dlogp: torch.Tensor, logits: torch.Tensor, targets: torch.T
     log-probabilities: one for each token (the targets' shape) or one for each sequence
     (batch), times the scalar ``upstream``."""
     d, dev = _logits(logits, targets)
-    if _dev(dlogp, stats, upstream) != dev:
+    if _place(dlogp, stats, upstream) != dev:
         raise ValueError("all tensors must be on the same device")
     _fp32((*targets.shape, 2), "stats", stats)
     span = 1
@@ -377,7 +402,7 @@ def preference_forward(logp: torch.Tensor, targets: torch.Tensor, vocab: int, re
     ones first: reward = beta * sum over counted tokens of (logp - ref), loss the mean over pairs
     of -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m) with m the pair's difference of
     rewards, dseq the loss's gradient by each sequence's summed log-probability."""
-    dev = _dev(logp, targets, ref)
+    dev = _place(logp, targets, ref)
     if logp.dim() != 2 or logp.shape[0] % 2 != 0:
         raise ValueError("expected 2 P x length: the preferred sequences, then the rejected ones")
     _fp32(targets.shape, "logp, ref", logp, ref)
