@@ -165,7 +165,7 @@ typedef struct lors_embedding_desc {
 lors_status_t lors_embedding_forward(const lors_embedding_t* p, const void* ids, const void* E, void* Y, void* stream);
 
 /* Device scratch bytes of lors_embedding_backward: the tokens sorted by id, and
- * partial sums of frequent ones.  (size_t)-1 if p is invalid. */
+ * partial sums of frequent ones; 0 for a few tokens.  (size_t)-1 if p is invalid. */
 size_t lors_embedding_workspace_bytes(const lors_embedding_t* p);
 
 /*

@@ -242,7 +242,8 @@ def _ids(rng, n, vocab, how):
     (3000, 20011, 771, "zipf", "bf16"), (8192, 1000, 40, "padded", "f32"), (8193, 512, 520, "zipf", "f32"),
     (16384, 300, 24, "zipf", "bf16"), (16385, 300, 24, "zipf", "bf16"), (20000, 70001, 136, "zipf", "f32"),
     (40961, 300001, 9, "padded", "f32"), (33000, 2, 16, "padded", "f32"), (17000, 512, 8, "one", "f32"),
-    (4096, 600, 72, "zipf", "bf16"), (4097, 600, 72, "zipf", "f32"), (65536, 5000, 8, "zipf", "f32"), (65537, 5000, 8, "padded", "f32"),
+    (255, 60, 72, "zipf", "bf16"), (256, 9, 1030, "padded", "f32"), (257, 9, 1030, "padded", "bf16"), (200, 3000, 5, "even", "bf16"),
+    (256, 40, 64, "one", "bf16"), (4096, 600, 72, "zipf", "bf16"), (4097, 600, 72, "zipf", "f32"), (65536, 5000, 8, "zipf", "f32"), (65537, 5000, 8, "padded", "f32"),
     (70001, 300001, 12, "zipf", "bf16")])
 def test_embedding(n, vocab, cols, how, dtype):
     rng = np.random.default_rng(n + vocab)

@@ -223,14 +223,15 @@ def test_workspace(lib):
     assert call_norm_backward(norm(), a, BASE + 30 * GAP, need - 1) == _lib.ERR_WORKSPACE
     assert call_norm_backward(norm(), a, BASE + 30 * GAP + 8, need) == _lib.ERR_ALIGN
     assert call_norm_backward(norm(), a, a[0], need) == _lib.ERR_ALIAS
-    # the embedding: 8 bytes a token, an fp32 row for every 32, more beyond what is counted
+    # the embedding: none for a few tokens, then 8 bytes each, an fp32 row for every 32, more beyond what is counted
     assert _lib.embedding_workspace_bytes(embedding(tokens=0)) == 0
-    assert _lib.embedding_workspace_bytes(embedding(tokens=64, cols=1000)) == 512 + -(-2 * 4000 // 256) * 256
+    assert _lib.embedding_workspace_bytes(embedding(tokens=256)) == 0
+    assert _lib.embedding_workspace_bytes(embedding(tokens=320, cols=1000)) == 2560 + -(-10 * 4000 // 256) * 256
     big = _lib.embedding_workspace_bytes(embedding(tokens=1 << 20, cols=4096))
     assert (1 << 20) * (16 + 4 * 4096 // 32) <= big <= (1 << 20) * (18 + 4 * 4096 // 32)
     assert _lib.embedding_workspace_bytes(embedding(cols=0)) == BAD
-    assert call_embedding_backward(embedding(), ptrs(3), None, 0) == _lib.ERR_WORKSPACE
-    assert call_embedding_backward(embedding(), ptrs(3), BASE + 2 * GAP, 1 << 20) == _lib.ERR_ALIAS
+    assert call_embedding_backward(embedding(tokens=1000), ptrs(3), None, 0) == _lib.ERR_WORKSPACE
+    assert call_embedding_backward(embedding(tokens=1000), ptrs(3), BASE + 2 * GAP, 1 << 20) == _lib.ERR_ALIAS
     # log-probabilities: none where the rows fill the chip
     assert _lib.logprob_workspace_bytes(logits(batch=2, length=4096, vocab=100000, batch_stride=0, row_stride=100000)) == 0
     assert _lib.logprob_workspace_bytes(logits(batch=0)) == 0
