@@ -51,6 +51,12 @@ __device__ __forceinline__ float exp_below(float t) {
     return y == 0.f ? 0.f : __builtin_fmaf(y, rest * 0.69314718f, y);
 }
 
+// t log2(e) for the terms of a sum.  With the constant in fp32 alone every term is off
+// by the same 1.3e-8 t, which does not average out: the logarithms of a sequence's
+// sums are off by 7e-8 each, and its reward by as many as it has tokens.  (The small
+// product first: added to the rounded large one it would be lost.)
+__device__ __forceinline__ float times_log2e(float t) { return __builtin_fmaf(t, kLog2e, t * kLog2eRest); }
+
 // The sum of exp(x - top) over what was seen, with top the largest of it.
 struct Running {
     float top = kNone, sum = 0.f;
@@ -71,7 +77,7 @@ struct Running {
 #pragma unroll
         for (int i = 0; i < B; ++i)
 #pragma unroll
-            for (int e = 0; e < N; ++e) s[e] += exp2_hw((x[i].v[e] - ref) * kLog2e);
+            for (int e = 0; e < N; ++e) s[e] += exp2_hw(times_log2e(x[i].v[e] - ref));
         sum += (s[0] + s[1]) + (s[2] + s[3]);
         if constexpr (N == 8) sum += (s[4] + s[5]) + (s[6] + s[7]);
     }
