@@ -204,7 +204,7 @@ size_t lors_logprob_workspace_bytes(const lors_logits_t* p);
 
 /*
  * logp = logits[target] - log of the sum of exp(logits) (fp32; 0 where the target does
- * not count).  stats (two fp32 a row, may be NULL): the row's largest logit and the sum
+ * not count).  stats (two fp32 a row, 8-byte aligned, may be NULL): the row's largest logit and the sum
  * of exp(logits - it), what the backward needs; 0, 0 where the target does not count.
  * Rows whose entries are all the type's lowest value have an even distribution; a row
  * of -Inf alone has none: NaN.

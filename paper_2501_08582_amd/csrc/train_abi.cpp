@@ -327,7 +327,7 @@ lors_status_t lors_logprob_forward(const lors_logits_t* p, const void* logits, c
     const int64_t n = p->batch * p->length, es = elt_size(p->dtype), is = index_size(p->index_dtype);
     const size_t need = lt::logprob_workspace_bytes(n, p->vocab, p->dtype == LORS_DTYPE_BF16);
     st = check_arrays({{logits, logits_bytes(p), es}, {targets, n * is, is}},
-                      {{logp, 4 * n, 4}, {stats, 8 * n, 4}, {workspace, static_cast<int64_t>(need), 16}});
+                      {{logp, 4 * n, 4}, {stats, 8 * n, 8}, {workspace, static_cast<int64_t>(need), 16}});
     if (st == LORS_OK) st = check_workspace(workspace, workspace_bytes, need);
     if (st != LORS_OK) return st;
     lt::LogprobArgs a = logprob_args(p, logits, targets);
@@ -349,7 +349,7 @@ lors_status_t lors_logprob_backward(const lors_logits_t* p, const float* dlogp, 
     const int64_t n = p->batch * p->length, es = elt_size(p->dtype), is = index_size(p->index_dtype);
     if (span < 1 || (some && (span > p->length || n % span != 0))) return LORS_ERR_SHAPE;
     st = check_arrays({{dlogp, 4 * (n / span), 4}, {upstream, 4, 4}, {logits, logits_bytes(p), es},
-                       {targets, n * is, is}, {stats, 8 * n, 4}},
+                       {targets, n * is, is}, {stats, 8 * n, 8}},
                       {{dlogits, n * p->vocab * es, es}});
     if (st != LORS_OK) return st;
     lt::LogprobArgs a = logprob_args(p, logits, targets);

@@ -22,6 +22,7 @@ from __future__ import annotations
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _lib
 from .ops import _dev, _dt, _ptr
@@ -147,6 +148,7 @@ class DropoutAddFn(torch.autograd.Function):
         return dropout(X, p, seed, offset, residual, rng_state)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY):
         p, seed, offset = ctx.args
         (rng_state,) = ctx.saved_tensors
@@ -237,6 +239,7 @@ class NormFn(torch.autograd.Function):
         return Y, Z if ctx.own_z else X.view_as(X)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY, dZ):
         kind, p, seed, offset = ctx.args
         Z, weight, mean, rstd, rng_state = ctx.saved_tensors
@@ -302,6 +305,7 @@ class EmbeddingFn(torch.autograd.Function):
         return embedding_forward(ids, E, scale)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY):
         (ids,) = ctx.saved_tensors
         return None, embedding_backward(dY.contiguous(), ids, ctx.vocab, ctx.scale), None
@@ -386,6 +390,7 @@ class TokenLogprobsFn(torch.autograd.Function):
         return logp
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dlogp):
         logits, targets, stats = ctx.saved_tensors
         return logprob_backward(dlogp.contiguous(), logits, targets, stats), None
@@ -436,6 +441,7 @@ class PreferenceLossFn(torch.autograd.Function):
         return loss, reward, logp
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss, _dreward, _dlogp):
         logits, targets, stats, dseq = ctx.saved_tensors
         return logprob_backward(dseq, logits, targets, stats, dloss.contiguous()), None, None, None, None

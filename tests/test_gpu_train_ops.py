@@ -492,6 +492,15 @@ def test_autograd_matches_the_plain_calls():
     assert torch.equal(loss, step[0]) and torch.equal(reward, step[1]) and torch.equal(logp, step[2]) and torch.equal(g, step[3])
 
 
+def test_second_derivatives_are_refused():
+    x = torch.randn(3, 40, device="cuda", requires_grad=True)
+    t = torch.zeros(3, dtype=torch.int64, device="cuda")
+    for y in (train.norm(x)[0], train.dropout_add(x, 0.5, 1), train.embedding(t, x), train.token_logprobs(x, t)):
+        (g,) = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad(g.sum(), x)
+
+
 def _everything(x, w, b, r, dy, ids, table, logits, t, ref, state):
     y, z, mean, rstd = train.norm_forward(x, w, b, residual=r, p=0.1, seed=1, offset=2, rng_state=state)
     back = train.norm_backward(dy, z, w, mean, rstd, dZ=dy, p=0.1, seed=1, offset=2, rng_state=state, need_dresidual=True,

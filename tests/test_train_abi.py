@@ -202,6 +202,9 @@ def test_other_refusals(lib):
     assert call_norm_forward(state, a) == _lib.ERR_ALIGN
     over = dropout(rng=_lib.Rng(1, 2, a[2]))
     assert call_dropout(over, a[:3]) == _lib.ERR_ALIAS
+    # the statistics of a row are pairs
+    x, t, logp, stats = ptrs(4)
+    assert call_logprob_forward(logits(), [x, t, logp, stats + 4]) == _lib.ERR_ALIGN
     # spans that do not divide the tokens
     for span in (0, -1, 3, 9, 16):
         assert call_logprob_backward(logits(), ptrs(6), span) == _lib.ERR_SHAPE
