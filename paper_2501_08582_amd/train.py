@@ -348,6 +348,10 @@ def logprob_forward(logits: torch.Tensor, targets: torch.Tensor) -> Tuple[torch.
     ``logprob_backward`` needs.  A target outside the vocabulary (-100) does not count:
     its results are 0 and its logits are not read."""
     d, dev = _logits(logits, targets)
+    return _logprob_forward(d, dev, logits, targets)
+
+
+def _logprob_forward(d: _lib.Logits, dev: torch.device, logits, targets):
     logp = torch.empty(targets.shape, dtype=torch.float32, device=dev)
     stats = logp.new_empty((*targets.shape, 2))
     need = _lib.logprob_workspace_bytes(d)
@@ -374,7 +378,11 @@ def logprob_backward(dlogp: torch.Tensor, logits: torch.Tensor, targets: torch.T
         _fp32(targets.shape, "dlogp", dlogp)
     if upstream is not None and (upstream.numel() != 1 or upstream.dtype != torch.float32):
         raise ValueError("upstream must be one fp32")
-    dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    return _logprob_backward(d, dev, dlogp, span, upstream, logits, targets, stats)
+
+
+def _logprob_backward(d: _lib.Logits, dev: torch.device, dlogp, span, upstream, logits, targets, stats):
+    dlogits = logits.new_empty(logits.shape)
     _call(dev, "lors_logprob_backward", _lib.logprob_backward, d, _ptr(dlogp), span, _ptr(upstream), _ptr(logits),
           _ptr(targets), _ptr(stats), _ptr(dlogits))
     return dlogits
@@ -414,19 +422,21 @@ def preference_forward(logp: torch.Tensor, targets: torch.Tensor, vocab: int, re
     P = logp.shape[0] // 2
     d = _lib.Preference(P, logp.shape[1], vocab, beta, smoothing, _index(targets, "targets"), 0)
     out = torch.empty(4 * P + 1, dtype=torch.float32, device=dev)  # reward, dseq, loss: one allocation
-    reward, dseq, loss = out[:2 * P], out[2 * P:4 * P], out[4 * P]
+    reward, dseq, loss = out.split((2 * P, 2 * P, 1))
     at = out.data_ptr()
     _call(dev, "lors_preference", _lib.preference, d, _ptr(logp), _ptr(ref), _ptr(targets), at + 16 * P, at, at + 8 * P)
-    return loss, reward, dseq
+    return loss.view(()), reward, dseq
 
 
 def preference_step(logits: torch.Tensor, targets: torch.Tensor, ref: Optional[torch.Tensor] = None,
                     beta: float = 0.1, smoothing: float = 0.0):
     """(loss, reward, logp, dlogits) of one training step's loss on logits 2 P x length
     x vocab: forward and gradient together, for loops without autograd."""
-    logp, stats = logprob_forward(logits, targets)
+    d, dev = _logits(logits, targets)
+    logp, stats = _logprob_forward(d, dev, logits, targets)
     loss, reward, dseq = preference_forward(logp, targets, logits.shape[-1], ref, beta, smoothing)
-    return loss, reward, logp, logprob_backward(dseq, logits, targets, stats)
+    span = max(1, logits.shape[-2])
+    return loss, reward, logp, _logprob_backward(d, dev, dseq, span, None, logits, targets, stats)
 
 
 class PreferenceLossFn(torch.autograd.Function):
