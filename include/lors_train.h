@@ -145,7 +145,7 @@ typedef enum lors_index_dtype {
 
 /*
  * tokens >= 0, vocab >= 1, cols >= 1, each < 2^31, scale finite; otherwise
- * LORS_ERR_SHAPE; the backward takes ceil(cols / 256) . max(vocab / 8, tokens / 32) < 2^31,
+ * LORS_ERR_SHAPE; the backward takes (ceil(cols / 256) + 1) . max(vocab / 8, tokens / 32) < 2^31,
  * otherwise LORS_ERR_UNSUPPORTED.  Ids outside 0 .. vocab - 1 stand for no token (padding): their
  * row of Y is zero and they have no part in the gradient.
  * grad_dtype: the type of dE.

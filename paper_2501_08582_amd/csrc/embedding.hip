@@ -343,8 +343,46 @@ __global__ __launch_bounds__(NT) void chunk_kernel(uint32_t chunks, uint32_t voc
     store_unit(part + chunk * cols + col, narrow<float>(acc), left);
 }
 
-// The lanes' units are those of what they write: N elements of G are 16 bytes.
-template <typename T, typename G, int TL>
+// A lane's part of a row of the gradient: elements first .. first + n - 1.  Its units
+// are those of what it writes, N elements of G being 16 bytes.  SHIFT: rows start
+// anywhere in a cache line of 128 bytes, and the units are counted from the line's
+// start: no line but a row's first and last is written by two waves, and those two go
+// through the cache, where their parts meet.  Lookup and gradient of 1501 tokens into
+// 50021 rows, against units counted from the row's start: x 771 fp32 48.5 us (55.8),
+// x 1544 bf16 45.8 (54.6); x 1541 bf16 73.8 both ways (a row that starts at an odd element
+// ends in units written one element at a time); 768 fp32, where nothing shifts, 46.
+// Lanes without a part stay (the search needs all of them): they read the row's
+// first unit, and store nothing.
+template <typename G, bool SHIFT>
+struct Part {
+    static constexpr int N = kUnit<G>;
+    static constexpr uint32_t kLine = 128 / sizeof(G);
+    int64_t first;
+    int n;
+    bool real, inner;  // inner: all of the part's line is this row's
+    __device__ __forceinline__ Part(int64_t unit, uint32_t v, int64_t cols, uint32_t phase) {
+        const uint32_t before = SHIFT ? (v * (uint32_t)cols + phase) & (kLine - 1) : 0;
+        const int64_t c = unit * N - before, end = min(c + N, cols);
+        first = c > 0 ? c : 0;
+        real = first < end;
+        inner = !SHIFT || (unit * N >= (before != 0 ? kLine : 0) && unit * N < ((cols + before) & ~(int64_t)(kLine - 1)));
+        if (!real) first = 0;
+        n = (int)((real ? end : min((int64_t)N, cols)) - first);
+    }
+    __device__ __forceinline__ void store(G* row, const F<N>& f) const {
+        if (!real) return;
+        if (inner) stream_unit(row + first, narrow<G>(f), n);
+        else store_unit(row + first, narrow<G>(f), n);
+    }
+};
+
+// Elements from the start of a cache line to p.
+template <typename G>
+__device__ __forceinline__ uint32_t phase_of(const G* p) {
+    return (uint32_t)((uintptr_t)p / sizeof(G)) & (Part<G, true>::kLine - 1);
+}
+
+template <typename T, typename G, int TL, bool SHIFT>
 __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t vocab, int64_t cols, uint32_t tiles,
                                                   uint32_t per, float scale, const uint2* __restrict__ sorted,
                                                   const T* __restrict__ dY, const float* __restrict__ part,
@@ -353,23 +391,21 @@ __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t voca
     const uint32_t group = block_id() * (NT / TL) + uniform<TL>(threadIdx.x / TL);
     const uint32_t v0 = group / tiles * per;
     if (v0 >= vocab) return;
-    int64_t col = ((int64_t)(group % tiles) * TL + threadIdx.x % TL) * N;
-    // lanes past the row stay (the search needs them): they read its first unit
-    const bool real = col < cols;
-    if (!real) col = 0;
-    const int left = (int)min(cols - col, (int64_t)N);
+    const int64_t unit = (int64_t)(group % tiles) * TL + threadIdx.x % TL;
+    const uint32_t phase = phase_of(dE);
     uint32_t pos = lower_bound<TL>(sorted, tokens, v0);
     uint32_t next = pos < tokens ? uniform<TL>(sorted[pos].x) : ~0u;
     for (uint32_t v = v0; v < min(v0 + per, vocab); ++v) {
+        const Part<G, SHIFT> at(unit, v, cols, phase);
         F<N> acc = {};
         while (next == v) {
             if (pos % kChunk == 0 && tokens - pos >= kChunk && sorted[pos + kChunk - 1].x == v) {
                 // whole chunks of a frequent token: their sums are there
                 const uint32_t n = (lower_bound<TL>(sorted, tokens, v + 1) - pos) / kChunk;
-                const float* p = part + (int64_t)(pos / kChunk) * cols + col;
+                const float* p = part + (int64_t)(pos / kChunk) * cols + at.first;
 #pragma unroll 8
                 for (uint32_t i = 0; i < n; ++i) {
-                    const F<N> f = widen(load_unit<float, N>(p + i * cols, left));
+                    const F<N> f = widen(load_unit<float, N>(p + i * cols, at.n));
 #pragma unroll
                     for (int e = 0; e < N; ++e) acc.v[e] += f.v[e];
                 }
@@ -384,14 +420,14 @@ __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t voca
                     pair[i] = i < room ? sorted[pos + i] : uint2{~0u, 0u};
                     n += pair[i].x == v;
                 }
-                add_tokens(acc, pair, n, dY, cols, col, left);
+                add_tokens(acc, pair, n, dY, cols, at.first, at.n);
                 pos += n;
             }
             next = pos < tokens ? uniform<TL>(sorted[pos].x) : ~0u;
         }
 #pragma unroll
         for (int e = 0; e < N; ++e) acc.v[e] *= scale;
-        if (real) stream_unit(dE + (int64_t)v * cols + col, narrow<G>(acc), left);
+        at.store(dE + (int64_t)v * cols, acc);
     }
 }
 
@@ -402,7 +438,7 @@ __global__ __launch_bounds__(NT) void rows_kernel(uint32_t tokens, uint32_t voca
 // tokens of one id take 31 us against 14, 512 (with 8 ids a lane) 60 against 14, which is
 // why it ends at 256.
 constexpr int kFewIds = 4;
-template <typename T, typename G, bool I64>
+template <typename T, typename G, bool I64, bool SHIFT>
 __global__ __launch_bounds__(NT) void rows_few_kernel(int tokens, uint32_t vocab, int64_t cols, uint32_t tiles,
                                                       uint32_t per, float scale, const void* __restrict__ ids,
                                                       const T* __restrict__ dY, G* __restrict__ dE) {
@@ -414,11 +450,10 @@ __global__ __launch_bounds__(NT) void rows_few_kernel(int tokens, uint32_t vocab
     uint32_t key[kFewIds];  // `vocab` and all ones are no row's id
 #pragma unroll
     for (int q = 0; q < kFewIds; ++q) key[q] = q * 64 + lane < tokens ? id_of<I64>(ids, q * 64 + lane, vocab) : ~0u;
-    int64_t col = ((int64_t)(group % tiles) * 64 + lane) * N;
-    const bool real = col < cols;
-    if (!real) col = 0;
-    const int left = (int)min(cols - col, (int64_t)N);
+    const int64_t unit = (int64_t)(group % tiles) * 64 + lane;
+    const uint32_t phase = phase_of(dE);
     for (uint32_t v = v0; v < min(v0 + per, vocab); ++v) {
+        const Part<G, SHIFT> at(unit, v, cols, phase);
         F<N> acc = {};
 #pragma unroll
         for (int q = 0; q < kFewIds; ++q) {
@@ -432,12 +467,12 @@ __global__ __launch_bounds__(NT) void rows_few_kernel(int tokens, uint32_t vocab
                     n += mine != 0;
                     mine &= mine - 1;
                 }
-                add_tokens(acc, pair, n, dY, cols, col, left);
+                add_tokens(acc, pair, n, dY, cols, at.first, at.n);
             }
         }
 #pragma unroll
         for (int e = 0; e < N; ++e) acc.v[e] *= scale;
-        if (real) stream_unit(dE + (int64_t)v * cols + col, narrow<G>(acc), left);
+        at.store(dE + (int64_t)v * cols, acc);
     }
 }
 
@@ -531,7 +566,18 @@ uint32_t rows_per_group(int64_t vocab, int64_t tiles) {
     return per;
 }
 
-template <typename T, typename G, int TL>
+// Whether rows of the gradient start inside cache lines, and the tiles of a row then:
+// a row and what its first line has before it.
+template <typename G>
+bool shifted(const EmbeddingArgs& a) {
+    return a.cols * sizeof(G) % 128 != 0 || (uintptr_t)a.dE % 128 != 0;
+}
+template <typename G>
+uint32_t row_tiles(const EmbeddingArgs& a, int64_t width, bool shift) {
+    return (uint32_t)((a.cols + (shift ? Part<G, true>::kLine - 1 : 0) + width - 1) / width);
+}
+
+template <typename T, typename G, int TL, bool SHIFT>
 hipError_t sums(const EmbeddingArgs& a, const uint2* sorted, float* part, hipStream_t s) {
     // fewer groups than 2^32: checked where the call is
     constexpr int N = kUnit<G>;
@@ -539,37 +585,38 @@ hipError_t sums(const EmbeddingArgs& a, const uint2* sorted, float* part, hipStr
     const uint32_t chunks = (uint32_t)(a.tokens / kChunk);
     const int64_t per = NT / TL;
     const int64_t chunk_blocks = ((int64_t)chunks * tiles + per - 1) / per;
-    const uint32_t rows = rows_per_group(a.vocab, tiles);
-    const int64_t row_blocks = ((a.vocab + rows - 1) / rows * tiles + per - 1) / per;
+    const uint32_t wide = row_tiles<G>(a, TL * N, SHIFT), rows = rows_per_group(a.vocab, wide);
+    const int64_t row_blocks = ((a.vocab + rows - 1) / rows * wide + per - 1) / per;
     if (chunks > 0)
         hipLaunchKernelGGL((chunk_kernel<T, N, TL>), grid_of(chunk_blocks), dim3(NT), 0, s, chunks,
                            (uint32_t)a.vocab, a.cols, tiles, sorted, (const T*)a.dY, part);
-    hipLaunchKernelGGL((rows_kernel<T, G, TL>), grid_of(row_blocks), dim3(NT), 0, s, (uint32_t)a.tokens,
-                       (uint32_t)a.vocab, a.cols, tiles, rows, a.scale, sorted, (const T*)a.dY, part, (G*)a.dE);
+    hipLaunchKernelGGL((rows_kernel<T, G, TL, SHIFT>), grid_of(row_blocks), dim3(NT), 0, s, (uint32_t)a.tokens,
+                       (uint32_t)a.vocab, a.cols, wide, rows, a.scale, sorted, (const T*)a.dY, part, (G*)a.dE);
     return hipGetLastError();
 }
 
 template <typename T, typename G>
 hipError_t backward(const EmbeddingArgs& a, hipStream_t s) {
     if (a.tokens <= kFewMost) {
-        const uint32_t tiles = (uint32_t)((a.cols + 64 * kUnit<G> - 1) / (64 * kUnit<G>));
+        const bool shift = shifted<G>(a);
+        const uint32_t tiles = row_tiles<G>(a, 64 * kUnit<G>, shift);
         const uint32_t per = rows_per_group(a.vocab, tiles);
         const int64_t blocks = ((a.vocab + per - 1) / per * tiles + NT / 64 - 1) / (NT / 64);
         auto launch = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, grid_of(blocks), dim3(NT), 0, s, (int)a.tokens, (uint32_t)a.vocab, a.cols, tiles, per,
                                a.scale, a.ids, (const T*)a.dY, (G*)a.dE);
         };
-        if (a.index64) launch(rows_few_kernel<T, G, true>);
-        else launch(rows_few_kernel<T, G, false>);
+        if (shift) launch(a.index64 ? rows_few_kernel<T, G, true, true> : rows_few_kernel<T, G, false, true>);
+        else launch(a.index64 ? rows_few_kernel<T, G, true, false> : rows_few_kernel<T, G, false, false>);
         return hipGetLastError();
     }
     const Layout w = layout_of(a.tokens, a.cols);
     const uint2* sorted = a.index64 ? sort<true>(a, w, s) : sort<false>(a, w, s);
     float* part = (float*)((uint8_t*)a.workspace + w.part);
     const int64_t units = (a.cols + kUnit<G> - 1) / kUnit<G>;
-    if (units <= 8) return sums<T, G, 8>(a, sorted, part, s);
-    if (units <= 16) return sums<T, G, 16>(a, sorted, part, s);
-    return sums<T, G, 64>(a, sorted, part, s);
+    if (units <= 8) return sums<T, G, 8, false>(a, sorted, part, s);
+    if (units <= 16) return sums<T, G, 16, false>(a, sorted, part, s);
+    return shifted<G>(a) ? sums<T, G, 64, true>(a, sorted, part, s) : sums<T, G, 64, false>(a, sorted, part, s);
 }
 
 template <typename T>
@@ -590,7 +637,8 @@ hipError_t forward(const EmbeddingArgs& a, hipStream_t s) {
 
 bool embedding_groups_fit(int64_t tokens, int64_t vocab, int64_t cols) {
     const int64_t rows = std::max((vocab + kRows - 1) / kRows, tokens / kChunk);
-    return (cols + 255) / 256 * rows < (int64_t)1 << 31;  // tiles of 256 columns at least; narrower groups have one
+    // tiles of 256 columns at least, one more for the line that a row starts in; narrower groups have one
+    return ((cols + 255) / 256 + 1) * rows < (int64_t)1 << 31;
 }
 
 size_t embedding_workspace_bytes(int64_t tokens, int64_t, int64_t cols) { return layout_of(tokens, cols).bytes; }

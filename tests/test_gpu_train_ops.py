@@ -282,6 +282,29 @@ def test_embedding_padding_ignores_its_values_and_empty_batches():
     assert not train.embedding_backward(torch.empty(0, 33, device="cuda"), none, 10).any()
 
 
+@pytest.mark.parametrize("grad", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab,cols", [
+    (3, 9, 1), (40, 21, 31), (40, 21, 32), (300, 21, 33), (300, 50, 64), (300, 33, 257), (260, 40, 1030), (70, 16, 2049)])
+def test_embedding_gradient_at_any_address(n, vocab, cols, grad):
+    """A table that starts anywhere in a cache line: the same gradient, and nothing
+    written around it."""
+    rng = np.random.default_rng(n + cols)
+    ids = torch.from_numpy(_ids(rng, n, vocab, "padded")).cuda()
+    dy, _ = normal(rng, (n, cols), "bf16")
+    want = train.embedding_backward(dy, ids, vocab, 0.5, grad_dtype=DT[grad])
+    d = train._embedding(ids, vocab, cols, 0.5, _lib.DTYPE_BF16, _lib.DTYPE_BF16 if grad == "bf16" else _lib.DTYPE_F32)
+    need = _lib.embedding_workspace_bytes(d)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    for shift in (1, 2, 31, 33, 63, 64):
+        buf = torch.full((vocab * cols + 256,), 7.0, dtype=DT[grad], device="cuda")
+        dE = buf[shift:shift + vocab * cols]
+        status = _lib.embedding_backward(d, ids.data_ptr(), dy.data_ptr(), dE.data_ptr(), ws.data_ptr(), need,
+                                         torch.cuda.current_stream().cuda_stream)
+        assert status == 0
+        assert torch.equal(dE.view(vocab, cols), want), shift
+        assert (buf[:shift] == 7).all() and (buf[shift + vocab * cols:] == 7).all(), shift
+
+
 # ---------------------------------------------------------------------------
 # log-probabilities.  With t = x - top, a term's exponent is rounded twice and its
 # exponential once: (3 |t| + 2) 2^-24 of it.  The sum takes vocab / 2048 steps in a
