@@ -9,6 +9,8 @@ own rounding, and a second one where the fp32 value lands on the other side of a
 `scale` the size of the terms that fp32 arithmetic rounds on the way and `c` the
 number of such roundings.  Each test says how its c comes about.
 """
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -21,6 +23,14 @@ pytestmark = pytest.mark.gpu
 U = {torch.bfloat16: 2.0**-8 * (1 + 2.0**-7), torch.float32: 2.0**-23}
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 SEED, OFFSET = 0x9E3779B97F4A7C15, (5 << 32) + 77
+
+
+@pytest.fixture(scope="module", autouse=True)
+def no_tensors_left_behind():
+    """A caught exception that a test keeps holds that test's frame, and so its tensors,
+    in a cycle.  It is collected here, not while a later test watches the allocator."""
+    yield
+    gc.collect()
 
 
 def f64(t):
