@@ -68,10 +68,7 @@ struct Running {
         for (int i = 0; i < B; ++i)
 #pragma unroll
             for (int e = 0; e < N; ++e) m = fmaxf(m, x[i].v[e]);
-        if (m > top) {
-            sum = top == kNone ? 0.f : sum * exp2_hw((top - m) * kLog2e);
-            top = m;
-        }
+        if (m > top) rescale(m);
         const float ref = top == kNone ? 0.f : top;  // all -Inf so far: they add nothing
         float s[N] = {};
 #pragma unroll
@@ -83,7 +80,8 @@ struct Running {
     }
 
     __device__ __forceinline__ void rescale(float to) {
-        sum = top == kNone ? sum : sum * exp2_hw((top - to) * kLog2e);  // a NaN sum stays
+        // below a top of -Inf the sum is 0, or NaN where a NaN was among the entries: it stays
+        sum = top == kNone ? sum : sum * exp2_hw((top - to) * kLog2e);
         top = to;
     }
 };
