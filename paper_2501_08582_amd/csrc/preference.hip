@@ -290,7 +290,9 @@ __device__ __forceinline__ void add_pair(double (&sum)[2], int64_t i, int64_t pa
     }
 }
 
-// The results of pair i from its sums; its loss is returned.
+// The rewards of pair i from its sums, and dseq of its preferred sequence; its loss is
+// returned.  The margin is a small difference of rewards that may be large: it exists
+// in 64 bits only.
 __device__ __forceinline__ double finish_pair(double won, double lost, int64_t i, int64_t pairs, double beta, double e,
                                               float* reward, float* dseq) {
     won *= beta;
@@ -298,10 +300,7 @@ __device__ __forceinline__ double finish_pair(double won, double lost, int64_t i
     const double margin = won - lost;
     reward[i] = (float)won;
     reward[pairs + i] = (float)lost;
-    const double d =
-        beta / (double)pairs * (e * exp(log_sigmoid(margin)) - (1.0 - e) * exp(log_sigmoid(-margin)));
-    dseq[i] = (float)d;
-    dseq[pairs + i] = (float)-d;
+    dseq[i] = (float)(beta / (double)pairs * (e * exp(log_sigmoid(margin)) - (1.0 - e) * exp(log_sigmoid(-margin))));
     return pair_loss(margin, e);
 }
 
@@ -338,6 +337,7 @@ __global__ __launch_bounds__(64 * kWaves) void preference_one_kernel(int pairs, 
 #pragma unroll
             for (int side = 0; side < 2; ++side) s[side] += sums[side][i * segs + seg];
         total += finish_pair(s[0], s[1], i, pairs, beta, e, reward, dseq);
+        dseq[pairs + i] = -dseq[i];
     }
     total = wave_sum(total);
     if (lane == 0) totals[wave] = total;
@@ -348,7 +348,9 @@ __global__ __launch_bounds__(64 * kWaves) void preference_one_kernel(int pairs, 
     *loss = (float)(total / (double)pairs);
 }
 
-// Many: a workgroup to a pair; preference_mean_kernel takes the mean.
+// Many: a workgroup to a pair.  Its loss, rounded to fp32 (2^-24 of it, as the mean will
+// be), waits in the place of the rejected sequence's dseq, which is the preferred one's
+// negated: preference_mean_kernel takes the mean and puts that there.
 template <bool I64>
 __global__ __launch_bounds__(64 * kWaves) void preference_kernel(int64_t pairs, int64_t length, uint32_t vocab,
                                                                  double beta, double e, const float* __restrict__ logp,
@@ -372,17 +374,18 @@ __global__ __launch_bounds__(64 * kWaves) void preference_kernel(int64_t pairs, 
         for (int w = 0; w < kWaves; ++w)
 #pragma unroll
             for (int side = 0; side < 2; ++side) s[side] += lds[side][w];
-        finish_pair(s[0], s[1], i, pairs, beta, e, reward, dseq);
+        dseq[pairs + i] = (float)finish_pair(s[0], s[1], i, pairs, beta, e, reward, dseq);
     }
 }
 
-__global__ __launch_bounds__(64 * kWaves) void preference_mean_kernel(int64_t pairs, double e,
-                                                                      const float* __restrict__ reward,
+__global__ __launch_bounds__(64 * kWaves) void preference_mean_kernel(int64_t pairs, float* __restrict__ dseq,
                                                                       float* __restrict__ loss) {
     __shared__ double lds[kWaves];
     double total = 0.0;
-    for (int64_t i = threadIdx.x; i < pairs; i += 64 * kWaves)
-        total += pair_loss((double)reward[i] - (double)reward[pairs + i], e);
+    for (int64_t i = threadIdx.x; i < pairs; i += 64 * kWaves) {
+        total += (double)dseq[pairs + i];
+        dseq[pairs + i] = -dseq[i];
+    }
     total = wave_sum(total);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = total;
     __syncthreads();
@@ -456,8 +459,7 @@ hipError_t preference(const PreferenceArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(preference_kernel<I64>, dim3((unsigned)std::min<int64_t>(a.pairs, 65536)), block, 0, s,
                        a.pairs, a.length, (uint32_t)a.vocab, a.beta, a.smoothing, a.logp, a.ref, a.targets, a.reward,
                        a.dseq);
-    hipLaunchKernelGGL(preference_mean_kernel, dim3(1), dim3(64 * kWaves), 0, s, a.pairs, a.smoothing, a.reward,
-                       a.loss);
+    hipLaunchKernelGGL(preference_mean_kernel, dim3(1), dim3(64 * kWaves), 0, s, a.pairs, a.dseq, a.loss);
     return hipGetLastError();
 }
 

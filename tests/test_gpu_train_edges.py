@@ -35,3 +35,25 @@ def test_logprobs_keep_a_nan_before_finite_entries(rows, V, dtype):
             # the other rows: V / 2048 steps, fewer than 64 joins and 4 |t| <= 4 . 12 roundings of the sum
             want, _, _ = ot.logprobs(f64(x[:-1][:4]), np.full(min(rows - 1, 4), V - 1))
             check("logp", logp[:-1][:4], want, 48 + 64 + V / 2048, 1)
+
+
+# ---------------------------------------------------------------------------
+# the paired loss of long sequences whose rewards are large and close: the margin is
+# taken in 64 bits, where fewer than 2^13 roundings of 2^-53 of a reward are 2^-40 of it,
+# and a pair's loss and the mean are rounded to fp32 once each
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("P,S,smoothing", [(8, 2048, 0.0), (4, 4096, 0.1), (1, 70000, 0.0), (600, 40, 0.2), (513, 1, 0.0)])
+def test_preference_of_close_large_rewards(P, S, smoothing):
+    rng = np.random.default_rng(P + S)
+    won = rng.standard_normal((P, S)) * 2.0 - 60.0
+    lost = won + rng.standard_normal((P, S)) * (10.0 / S**0.5)
+    logp = torch.from_numpy(np.concatenate([won, lost]).astype(np.float32)).cuda()
+    l64 = f64(logp)
+    targets = torch.zeros(2 * P, S, dtype=torch.int64, device="cuda")
+    loss, reward, dseq = train.preference_forward(logp, targets, 9, None, 0.1, smoothing)
+    want = ot.preference(l64, np.ones_like(l64, dtype=bool), None, 0.1, smoothing)
+    size = 0.1 * np.abs(l64).sum(1).max() * 2.0**-16
+    check("reward", reward, want[1], size, 1)
+    check("loss", loss, np.asarray(want[0]), size, 1)
+    check("dseq", dseq, want[2], size * 0.1 / P, 1)
+    assert torch.equal(dseq[:P], -dseq[P:])
