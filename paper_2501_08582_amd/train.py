@@ -415,17 +415,28 @@ def preference_forward(logp: torch.Tensor, targets: torch.Tensor, vocab: int, re
     ones first: reward = beta * sum over counted tokens of (logp - ref), loss the mean over pairs
     of -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m) with m the pair's difference of
     rewards, dseq the loss's gradient by each sequence's summed log-probability."""
+    return _preference_forward(logp, targets, vocab, ref, beta, smoothing, shared=True)
+
+
+def _preference_forward(logp, targets, vocab, ref, beta, smoothing, shared: bool):
+    """``shared``: the results are views of one allocation.  Autograd takes none of those
+    for the outputs of an op that a program may change in place."""
     dev = _place(logp, targets, ref)
     if logp.dim() != 2 or logp.shape[0] % 2 != 0:
         raise ValueError("expected 2 P x length: the preferred sequences, then the rejected ones")
     _fp32(targets.shape, "logp, ref", logp, ref)
     P = logp.shape[0] // 2
     d = _lib.Preference(P, logp.shape[1], vocab, beta, smoothing, _index(targets, "targets"), 0)
-    out = torch.empty(4 * P + 1, dtype=torch.float32, device=dev)  # reward, dseq, loss: one allocation
-    reward, dseq, loss = out.split((2 * P, 2 * P, 1))
-    at = out.data_ptr()
-    _call(dev, "lors_preference", _lib.preference, d, _ptr(logp), _ptr(ref), _ptr(targets), at + 16 * P, at, at + 8 * P)
-    return loss.view(()), reward, dseq
+    if shared:
+        out = torch.empty(4 * P + 1, dtype=torch.float32, device=dev)
+        reward, dseq, loss = out.split((2 * P, 2 * P, 1))
+        loss, at = loss.view(()), out.data_ptr()
+        places = at + 16 * P, at, at + 8 * P
+    else:
+        loss, reward, dseq = (torch.empty(n, dtype=torch.float32, device=dev) for n in ((), 2 * P, 2 * P))
+        places = _ptr(loss), _ptr(reward), _ptr(dseq)
+    _call(dev, "lors_preference", _lib.preference, d, _ptr(logp), _ptr(ref), _ptr(targets), *places)
+    return loss, reward, dseq
 
 
 def preference_step(logits: torch.Tensor, targets: torch.Tensor, ref: Optional[torch.Tensor] = None,
@@ -445,7 +456,7 @@ class PreferenceLossFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, ref, beta, smoothing):
         logp, stats = logprob_forward(logits, targets)
-        loss, reward, dseq = preference_forward(logp, targets, logits.shape[-1], ref, beta, smoothing)
+        loss, reward, dseq = _preference_forward(logp, targets, logits.shape[-1], ref, beta, smoothing, shared=False)
         ctx.save_for_backward(logits, targets, stats, dseq)
         ctx.mark_non_differentiable(reward, logp)
         return loss, reward, logp

@@ -57,3 +57,29 @@ def test_preference_of_close_large_rewards(P, S, smoothing):
     check("loss", loss, np.asarray(want[0]), size, 1)
     check("dseq", dseq, want[2], size * 0.1 / P, 1)
     assert torch.equal(dseq[:P], -dseq[P:])
+
+
+# ---------------------------------------------------------------------------
+# results of the paired loss under autograd, changed in place
+# ---------------------------------------------------------------------------
+def test_results_of_the_preference_loss_can_be_changed_in_place():
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(4, 7, 99, generator=g, device="cuda", requires_grad=True)
+    t = torch.randint(0, 99, (4, 7), generator=g, device="cuda")
+    first, first_reward, _ = train.preference_loss(x, t, None, 0.2)
+    (want,) = torch.autograd.grad(first, x)
+    loss, reward, logp = train.preference_loss(x, t, None, 0.2)
+    loss /= 2  # halves the gradient, exactly
+    reward.mul_(3)
+    logp.zero_()
+    (got,) = torch.autograd.grad(loss, x)
+    assert torch.equal(got, want / 2) and float(loss.detach()) == float(first.detach()) / 2
+    assert torch.equal(reward, 3 * first_reward)
+    loss, _, _ = train.preference_loss(x, t, None, 0.2)
+    loss += x.square().sum()
+    (got,) = torch.autograd.grad(loss, x)
+    assert torch.equal(got, want + 2 * x.detach())
+    loss, reward, _ = train.preference_loss(x, t, None, 0.2)
+    loss.detach().mul_(0)
+    (got,) = torch.autograd.grad(loss, x)
+    assert torch.equal(got, want) and torch.equal(reward, first_reward)
