@@ -178,10 +178,49 @@ __global__ __launch_bounds__(kSortThreads) void digit_count_kernel(int64_t token
     counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
 }
 
-// SELF: counts is not there.
+// The counts of many tiles become the places' starts: of every tile and digit the tokens
+// of that digit in earlier tiles, and in a last row those of all.  A lane to a digit, a run of
+// tiles to a wave, kScanAhead of them in flight.  Without it every workgroup of the
+// placement reads all tiles' counts, which grows with the square of the tokens.
+constexpr int kScanWaves = 16;
+constexpr int kScanAhead = 8;
+
+__global__ __launch_bounds__(64 * kScanWaves) void digit_scan_kernel(int64_t tiles, uint32_t* __restrict__ counts) {
+    __shared__ uint32_t total[kScanWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t begin = tiles * wave / kScanWaves, end = tiles * (wave + 1) / kScanWaves;
+    uint32_t* const column = counts + blockIdx.x * 64 + lane;
+    auto load = [&](uint32_t (&c)[kScanAhead], int64_t b) {
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i) c[i] = b + i < end ? column[(b + i) * kDigits] : 0;
+    };
+    uint32_t sum = 0;
+    for (int64_t b = begin; b < end; b += kScanAhead) {
+        uint32_t c[kScanAhead];
+        load(c, b);
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i) sum += c[i];
+    }
+    total[wave][lane] = sum;
+    __syncthreads();
+    uint32_t at = 0;
+    for (int w = 0; w < wave; ++w) at += total[w][lane];
+    for (int64_t b = begin; b < end; b += kScanAhead) {
+        uint32_t c[kScanAhead];
+        load(c, b);
+#pragma unroll
+        for (int i = 0; i < kScanAhead; ++i) {
+            if (b + i < end) column[(b + i) * kDigits] = at;
+            at += c[i];
+        }
+    }
+    if (wave == kScanWaves - 1) column[tiles * kDigits] = at;
+}
+
+// SELF: counts is not there.  scanned: digit_scan_kernel has made starts of them.
 template <int Q, bool SELF, bool FIRST, bool I64>
 __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(int64_t tokens, uint32_t vocab, int shift,
-                                                                   const void* __restrict__ ids,
+                                                                   bool scanned, const void* __restrict__ ids,
                                                                    const uint2* __restrict__ in,
                                                                    const uint32_t* __restrict__ counts,
                                                                    uint2* __restrict__ out) {
@@ -210,11 +249,16 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(int64_t token
         earlier = others[0][threadIdx.x];
         all = earlier + others[1][threadIdx.x];
     } else {
+        if (scanned) {
+            earlier = counts[(int64_t)blockIdx.x * kDigits + threadIdx.x];
+            all = counts[(int64_t)gridDim.x * kDigits + threadIdx.x];
+        } else {
 #pragma unroll 4
-        for (uint32_t b = 0; b < gridDim.x; ++b) {
-            const uint32_t c = counts[(int64_t)b * kDigits + threadIdx.x];
-            all += c;
-            if (b < blockIdx.x) earlier += c;
+            for (uint32_t b = 0; b < gridDim.x; ++b) {
+                const uint32_t c = counts[(int64_t)b * kDigits + threadIdx.x];
+                all += c;
+                if (b < blockIdx.x) earlier += c;
+            }
         }
         __syncthreads();
     }
@@ -485,11 +529,14 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // digits in short tiles.  Whole gradient of a table of 64 rows, us: 4096 tokens 20.7 by
 // counting, 20.9 by digits; 6144 26 and 22; 8192 digits counted by all 25, by a
 // launch 25; 12288 31 and 25; 65536 tokens in tiles of 1024 32, 131072 in tiles of
-// 4096 37.
+// 4096 37.  Counts of the tiles scanned by a launch of its own against read by every
+// workgroup, tokens into 512 x 8: 131072 (32 tiles) 87 and 85, 262144 (64) 94 and 95, 524288
+// 106 and 115, 4194304 349 and 471; the latter goes on with the square.
 constexpr int64_t kFewMost = 64 * kFewIds;  // tokens that are not sorted
 constexpr int64_t kRankMost = 4096;
 constexpr int64_t kSelfMost = 8192;
 constexpr int64_t kShortMost = 65536;
+constexpr int64_t kUnscannedTiles = 64;  // more tiles than these have their counts scanned
 
 int digit_passes(int64_t vocab) {
     int bits = 1;
@@ -514,19 +561,23 @@ Layout layout_of(int64_t tokens, int64_t cols) {
     const bool digits = tokens > kRankMost;
     w.other = pairs;
     w.counts = digits ? 2 * pairs : pairs;
-    w.part = w.counts + (tokens > kSelfMost ? (size_t)tiles_of(tokens) * kDigits * 4 : 0);
+    w.part = w.counts + (tokens > kSelfMost ? (size_t)(tiles_of(tokens) + 1) * kDigits * 4 : 0);  // a last row when scanned
     w.bytes = w.part + up256((size_t)(tokens / kChunk) * cols * 4);
     return w;
 }
 
 template <int Q, bool SELF, bool FIRST, bool I64>
 void digit_pass(const EmbeddingArgs& a, int shift, const uint2* in, uint32_t* counts, uint2* out, hipStream_t s) {
-    const dim3 grid((unsigned)tiles_of(a.tokens)), block(kSortThreads);
+    const int64_t tiles = tiles_of(a.tokens);
+    const dim3 grid((unsigned)tiles), block(kSortThreads);
+    const bool scan = !SELF && tiles > kUnscannedTiles;
     if constexpr (!SELF)
         hipLaunchKernelGGL((digit_count_kernel<Q, FIRST, I64>), grid, block, 0, s, a.tokens, (uint32_t)a.vocab, shift,
                            a.ids, in, counts);
+    if (scan)
+        hipLaunchKernelGGL(digit_scan_kernel, dim3(kDigits / 64), dim3(64 * kScanWaves), 0, s, tiles, counts);
     hipLaunchKernelGGL((digit_place_kernel<Q, SELF, FIRST, I64>), grid, block, 0, s, a.tokens, (uint32_t)a.vocab,
-                       shift, a.ids, in, counts, out);
+                       shift, scan, a.ids, in, counts, out);
 }
 
 // The sorted pairs, in one of the two arrays.

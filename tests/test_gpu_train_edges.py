@@ -6,7 +6,7 @@ import torch
 
 from oracle import train as ot
 from paper_2501_08582_amd import train
-from test_gpu_train_ops import DT, check, f64
+from test_gpu_train_ops import DT, check, f64, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +83,40 @@ def test_results_of_the_preference_loss_can_be_changed_in_place():
     loss.detach().mul_(0)
     (got,) = torch.autograd.grad(loss, x)
     assert torch.equal(got, want) and torch.equal(reward, first_reward)
+
+
+# ---------------------------------------------------------------------------
+# gradients of tables from so many tokens that their digits' counts are scanned
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("n,vocab,cols", [(262144, 700, 8), (262145, 700, 9), (266241, 3, 1), (700001, 300001, 4), (1 << 21, 5000, 3)])
+def test_embedding_gradient_of_very_many_tokens(n, vocab, cols):
+    rng = np.random.default_rng(n + vocab)
+    ids = rng.integers(-1, vocab + 1, n)  # some of them padding
+    dy, dy64 = normal(rng, (n, cols), "f32")
+    ok = (ids >= 0) & (ids < vocab)
+    ref, size = (np.stack([np.bincount(ids[ok], a[ok, c], vocab) for c in range(cols)], 1) for a in (dy64, np.abs(dy64)))
+    dev = torch.from_numpy(ids).cuda()
+    got = train.embedding_backward(dy, dev, vocab)
+    most = np.bincount(ids[ok]).max()  # in chunks of 32, then their sums, one after the other
+    check("dE", got, ref, size, 66 + most / 32)
+    assert torch.equal(train.embedding_backward(dy, dev.to(torch.int32), vocab), got)
+
+
+def test_embedding_gradient_takes_time_in_proportion_to_its_tokens():
+    times = []
+    for n in (1 << 22, 1 << 26):
+        ids = torch.randint(0, 512, (n,), dtype=torch.int32, device="cuda")
+        dy = torch.ones(n, 1, device="cuda")
+        got = train.embedding_backward(dy, ids, 512)  # sums of ones below 2^24 are exact
+        assert torch.equal(got[:, 0].long(), torch.bincount(ids, minlength=512))
+        best = float("inf")
+        for _ in range(3):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            train.embedding_backward(dy, ids, 512)
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        times.append(best)
+    # 16 times the tokens; a term with their square would be 256 times as large
+    assert times[1] < 40 * times[0], times
