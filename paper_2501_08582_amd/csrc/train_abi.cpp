@@ -123,9 +123,10 @@ lors_status_t lors_dropout(const lors_dropout_t* p, const void* X, const void* r
 // ---------------------------------------------------------------------------
 static lors_status_t check_norm(const lors_norm_t* p) {
     if (!valid_dtype(p->dtype) || !valid_dtype(p->grad_dtype)) return LORS_ERR_DTYPE;
+    if (p->kind != LORS_NORM_LAYER && p->kind != LORS_NORM_RMS) return LORS_ERR_UNSUPPORTED;
     if (p->rows < 0 || p->rows > kMaxExtent || p->cols < 1 || p->cols > LORS_NORM_MAX_COLS) return LORS_ERR_SHAPE;
     if (!std::isfinite(p->eps) || p->eps < 0.0 || threshold_of(p->p) < 0) return LORS_ERR_SHAPE;
-    if ((p->kind != LORS_NORM_LAYER && p->kind != LORS_NORM_RMS) || p->flags != 0) return LORS_ERR_UNSUPPORTED;
+    if (p->flags != 0) return LORS_ERR_UNSUPPORTED;
     return LORS_OK;
 }
 
