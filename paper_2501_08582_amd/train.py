@@ -133,8 +133,7 @@ def dropout(X: torch.Tensor, p: float, seed: int, offset: int = 0, residual: Opt
     d = _lib.Dropout(rows, cols, p, _rng(p, seed, offset, rng_state), _dt(X), 0)
     if out is None:
         out = torch.empty_like(X)
-    if rows:
-        _call(dev, "lors_dropout", _lib.dropout, d, X.data_ptr(), _ptr(residual), out.data_ptr())
+    _call(dev, "lors_dropout", _lib.dropout, d, X.data_ptr(), _ptr(residual), out.data_ptr())
     return out
 
 
@@ -182,9 +181,8 @@ def norm_forward(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: O
     Z = torch.empty_like(X) if residual is not None or _drops(p) else None
     rstd = torch.empty(X.shape[:-1], dtype=torch.float32, device=dev) if need_stats else None
     mean = torch.empty_like(rstd) if need_stats and k == _lib.NORM_LAYER else None
-    if rows:
-        _call(dev, "lors_norm_forward", _lib.norm_forward, d, X.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias),
-              Y.data_ptr(), _ptr(Z), _ptr(mean), _ptr(rstd))
+    _call(dev, "lors_norm_forward", _lib.norm_forward, d, X.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias),
+          Y.data_ptr(), _ptr(Z), _ptr(mean), _ptr(rstd))
     return Y, X if Z is None else Z, mean, rstd
 
 

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import train as ot
-from paper_2501_08582_amd import train
+from paper_2501_08582_amd import _lib, train
 from test_gpu_train_ops import DT, check, f64, normal
 
 pytestmark = pytest.mark.gpu
@@ -120,3 +120,23 @@ def test_embedding_gradient_takes_time_in_proportion_to_its_tokens():
         times.append(best)
     # 16 times the tokens; a term with their square would be 256 times as large
     assert times[1] < 40 * times[0], times
+
+
+# ---------------------------------------------------------------------------
+# empty batches: refusals are the same
+# ---------------------------------------------------------------------------
+def test_empty_batches_are_checked_too():
+    x = torch.empty(0, 8, device="cuda")
+    assert train.dropout(x, 0.1, 1, residual=x.clone()).shape == (0, 8)
+    y, z, mean, rstd = train.norm_forward(x, torch.ones(8, device="cuda"), residual=x.clone(), p=0.1)
+    assert y.shape == z.shape == (0, 8) and mean.shape == rstd.shape == (0,)
+    for p in (-0.1, 1.0, float("nan")):
+        for call in (lambda: train.dropout(x, p, 0), lambda: train.norm_forward(x, p=p)):
+            with pytest.raises(_lib.LorsError) as e:
+                call()
+            assert e.value.status == _lib.ERR_SHAPE
+            del e
+    with pytest.raises(_lib.LorsError):
+        train.norm_forward(x, eps=-1.0)
+    with pytest.raises(_lib.LorsError):
+        train.norm_forward(torch.empty(0, 32769, device="cuda"))
