@@ -140,3 +140,30 @@ def test_empty_batches_are_checked_too():
         train.norm_forward(x, eps=-1.0)
     with pytest.raises(_lib.LorsError):
         train.norm_forward(torch.empty(0, 32769, device="cuda"))
+
+
+# ---------------------------------------------------------------------------
+# the norm's weight gradients in bf16, the type that training asks for: those in fp32
+# rounded once, and a bound of their own.  Each of its 8 sums of `rows` terms has fewer
+# than 256 roundings in a chain, h is off by 128 of (|z| rstd + |h|).
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,kind", [(1, 40, "rms"), (7, 1000, "layer"), (700, 333, "rms"), (600, 5120, "layer"),
+                                            (300, 20000, "rms")])
+def test_norm_weight_gradients_in_bf16(rows, cols, kind, dtype):
+    rng = np.random.default_rng(rows + cols)
+    z, z64 = normal(rng, (rows, cols), dtype, 1.5, 0.7)
+    dy, dy64 = normal(rng, (rows, cols), dtype)
+    w, w64 = normal(rng, cols, dtype, 0.2, 1.0)
+    _, _, mean, rstd = train.norm_forward(z, w, kind=kind)
+    _, _, dw, db = train.norm_backward(dy, z, w, mean, rstd, kind, need_dbias=True, grad_dtype=torch.bfloat16)
+    _, _, wide_w, wide_b = train.norm_backward(dy, z, w, mean, rstd, kind, need_dbias=True, grad_dtype=torch.float32)
+    assert dw.dtype == db.dtype == torch.bfloat16
+    assert torch.equal(dw, wide_w.bfloat16()) and torch.equal(db, wide_b.bfloat16())
+    eps = float(np.float32(1e-5))
+    _, want_w, want_b = ot.norm_backward(dy64, z64, w64, eps, kind == "rms")
+    m64, s64 = ot.stats(z64, eps, kind == "rms")
+    h = np.abs((z64 - m64) * s64)
+    big = np.abs(z64).max(1, keepdims=True) * s64
+    check("dweight", dw, want_w, (np.abs(dy64) * (big + h.max(1, keepdims=True) + h)).sum(0), 256)
+    check("dbias", db, want_b, np.abs(dy64).sum(0), 256)
