@@ -141,9 +141,7 @@ __global__ __launch_bounds__(64 * kRankWaves) void rank_kernel(int tokens, uint3
 // By digits of 9 bits, the lowest first.  A workgroup takes a tile of tokens and
 // places them behind those of lower digits and of earlier tiles, in their order.
 // For that it needs the digits of all tiles: of a short batch it counts them
-// itself, of a long one they are counted by a launch before.  8192 tokens, two
-// digits: 8.4 us each so, against 4.6 and 4.8 for the two launches and the time
-// between them; 16384: 12.5, against 4.6 and 4.8.
+// itself, of a long one they are counted by a launch before.
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = kDigits;  // one thread per digit where tiles are joined
@@ -526,15 +524,18 @@ __global__ __launch_bounds__(NT) void rows_few_kernel(int tokens, uint32_t vocab
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 // How many tokens are sorted by counting, by digits that every workgroup counts, by
-// digits in short tiles.  Whole gradient of a table of 64 rows, us: 4096 tokens 20.7 by
-// counting, 20.9 by digits; 6144 26 and 22; 8192 digits counted by all 25, by a
-// launch 25; 12288 31 and 25; 65536 tokens in tiles of 1024 32, 131072 in tiles of
-// 4096 37.  Counts of the tiles scanned by a launch of its own against read by every
-// workgroup, tokens into 512 x 8: 131072 (32 tiles) 87 and 85, 262144 (64) 94 and 95, 524288
-// 106 and 115, 4194304 349 and 471; the latter goes on with the square.
+// digits in short tiles.  Whole gradient, us:
+//   a table of 64 rows: 4096 tokens 20.7 by counting, 20.9 by digits; 6144 26 and 22;
+//   65536 in tiles of 1024 32, 131072 in tiles of 4096 37.
+//   Digits counted by every workgroup, or by a launch, into 64 x 64 bf16: 4224 tokens 34
+//   and 36, 6144 39.5 and 40.5, 8192 41 and 42; into 775 x 735 fp32: 22 and 23.5, 25.3 and
+//   24.6, 29 and 25.3; into 32768 x 4096 bf16: 63 and 64, 64 and 64, 64 and 61.
+//   Counts scanned by a launch, or all read by every workgroup, into 512 x 8: 131072
+//   tokens (32 tiles) 87 and 85, 262144 (64) 94 and 95, 524288 106 and 115, 4194304 349 and
+//   471; the latter goes on with the square.
 constexpr int64_t kFewMost = 64 * kFewIds;  // tokens that are not sorted
 constexpr int64_t kRankMost = 4096;
-constexpr int64_t kSelfMost = 8192;
+constexpr int64_t kSelfMost = 6144;
 constexpr int64_t kShortMost = 65536;
 constexpr int64_t kUnscannedTiles = 64;  // more tiles than these have their counts scanned
 
