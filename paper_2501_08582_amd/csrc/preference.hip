@@ -119,9 +119,10 @@ struct Rows {
     }
 };
 
-// An element takes a conversion, half a maximum, a difference, a product, an
-// exponential (a quarter of the rate) and a sum: by that count two thirds of the time
-// that the two bytes of a bf16 take.
+// An element takes a conversion, half a maximum, a difference, a product and an fma, an
+// exponential (a quarter of the rate) and a sum, 9.5 of the chip's instructions: by that count
+// three quarters of the time that the two bytes of a bf16 take.  A whole row of one
+// compute unit is bound by them: 131072 entries are 8 us of the kernel's 9.2.
 // A row's `splits` workgroups of W threads take a run of it each; with splits > 1 their (top, sum) go to
 // `part` and logprob_join_kernel finishes.
 template <typename T, bool I64, int W>
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(W) void logprob_fwd_kernel(Rows rows, uint32_t spli
     const uint32_t whole = min(end, rows.vocab / N);
     Running r;
     uint32_t u = begin + threadIdx.x;
-    constexpr int kBatch = W == 1024 ? 8 : 4;  // units in flight: a row of few is bound by the wait for them
+    constexpr int kBatch = W == 1024 ? 8 : 4;  // units in flight: few rows have few waves to wait beside them
     for (; u + (kBatch - 1) * W < whole; u += kBatch * W) {
         Raw<T, N> raw[kBatch];
 #pragma unroll
@@ -401,9 +402,15 @@ constexpr int64_t kOneMost = 16384;  // tokens of both sides that one workgroup 
 
 // How the forward takes its rows.  Many rows fill the chip with workgroups of 256
 // threads each.  A few take 1024 threads each, and very long ones of them several
-// workgroups, whose sums a second launch joins: 4 x 131072 bf16 9.2 us so, against
-// 3.2 and 2.8 in 64 workgroups and a join -- but a call of two launches costs its
-// caller 16.4 us, of one 11.4.
+// workgroups, whose sums a second launch joins.  A call of two launches costs its caller
+// 15.5 us at least, one of one launch 11.3; in a captured graph the second costs less.  4 rows,
+// us a call, and in a graph:
+//   bf16: 131072 entries whole 11.3, 9.7; 200064 whole 13.0, 13.4, in pieces of 128 KB 15.5, 8.7;
+//   256000 whole 17.3, 17.7, pieces of 128 KB 15.4, 10.2; 393213 whole 28.3, 28.8, pieces of
+//   256 KB 19.7, 19.9, of 128 KB 15.7, 11.0;
+//   fp32: 131072 whole 11.4, 9.8, pieces of 256 KB 15.7, 8.8; 262141 whole 17.2, 17.5, 16.3, 11.0.
+// Smaller pieces lose where rows times pieces come to fill the chip: 64 x 1000000 bf16 31.5 in
+// pieces of 256 KB, 35.5 of 128 KB; 200 x 256000 25.9 whole, 32.4 of 128 KB.
 struct FwdPlan {
     int threads;
     uint32_t splits;
