@@ -233,7 +233,9 @@ lors_status_t lors_logprob_backward(const lors_logits_t* p, const float* dlogp, 
  *   dseq[b]   = d loss / d(sum of logp of sequence b)
  * e: label smoothing, 0 <= e <= 0.5; beta finite; pairs >= 1, length >= 0, 2 pairs . length
  * < 2^31; otherwise LORS_ERR_SHAPE.  reward and dseq: 2 pairs fp32; loss: one fp32.
- * ref NULL: a reference of 0 everywhere.  Sums over tokens and pairs are in 64 bits.
+ * ref NULL: a reference of 0 everywhere.  Sums over tokens and pairs and the margins are in
+ * 64 bits; of many pairs (above 512, or 16384 tokens) each one's loss is rounded to fp32
+ * before their mean.
  */
 typedef struct lors_preference_desc {
     int64_t pairs;

@@ -6,10 +6,10 @@
 // sums alike, and each sum runs over the tokens in their order, so that the
 // result does not depend on which workgroup is faster.
 //
-// The lookup is bound by memory: 8192 x 4096 bf16 22 us (134 MB, 6 TB/s).  So is the
-// writing of the gradient: 32768 x 4096 from 8192 tokens 70 us (335 MB, 4.8 TB/s),
-// 131072 x 4096 from 16384 tokens 230 us (1.2 GB, 5.2 TB/s).  The sort before it is a
-// chain of waits: 17 us for 8192 tokens, 19 for 16384, 7 for 1501.
+// The lookup is bound by memory: 8192 x 4096 bf16 22 us (107 MB with the rows that tokens
+// share read once or twice, 4.9 TB/s).  So is the writing of the gradient: 32768 x 4096 from
+// 8192 tokens 71 us (322 MB, 4.5 TB/s), 131072 x 4096 from 16384 tokens 228 us (1.17 GB, 5.1
+// TB/s).  The sort before it is a chain of waits: 19 us for 8192 or 16384 tokens, 7 for 1501.
 #include <algorithm>
 #include <utility>
 
@@ -341,7 +341,8 @@ constexpr uint32_t kChunk = 32;
 // call to call (lookup and gradient, us): 8 x 8 122 at 8192 tokens into 32768 x 4096, 304
 // at 16384 into 131072 x 4096, 54 at 1501 into 50021 x 771 fp32; 4 rows 129, 308, 50; 16
 // rows 124, 314, 57; 16 in flight 120, 307, 51, but 59 against 52 with 32768 tokens of
-// 32768 ids.
+// 32768 ids.  (Units counted from the row's start; from the cache line's, below, 8 x 8 takes
+// 47 in the last case.)
 constexpr uint32_t kRows = 8;
 constexpr int kBatch = 8;
 

@@ -122,7 +122,7 @@ struct Rows {
 // An element takes a conversion, half a maximum, a difference, a product and an fma, an
 // exponential (a quarter of the rate) and a sum, 9.5 of the chip's instructions: by that count
 // three quarters of the time that the two bytes of a bf16 take.  A whole row of one
-// compute unit is bound by them: 131072 entries are 8 us of the kernel's 9.2.
+// compute unit is bound by them: 131072 entries are 8 us of the kernel's 9.7.
 // A row's `splits` workgroups of W threads take a run of it each; with splits > 1 their (top, sum) go to
 // `part` and logprob_join_kernel finishes.
 template <typename T, bool I64, int W>
