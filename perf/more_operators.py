@@ -344,8 +344,10 @@ def _own(st):
     if case["op"] == "ortho":
         if case["run"] == "direction":
             return {"direction": torch.cat([d.reshape(-1) for d in train.orthogonalize(st["grads"], coefficients=COEFFICIENTS, eps=EPS)])}
-        train.orthogonal_update(st["masters"], st["grads"], st["momenta"], LR, params=st["params"], momentum=BETA, nesterov=True,
-                                weight_decay=DECAY, coefficients=COEFFICIENTS, eps=EPS)
+        if "optimizer" not in st:  # a program makes it once and keeps it
+            st["optimizer"] = train.OrthogonalUpdate(st["masters"], st["params"], st["momenta"], momentum=BETA, nesterov=True,
+                                                     weight_decay=DECAY, coefficients=COEFFICIENTS, eps=EPS)
+        st["optimizer"].step(st["grads"], LR)
         return {"momentum": st["momentum"], "master": st["master"], "param": st["param"]}
     token, logp = train.sample(st["logits"], st["u"], st["temperature"], st["top_k"], st["top_p"], st["min_p"])
     return {"token": token, "logp": logp}
