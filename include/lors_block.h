@@ -1,0 +1,94 @@
+/*
+ * lors_block.h -- C ABI of three operators that a fine-tuning loop of gated
+ * models needs beside the layer (lors.h) and the operators around it
+ * (lors_train.h), for AMD MI355X (gfx950):
+ *
+ *   gated    H = act(G) . U, the gated half of a feed-forward block, out of two
+ *            sparsity-preserved LoRA projections, and its gradients
+ *   update   orthogonalised (Newton-Schulz) update directions of matrices with a
+ *            short side, such as adapters, and the optimiser's step with them
+ *   sample   tokens drawn from logits: temperature, top-k, top-p, min-p
+ *
+ * Conventions are those of lors.h: the same status codes, arguments validated on
+ * the host in the order
+ *   null -> dtype/format -> shape/range -> alignment -> alias -> workspace
+ * before any HIP call, caller-owned buffers, no allocation of device memory, asynchronous work on
+ * `stream`.  Outputs must not overlap any input, each other or the workspace
+ * (LORS_ERR_ALIAS).  Arrays of no elements may be NULL.
+ */
+#ifndef LORS_BLOCK_H
+#define LORS_BLOCK_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "lors.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Version of this interface: major * 10000 + minor * 100 + patch. */
+int lors_block_version(void);
+
+/* -------------------------------------------------------------------- gated */
+
+typedef enum lors_activation {
+    LORS_ACT_SILU = 0, /* g / (1 + exp(-g)) */
+    LORS_ACT_GELU = 1  /* g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2 */
+} lors_activation_t;
+
+/* One of the block's two projections, as lors_forward takes them. */
+typedef struct lors_projection {
+    const void* W;            /* R x C */
+    const uint32_t* M_packed; /* the problem's mask format */
+    const void* B;            /* R x r */
+    const void* A;            /* r x C */
+} lors_projection_t;
+
+/*
+ * The problem p describes both projections: they share R, C, r, scale, dtype and
+ * mask format.  Limits and errors are those of lors_problem_t; the tiles of both
+ * together must number below 2^31 (LORS_ERR_UNSUPPORTED).  Pointers are 16-byte
+ * aligned.  An unknown activation is refused in LORS_ERR_MASK_FORMAT's place of
+ * the order, with LORS_ERR_UNSUPPORTED.
+ *
+ * Scratch bytes of lors_gated_forward (without G and U) and, with backward != 0,
+ * of lors_gated_backward: the two transposed masks, padded copies of B where r is
+ * no multiple of 8, and dG and dU (L x R each).  (size_t)-1 if p is invalid for
+ * the call.
+ */
+size_t lors_gated_workspace_bytes(const lors_problem_t* p, int backward);
+
+/*
+ * G = X . Wg'^T, U = X . Wu'^T, H = act(G) . U (L x R), with W' = select(M, W + s.B.A, 0)
+ * rounded to the dtype, as in lors_forward.  G and U: where the projections'
+ * results are kept for the backward, both or neither (LORS_ERR_NULL); NULL for
+ * serving.  G and U are rounded once.  H is computed from their fp32 sums in
+ * bf16 (in batches of tiles act(G) is rounded to bf16 before the product), and
+ * from the stored G and U in fp32.  p->flags: 0, otherwise LORS_ERR_UNSUPPORTED.
+ */
+lors_status_t lors_gated_forward(const lors_problem_t* p, int32_t activation, const void* X,
+                                 const lors_projection_t* gate, const lors_projection_t* up, void* G, void* U, void* H,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward from dH (L x R) and the G and U that the forward kept:
+ *   dG = dH . U . act'(G), dU = dH . act(G)   (rounded to the dtype, in the workspace)
+ *   dX = dG . Wg' + dU . Wu'                  (skipped if dX is NULL; rounded once)
+ *   dB, dA of each projection as lors_backward's, from dG and dU: fp32,
+ *   overwritten, their sums' order not fixed.
+ * p->flags: 0 or LORS_FLAG_REUSE_MASK_T (the workspace still holds the transposed
+ * masks of an earlier call with the same R, C, r, L and masks), otherwise
+ * LORS_ERR_UNSUPPORTED.
+ */
+lors_status_t lors_gated_backward(const lors_problem_t* p, int32_t activation, const void* dH, const void* X,
+                                  const lors_projection_t* gate, const lors_projection_t* up, const void* G,
+                                  const void* U, void* dX, float* dB_gate, float* dA_gate, float* dB_up, float* dA_up,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* LORS_BLOCK_H */

@@ -1,8 +1,8 @@
 """ctypes binding of ``liblors.so`` (argument marshalling only).
 
-Every function here forwards to the C ABI declared in ``include/lors.h`` and
-``include/lors_train.h`` (the operators around the layer) and turns a non-zero
-status into :class:`LorsError`.  There is no fallback: if the
+Every function here forwards to the C ABI declared in ``include/lors.h``,
+``include/lors_train.h`` (the operators around the layer) and ``include/lors_block.h``
+(gated block, adapter updates, sampling) and turns a non-zero status into :class:`LorsError`.  There is no fallback: if the
 library is missing the first call raises.
 """
 from __future__ import annotations
@@ -55,6 +55,14 @@ EXPORTED_TRAIN = (
     "lors_train_version", "lors_dropout", "lors_norm_forward", "lors_norm_workspace_bytes", "lors_norm_backward",
     "lors_embedding_forward", "lors_embedding_workspace_bytes", "lors_embedding_backward",
     "lors_logprob_workspace_bytes", "lors_logprob_forward", "lors_logprob_backward", "lors_preference",
+)
+
+# include/lors_block.h
+ACT_SILU = 0
+ACT_GELU = 1
+
+EXPORTED_BLOCK = (
+    "lors_block_version", "lors_gated_workspace_bytes", "lors_gated_forward", "lors_gated_backward",
 )
 
 
@@ -142,6 +150,15 @@ class Preference(ctypes.Structure):
     ]
 
 
+class Projection(ctypes.Structure):
+    _fields_ = [
+        ("W", ctypes.c_void_p),
+        ("M_packed", ctypes.c_void_p),
+        ("B", ctypes.c_void_p),
+        ("A", ctypes.c_void_p),
+    ]
+
+
 class LorsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -159,6 +176,7 @@ _sz = ctypes.c_size_t
 
 def _declare(lib) -> None:
     P = ctypes.POINTER(Problem)
+    PJ = ctypes.POINTER(Projection)
     sig = {
         "lors_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "lors_version": (ctypes.c_int, []),
@@ -189,6 +207,10 @@ def _declare(lib) -> None:
         "lors_logprob_forward": (ctypes.c_int, [ctypes.POINTER(Logits)] + [_vp] * 5 + [_sz, _vp]),
         "lors_logprob_backward": (ctypes.c_int, [ctypes.POINTER(Logits), _vp, _i64] + [_vp] * 6),
         "lors_preference": (ctypes.c_int, [ctypes.POINTER(Preference)] + [_vp] * 7),
+        "lors_block_version": (ctypes.c_int, []),
+        "lors_gated_workspace_bytes": (_sz, [P, ctypes.c_int]),
+        "lors_gated_forward": (ctypes.c_int, [P, _i32, _vp, PJ, PJ, _vp, _vp, _vp, _vp, _sz, _vp]),
+        "lors_gated_backward": (ctypes.c_int, [P, _i32, _vp, _vp, PJ, PJ] + [_vp] * 8 + [_sz, _vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -324,3 +346,18 @@ def logprob_backward(p: Logits, dlogp, span, upstream, logits, targets, lse, dlo
 
 def preference(p: Preference, logp, ref, targets, loss, reward, dseq, stream) -> int:
     return lib().lors_preference(ctypes.byref(p), logp, ref, targets, loss, reward, dseq, stream)
+
+
+def gated_workspace_bytes(p: Problem, backward: bool) -> int:
+    return lib().lors_gated_workspace_bytes(ctypes.byref(p), int(backward))
+
+
+def gated_forward(p: Problem, activation, X, gate: Projection, up: Projection, G, U, H, ws, ws_bytes, stream) -> int:
+    return lib().lors_gated_forward(ctypes.byref(p), activation, X, ctypes.byref(gate), ctypes.byref(up), G, U, H, ws,
+                                    ws_bytes, stream)
+
+
+def gated_backward(p: Problem, activation, dH, X, gate: Projection, up: Projection, G, U, dX, dB_gate, dA_gate, dB_up,
+                   dA_up, ws, ws_bytes, stream) -> int:
+    return lib().lors_gated_backward(ctypes.byref(p), activation, dH, X, ctypes.byref(gate), ctypes.byref(up), G, U, dX,
+                                     dB_gate, dA_gate, dB_up, dA_up, ws, ws_bytes, stream)

@@ -11,6 +11,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "abi_common.hpp"
 #include "lors.h"
 #include "kernels.hpp"
 
@@ -56,9 +57,13 @@ int64_t elt_size(int32_t dtype) { return dtype == LORS_DTYPE_BF16 ? 2 : 4; }
 bool valid_dtype(int32_t d) { return d == LORS_DTYPE_BF16 || d == LORS_DTYPE_F32; }
 bool valid_format(int32_t f) { return f == LORS_MASK_BITMAP || f == LORS_MASK_2_4; }
 
+lors_status_t from_hip(hipError_t e) { return e == hipSuccess ? LORS_OK : LORS_ERR_HIP; }
+
+}  // namespace
+
 // Problem-level checks shared by forward/backward/workspace query, in the
 // documented order (dtype/format, then shape/range).
-lors_status_t check_problem(const lors_problem_t* p) {
+lors_status_t lors::check_problem(const lors_problem_t* p) {
     if (!valid_dtype(p->dtype)) return LORS_ERR_DTYPE;
     if (!valid_format(p->mask_format)) return LORS_ERR_MASK_FORMAT;
     if (p->R < 1 || p->C < 1 || p->L < 0 || p->r < 1 || p->r > kMaxRank) return LORS_ERR_SHAPE;
@@ -92,10 +97,7 @@ lors_status_t check_problem(const lors_problem_t* p) {
     if (t256 > kMaxExtent || t256x > kMaxExtent || t256g > kMaxExtent) return LORS_ERR_UNSUPPORTED;
     return LORS_OK;
 }
-
-lors_status_t from_hip(hipError_t e) { return e == hipSuccess ? LORS_OK : LORS_ERR_HIP; }
-
-}  // namespace
+using lors::check_problem;
 
 extern "C" {
 

@@ -1,0 +1,209 @@
+// C ABI of the gated block, orthogonalised updates and sampling: argument validation
+// and dispatch to the gfx950 kernels.
+//
+// Validation runs entirely on the host, in the order null, dtype/format,
+// shape/range, alignment, alias, workspace, before any HIP call, so every rejected
+// call is free of side effects.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "abi_common.hpp"
+#include "kernels.hpp"
+#include "lors_block.h"
+
+namespace {
+
+using namespace lors::abi;
+
+int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
+
+// ---------------------------------------------------------------------------
+// gated
+// ---------------------------------------------------------------------------
+lors_status_t check_gated(const lors_problem_t* p, int32_t activation, uint32_t flags) {
+    lors_status_t st = lors::check_problem(p);
+    if (st == LORS_ERR_DTYPE || st == LORS_ERR_MASK_FORMAT) return st;
+    if (activation != LORS_ACT_SILU && activation != LORS_ACT_GELU) return LORS_ERR_UNSUPPORTED;
+    if (st != LORS_OK) return st;
+    if ((p->flags & ~flags) != 0u) return LORS_ERR_UNSUPPORTED;
+    // both projections' G tiles in one grid
+    if (2 * ((p->R + 255) / 256) * ((p->C + 255) / 256) > kMaxExtent) return LORS_ERR_UNSUPPORTED;
+    return LORS_OK;
+}
+
+// The backward's scratch: both transposed masks, both padded B's, dG, dU.
+struct GatedScratch {
+    int64_t mt, pad, grad, total;
+    explicit GatedScratch(const lors_problem_t* p) {
+        const bool bf16 = p->dtype == LORS_DTYPE_BF16;
+        const int64_t rp = (p->r + 7) / 8 * 8;
+        mt = bf16 ? round256(p->C * ((p->R + 31) / 32) * 4) : 0;
+        pad = bf16 && rp != p->r ? round256(2 * p->R * rp) : 0;
+        grad = round256(p->L * p->R * elt_size(p->dtype));
+        total = 2 * (mt + pad + grad);
+    }
+};
+
+int64_t gated_forward_bytes(const lors_problem_t* p) {
+    return p->dtype == LORS_DTYPE_BF16 ? 0 : 2 * round256(p->L * p->R * 4);
+}
+
+bool complete(const lors_projection_t* q) {
+    return q != nullptr && q->W != nullptr && q->M_packed != nullptr && q->B != nullptr && q->A != nullptr;
+}
+
+lors::LayerArgs gated_args(const lors_problem_t* p, int32_t activation, const void* X, const lors_projection_t* gate,
+                           const lors_projection_t* up, lors::SecondArgs& second) {
+    lors::LayerArgs a{};
+    a.R = p->R;
+    a.C = p->C;
+    a.L = p->L;
+    a.r = p->r;
+    a.r_grad = p->r;
+    a.scale = p->scale;
+    a.two_four = p->mask_format == LORS_MASK_2_4;
+    a.X = X;
+    a.W = gate->W;
+    a.M = gate->M_packed;
+    a.B = gate->B;
+    a.A = gate->A;
+    second = lors::SecondArgs{};
+    second.W = up->W;
+    second.M = up->M_packed;
+    second.B = up->B;
+    second.A = up->A;
+    second.gelu = activation == LORS_ACT_GELU;
+    a.second = &second;
+    return a;
+}
+
+// The launchers of one projection, on the second one of a.
+lors::LayerArgs second_alone(const lors::LayerArgs& a) {
+    lors::LayerArgs b = a;
+    const lors::SecondArgs& q = *a.second;
+    b.W = q.W;
+    b.M = q.M;
+    b.Mt = q.Mt;
+    b.B = q.B;
+    b.A = q.A;
+    b.dY = q.dY;
+    b.dB = q.dB;
+    b.dA = q.dA;
+    b.second = nullptr;
+    return b;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lors_block_version(void) { return 10000; }
+
+size_t lors_gated_workspace_bytes(const lors_problem_t* p, int backward) {
+    if (p == nullptr || check_gated(p, LORS_ACT_SILU, backward ? LORS_FLAG_REUSE_MASK_T : 0u) != LORS_OK)
+        return static_cast<size_t>(-1);
+    return static_cast<size_t>(backward ? GatedScratch(p).total : gated_forward_bytes(p));
+}
+
+lors_status_t lors_gated_forward(const lors_problem_t* p, int32_t activation, const void* X,
+                                 const lors_projection_t* gate, const lors_projection_t* up, void* G, void* U, void* H,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+    if (p == nullptr || !complete(gate) || !complete(up)) return LORS_ERR_NULL;
+    if (p->L != 0 && (X == nullptr || H == nullptr || (G == nullptr) != (U == nullptr))) return LORS_ERR_NULL;
+    lors_status_t st = check_gated(p, activation, 0u);
+    if (st != LORS_OK) return st;
+    const int64_t es = elt_size(p->dtype), R = p->R, C = p->C, L = p->L, r = p->r;
+    const int64_t m = static_cast<int64_t>(lors_mask_packed_bytes(R, C)), y = L * R * es;
+    const bool bf16 = p->dtype == LORS_DTYPE_BF16, save = G != nullptr;
+    const int64_t need = save ? 0 : gated_forward_bytes(p);
+    st = check_arrays({{X, L * C * es, 16}, {gate->W, R * C * es, 16}, {gate->M_packed, m, 16}, {gate->B, R * r * es, 16},
+                       {gate->A, r * C * es, 16}, {up->W, R * C * es, 16}, {up->M_packed, m, 16}, {up->B, R * r * es, 16},
+                       {up->A, r * C * es, 16}},
+                      {{H, y, 16}, {G, y, 16}, {U, y, 16}, {need ? workspace : nullptr, need, 16}});
+    if (st == LORS_OK) st = check_workspace(workspace, workspace_bytes, static_cast<size_t>(need));
+    if (st != LORS_OK || L == 0) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    lors::SecondArgs second;
+    lors::LayerArgs a = gated_args(p, activation, X, gate, up, second);
+    if (bf16) {
+        a.Y = H;
+        second.G = G;
+        second.U = U;
+        return from_hip(lors::launch_gated_fwd_bf16(a, s));
+    }
+    a.Y = save ? G : workspace;
+    lors::LayerArgs b = second_alone(a);
+    b.Y = save ? U : static_cast<uint8_t*>(workspace) + need / 2;
+    hipError_t e = lors::launch_fwd_f32(a, s);
+    if (e == hipSuccess) e = lors::launch_fwd_f32(b, s);
+    if (e == hipSuccess) e = lors::launch_gated_join(a.Y, b.Y, H, L * R, second.gelu, false, s);
+    return from_hip(e);
+}
+
+lors_status_t lors_gated_backward(const lors_problem_t* p, int32_t activation, const void* dH, const void* X,
+                                  const lors_projection_t* gate, const lors_projection_t* up, const void* G,
+                                  const void* U, void* dX, float* dB_gate, float* dA_gate, float* dB_up, float* dA_up,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+    if (p == nullptr || !complete(gate) || !complete(up)) return LORS_ERR_NULL;
+    if (dB_gate == nullptr || dA_gate == nullptr || dB_up == nullptr || dA_up == nullptr) return LORS_ERR_NULL;
+    if (p->L != 0 && (dH == nullptr || X == nullptr || G == nullptr || U == nullptr)) return LORS_ERR_NULL;
+    lors_status_t st = check_gated(p, activation, LORS_FLAG_REUSE_MASK_T);
+    if (st != LORS_OK) return st;
+    const int64_t es = elt_size(p->dtype), R = p->R, C = p->C, L = p->L, r = p->r;
+    const int64_t m = static_cast<int64_t>(lors_mask_packed_bytes(R, C)), y = L * R * es;
+    const GatedScratch ws(p);
+    st = check_arrays({{dH, y, 16}, {G, y, 16}, {U, y, 16}, {X, L * C * es, 16}, {gate->W, R * C * es, 16},
+                       {gate->M_packed, m, 16}, {gate->B, R * r * es, 16}, {gate->A, r * C * es, 16}, {up->W, R * C * es, 16},
+                       {up->M_packed, m, 16}, {up->B, R * r * es, 16}, {up->A, r * C * es, 16}},
+                      {{dX, L * C * es, 16}, {dB_gate, R * r * 4, 16}, {dA_gate, r * C * 4, 16}, {dB_up, R * r * 4, 16},
+                       {dA_up, r * C * 4, 16}, {workspace, ws.total, 16}});
+    if (st == LORS_OK) st = check_workspace(workspace, workspace_bytes, static_cast<size_t>(ws.total));
+    if (st != LORS_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool bf16 = p->dtype == LORS_DTYPE_BF16;
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    lors::SecondArgs second;
+    lors::LayerArgs a = gated_args(p, activation, X, gate, up, second);
+    a.dX = dX;
+    a.dB = dB_gate;
+    a.dA = dA_gate;
+    second.dB = dB_up;
+    second.dA = dA_up;
+    a.Mt = reinterpret_cast<const uint32_t*>(at);
+    second.Mt = reinterpret_cast<const uint32_t*>(at + ws.mt);
+    a.b_pad = ws.pad ? at + 2 * ws.mt : nullptr;
+    second.b_pad = ws.pad ? at + 2 * ws.mt + ws.pad : nullptr;
+    void* dG = at + 2 * (ws.mt + ws.pad);
+    void* dU = static_cast<uint8_t*>(dG) + ws.grad;
+    a.dY = dG;
+    second.dY = dU;
+    hipError_t e = hipSuccess;
+    // the bf16 dX launch clears dB and dA of both projections for the atomics of the
+    // adapters' gradients
+    a.clear_grads = bf16 && dX != nullptr && L != 0;
+    if (!a.clear_grads) {
+        e = lors::launch_zero2_f32(dB_gate, R * r, dA_gate, r * C, s);
+        if (e == hipSuccess) e = lors::launch_zero2_f32(dB_up, R * r, dA_up, r * C, s);
+    }
+    if (e != hipSuccess || L == 0) return from_hip(e);
+    e = lors::launch_gated_split(dH, G, U, dG, dU, L * R, second.gelu, bf16, s);
+    if (bf16) {
+        if ((p->flags & LORS_FLAG_REUSE_MASK_T) == 0u) {
+            if (e == hipSuccess) e = lors::launch_mask_transpose(a.M, R, C, a.two_four, const_cast<uint32_t*>(a.Mt), s);
+            if (e == hipSuccess)
+                e = lors::launch_mask_transpose(second.M, R, C, a.two_four, const_cast<uint32_t*>(second.Mt), s);
+        }
+        if (e == hipSuccess) e = lors::launch_gated_dx_bf16(a, s);
+        if (e == hipSuccess) e = lors::launch_gated_g_bf16(a, s);
+        return from_hip(e);
+    }
+    const lors::LayerArgs b = second_alone(a);
+    if (e == hipSuccess && dX != nullptr) e = lors::launch_gated_dx_f32(a, s);
+    if (e == hipSuccess) e = lors::launch_g_f32(a, s);
+    if (e == hipSuccess) e = lors::launch_g_f32(b, s);
+    return from_hip(e);
+}
+
+}  // extern "C"

@@ -29,9 +29,25 @@
 // zero-filled copy of B); ranks above 64 as half-feature tiles only.
 #include "gemm_common.hpp"
 #include "kernels.hpp"
+#include "gated.hpp"
 
 #include <cmath>
 #include <type_traits>
+
+// The units that instantiate the gated block's kernels define LORS_GATED.
+#ifdef LORS_GATED
+#define LORS_FIRST(name) name##_gate
+#define LORS_MORE , GatedGrad pair
+#define LORS_PAIR , grad_pair_of(a)
+#define LORS_DX launch_gated_dx_bf16
+#define LORS_DX_THIN launch_gated_dx_thin_bf16
+#else
+#define LORS_FIRST(name) name
+#define LORS_MORE
+#define LORS_PAIR
+#define LORS_DX launch_dx_bf16
+#define LORS_DX_THIN launch_dx_thin_bf16
+#endif
 
 namespace lors {
 namespace {
@@ -101,13 +117,16 @@ struct Layout {
 // are zero); ra: the rows of A that exist (A rows ra .. r-1 are read as zero).
 // TM, NF < (BM, 2): a thin tile of TM tokens and 128 NF input features, as in
 // the forward kernel.
+// LORS_GATED: the two projections of a gated block (GatedGrad, gated.hpp): the
+// accumulators take the second's products after the first's, so that dX is their
+// unrounded sum.  The pipeline drains and fills once between them.
 template <int RK, bool KRAG, bool FOLD, int TM, int NF>
 __global__ __launch_bounds__(NT, 1) void dx_kernel(
-    const uint16_t* __restrict__ dY, const uint16_t* __restrict__ W,
-    const uint32_t* __restrict__ Mt, const uint16_t* __restrict__ Bm,
-    const uint16_t* __restrict__ Am, uint16_t* __restrict__ dX, int64_t L, int R, int C, int r,
+    const uint16_t* __restrict__ LORS_FIRST(dY), const uint16_t* __restrict__ LORS_FIRST(W),
+    const uint32_t* __restrict__ LORS_FIRST(Mt), const uint16_t* __restrict__ LORS_FIRST(Bm),
+    const uint16_t* __restrict__ LORS_FIRST(Am), uint16_t* __restrict__ dX, int64_t L, int R, int C, int r,
     int ra, float s, int tiles_m, int tiles_n, float* __restrict__ z0, int64_t nz0,
-    float* __restrict__ z1, int64_t nz1, int n_full, int split, float* __restrict__ part) {
+    float* __restrict__ z1, int64_t nz1, int n_full, int split, float* __restrict__ part LORS_MORE) {
     using Lay = Layout<RK, TM, NF>;
     constexpr int MBW = TM / 32;  // 32-token blocks per wave
     constexpr int SPAN = thin_span(TM);  // tokens of a logical tile
@@ -134,6 +153,10 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
         for (int64_t t = (int64_t)blockIdx.x * NT + tid; t < nz0 + nz1; t += stride) {
             if (t < nz0) z0[t] = 0.f;
             else z1[t - nz0] = 0.f;
+#ifdef LORS_GATED
+            if (t < nz0) pair.dB[t] = 0.f;
+            else pair.dA[t - nz0] = 0.f;
+#endif
         }
     }
 
@@ -185,6 +208,29 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
     // M^T is a plain bitmap whatever the caller's layout.
     if (tid < 16) *(u32x2*)(smem + Lay::LUT + 8 * tid) = select_lut16_entry<false>((uint32_t)tid);
 
+#ifdef LORS_GATED
+    f32x16 acc[MBW][NF];
+#pragma unroll
+    for (int i = 0; i < MBW; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    const int ncol0 = 32 * NF * wave + l32;
+    // the projections of a gated block: the gate's contraction, then the up
+    // projection's
+#pragma unroll 1
+    for (int seg = 0; seg < 2; ++seg) {
+    const uint16_t* dY = seg == 0 ? dY_gate : pair.dY;
+    const uint16_t* W = seg == 0 ? W_gate : pair.W;
+    const uint32_t* Mt = seg == 0 ? Mt_gate : pair.Mt;
+    const uint16_t* Bm = seg == 0 ? Bm_gate : pair.B;
+    const uint16_t* Am = seg == 0 ? Am_gate : pair.A;
+    if (seg == 1) {
+        wait_vmcnt<0>();  // the last copies of the first loop
+        lds_barrier();    // every wave is done with its stages
+    }
+#endif
     // ---- slab copies.  Copies 0..ND-1: dY slab rows 8*(ND*wave + q) + lane/8
     // (64 k per row); copies ND..ND+NWC-1: this wave's W block, its 32 NF
     // columns (NF = 2: rows 8q + lane/8 in the tr64 layout; NF = 1: rows
@@ -268,7 +314,9 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
     // Rows of the merge A operand: lane (rho = l32, h) reads B row pi(rho).
     const int rho = l32;
     const int pik = 16 * (rho >> 4) + 8 * ((rho >> 2) & 1) + 4 * ((rho >> 3) & 1) + (rho & 3);
+#ifndef LORS_GATED
     const int ncol0 = 32 * NF * wave + l32;
+#endif
     // transpose-read offsets of the raw W fragments in this wave's W block,
     // sub-step 0 (sub-step c4 is 16 rows further): group g of 16 lanes reads
     // rows 8(g/2) + 4t + 0..3, columns 32nb + 16(g%2) + 0..15
@@ -285,6 +333,7 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
     }
     auto doff = [&](int mb, int c4) { return Lay::D + slab64_off(32 * mb + l32, 2 * c4 + h); };
 
+#ifndef LORS_GATED
     f32x16 acc[MBW][NF];
 #pragma unroll
     for (int i = 0; i < MBW; ++i)
@@ -292,6 +341,7 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
         for (int j = 0; j < NF; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+#endif
 
     bf16x8 da[MBW], db[MBW];  // dY fragments of alternate sub-steps
     u32x4 wa[NF], wb[NF];     // W' fragments of alternate sub-steps
@@ -563,10 +613,14 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
         SLOT_END();
         st = sx;
     }
+#ifdef LORS_GATED
+    }
+#endif
     // ---- epilogue: round to bf16, stage the wave's TM x 32 NF block in LDS
     // (rows of 32 NF outputs), then 16-byte stores of whole rows.
     wait_vmcnt<0>();
     lds_barrier();  // every wave's copies landed and every read of the stages done
+#ifndef LORS_GATED
     if (TM == BM && NF == 2 && (int)blockIdx.x >= n_full) {
         // a piece of a split tile: its unrounded fp32 partial sums go to slice
         // blockIdx.x - n_full of `part` (256 tokens x 256 features); the
@@ -581,6 +635,7 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
                     dst[(32 * mb + 8 * (v >> 2) + 4 * h + (v & 3)) * BN + ncol0 + 32 * nb] = acc[mb][nb][v];
         return;
     }
+#endif
     constexpr int OW = 32 * NF;   // outputs per staged row
     constexpr int CH = OW / 8;    // 16-byte chunks per row
     uint16_t* ol = (uint16_t*)(smem + wave * (TM * OW * 2));
@@ -619,7 +674,7 @@ void launch_tm(const LayerArgs& a, hipStream_t st, int ra, int grid, int tiles_m
     hipLaunchKernelGGL((dx_kernel<RK, KRAG, FOLD, TM, NF>), dim3(grid), dim3(NT), 0, st, (const uint16_t*)a.dY,
                        (const uint16_t*)a.W, a.Mt, (const uint16_t*)a.B, (const uint16_t*)a.A, (uint16_t*)a.dX, a.L,
                        (int)a.R, (int)a.C, (int)a.r, ra, a.scale, tiles_m, tiles_n, z0, nz0, z1, nz1, n_full,
-                       split, part);
+                       split, part LORS_PAIR);
 }
 
 #ifndef LORS_THIN_TILES
@@ -666,7 +721,7 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st, int ra) {
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && tp.tm > 0)
-        e = launch_dx_thin_bf16(a, st, ra, tp.n_full, tp.tail, tp.tm, a.clear_grads && !clear_here);
+        e = LORS_DX_THIN(a, st, ra, tp.n_full, tp.tail, tp.tm, a.clear_grads && !clear_here);
     if (e == hipSuccess && sp.split > 1)
         e = launch_split_reduce_bf16(part, sp.n_full, sp.split, tiles_m, tiles_n, GROUP_M, a.L, (int)a.C, nullptr,
                                      a.dX, st);
@@ -714,7 +769,7 @@ hipError_t launch_thin_rk(const LayerArgs& a, hipStream_t st, int ra, int first,
 
 #ifdef LORS_THIN_TILES
 
-hipError_t launch_dx_thin_bf16(const LayerArgs& a, hipStream_t st, int ra, int first, int tail, int tm, bool clear) {
+hipError_t LORS_DX_THIN(const LayerArgs& a, hipStream_t st, int ra, int first, int tail, int tm, bool clear) {
     if (tail <= 0) return hipSuccess;
     // a.r: a multiple of 8 (see launch_dx_bf16)
     if (a.r < 8 || a.r % 8 != 0) return hipErrorInvalidValue;
@@ -733,13 +788,16 @@ hipError_t launch_dx_thin_bf16(const LayerArgs& a, hipStream_t st, int ra, int f
 
 #else
 
-hipError_t launch_dx_bf16(const LayerArgs& a, hipStream_t st) {
+hipError_t LORS_DX(const LayerArgs& a, hipStream_t st) {
     if (a.L == 0 || a.dX == nullptr) return hipSuccess;
     if (a.Mt == nullptr || a.r < 1 || a.r > 128) return hipErrorInvalidValue;
     // The B slab is copied in whole 16-byte chunks of its rows.  A rank that
     // is not a multiple of 8 works on a copy of B whose rows are padded with
     // zero columns to rp = roundup8(r); the missing A rows are read as zero.
     LayerArgs ap = a;
+#ifdef LORS_GATED
+    SecondArgs padded;
+#endif
     const int ra = (int)a.r;
     const int rp = (ra + 7) / 8 * 8;
     if (rp != ra) {
@@ -748,6 +806,13 @@ hipError_t launch_dx_bf16(const LayerArgs& a, hipStream_t st) {
         if (e != hipSuccess) return e;
         ap.B = a.b_pad;
         ap.r = rp;
+#ifdef LORS_GATED
+        const hipError_t e2 = launch_pad_cols_bf16(a.second->B, a.R, a.r, rp, a.second->b_pad, st);
+        if (e2 != hipSuccess) return e2;
+        padded = *a.second;
+        padded.B = padded.b_pad;
+        ap.second = &padded;
+#endif
     }
     switch ((rp + 15) / 16) {
         case 1: return launch_rk<1>(ap, st, ra);
@@ -761,7 +826,7 @@ hipError_t launch_dx_bf16(const LayerArgs& a, hipStream_t st) {
     const int n = thin_only_plan(a.L, a.C, run);
     hipError_t e = hipSuccess;
     for (int i = 0; i < n && e == hipSuccess; ++i)
-        e = launch_dx_thin_bf16(ap, st, ra, run[i].n_full, run[i].tail, run[i].tm, a.clear_grads && i == 0);
+        e = LORS_DX_THIN(ap, st, ra, run[i].n_full, run[i].tail, run[i].tm, a.clear_grads && i == 0);
     return e;
 }
 

@@ -123,8 +123,9 @@ __global__ __launch_bounds__(NT) void fwd_f32(const float* __restrict__ X, const
     }
 }
 
-// dX[L x C] = dY . W', K = R.
-template <int RP>
+// dX[L x C] = dY . W', K = R.  ADD: added to what dX holds (a gated block's second
+// projection).
+template <int RP, bool ADD>
 __global__ __launch_bounds__(NT) void dx_f32(const float* __restrict__ dY, const float* __restrict__ W,
                                              const uint32_t* __restrict__ Mp, const float* __restrict__ Bm,
                                              const float* __restrict__ Am, float* __restrict__ dX, int64_t L, int R,
@@ -181,7 +182,11 @@ __global__ __launch_bounds__(NT) void dx_f32(const float* __restrict__ dY, const
     __syncthreads();
     if (tid < T * T / 4) {
         const int row = tid >> 3, gn = n0 + 4 * (tid & 7);
-        if (m0 + row < L && gn < C) *(f32x4*)(dX + (m0 + row) * C + gn) = sum_partials(red, row, tid & 7);
+        if (m0 + row < L && gn < C) {
+            f32x4 sum = sum_partials(red, row, tid & 7);
+            if constexpr (ADD) sum += *(const f32x4*)(dX + (m0 + row) * C + gn);
+            *(f32x4*)(dX + (m0 + row) * C + gn) = sum;
+        }
     }
 }
 
@@ -295,15 +300,30 @@ hipError_t launch_fwd_f32(const LayerArgs& a, hipStream_t st) {
     });
 }
 
-hipError_t launch_dx_f32(const LayerArgs& a, hipStream_t st) {
+template <bool ADD>
+static hipError_t launch_dx(const LayerArgs& a, hipStream_t st) {
     if (a.L == 0 || a.dX == nullptr) return hipSuccess;
     return over_tiles(a.C, a.L, [&](dim3 grid, int x0, int y0) {
         with_rank_pairs(a.r, [&](auto rp) {
-            hipLaunchKernelGGL(dx_f32<decltype(rp)::value>, grid, dim3(NT), 0, st, (const float*)a.dY,
+            hipLaunchKernelGGL((dx_f32<decltype(rp)::value, ADD>), grid, dim3(NT), 0, st, (const float*)a.dY,
                                (const float*)a.W, a.M, (const float*)a.B, (const float*)a.A, (float*)a.dX, a.L,
                                (int)a.R, (int)a.C, (int)a.r, a.scale, (int)a.two_four, x0, y0);
         });
     });
+}
+
+hipError_t launch_dx_f32(const LayerArgs& a, hipStream_t st) { return launch_dx<false>(a, st); }
+
+hipError_t launch_gated_dx_f32(const LayerArgs& a, hipStream_t st) {
+    const hipError_t e = launch_dx<false>(a, st);
+    if (e != hipSuccess) return e;
+    LayerArgs b = a;
+    b.dY = a.second->dY;
+    b.W = a.second->W;
+    b.M = a.second->M;
+    b.B = a.second->B;
+    b.A = a.second->A;
+    return launch_dx<true>(b, st);
 }
 
 hipError_t launch_g_f32(const LayerArgs& a, hipStream_t st) {

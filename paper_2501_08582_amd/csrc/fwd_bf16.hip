@@ -43,9 +43,27 @@
 // before the barrier, as soon as the wave's own W copies have landed.
 #include "gemm_common.hpp"
 #include "kernels.hpp"
+#include "gated.hpp"
 
 #include <cmath>
 #include <type_traits>
+
+// The units that instantiate the gated block's kernels define LORS_GATED.
+#ifdef LORS_GATED
+#define LORS_FIRST(name) name##_gate
+#define LORS_MORE , Gated pair
+#define LORS_PAIR , pair_of(a)
+#define LORS_FWD launch_gated_fwd_bf16
+#define LORS_FWD_THIN launch_gated_fwd_thin_bf16
+#define LORS_FWD_FEW launch_gated_fwd_few_bf16
+#else
+#define LORS_FIRST(name) name
+#define LORS_MORE
+#define LORS_PAIR
+#define LORS_FWD launch_fwd_bf16
+#define LORS_FWD_THIN launch_fwd_thin_bf16
+#define LORS_FWD_FEW launch_fwd_few_bf16
+#endif
 
 namespace lors {
 namespace {
@@ -101,13 +119,15 @@ struct Layout {
 // accumulators, merges 32 NF rows of W', and the MFMA slots, X reads and
 // merge pieces of the missing token and feature blocks drop out of the
 // schedule.
+// LORS_GATED: the two projections of a gated block (Gated, gated.hpp), whose tiles a
+// workgroup computes one after the other; see the epilogue.
 template <int RK, bool KRAG, bool FOLD, int TM, int NF>
 __global__ __launch_bounds__(NT, 1) void fwd_kernel(
-    const uint16_t* __restrict__ X, const uint16_t* __restrict__ W,
-    const uint32_t* __restrict__ Mp, const uint16_t* __restrict__ Bm,
-    const uint16_t* __restrict__ Am, const uint16_t* __restrict__ bias,
+    const uint16_t* __restrict__ X, const uint16_t* __restrict__ LORS_FIRST(W),
+    const uint32_t* __restrict__ LORS_FIRST(Mp), const uint16_t* __restrict__ LORS_FIRST(Bm),
+    const uint16_t* __restrict__ LORS_FIRST(Am), const uint16_t* __restrict__ bias,
     uint16_t* __restrict__ Y, int64_t L, int R, int C, int r, float s, int tiles_m,
-    int tiles_n, int n_full, int split, float* __restrict__ part, int two_four) {
+    int tiles_n, int n_full, int split, float* __restrict__ part, int two_four LORS_MORE) {
     using Lay = Layout<RK, TM, NF>;
     constexpr int MBW = TM / 32;  // 32-token blocks per wave
     constexpr int SPAN = thin_span(TM);  // tokens of a logical tile
@@ -146,6 +166,16 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
         n0 = tn * BN + (u / (SPAN / TM)) * Lay::FT;
         if (m0 >= L || n0 >= R) return;  // a part of an edge tile that holds no output
     }
+#ifdef LORS_GATED
+    // the projections of a gated block: the gate's tile, then the up projection's
+#pragma unroll 1
+    for (int seg = 0; seg < 2; ++seg) {
+    const uint16_t* W = seg == 0 ? W_gate : pair.W;
+    const uint32_t* Mp = seg == 0 ? Mp_gate : pair.M;
+    const uint16_t* Bm = seg == 0 ? Bm_gate : pair.B;
+    const uint16_t* Am = seg == 0 ? Am_gate : pair.A;
+    if (seg == 1) lds_barrier();  // every wave has read its staged outputs
+#endif
     // last rows of the X and W slabs that exist
     const int lastm = (int)min(L - 1 - m0, (int64_t)(TM - 1));
     const int lastn = min(R - 1 - n0, Lay::FT - 1);
@@ -526,6 +556,7 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
     // in LDS (rows of 32 NF outputs), then 16-byte stores of whole rows.
     wait_vmcnt<0>();
     lds_barrier();  // every wave's copies landed and every read of the stages done
+#ifndef LORS_GATED
     if (TM == BM && NF == 2 && (int)blockIdx.x >= n_full) {
         // a piece of a split tile: its unrounded fp32 partial sums go to slice
         // blockIdx.x - n_full of `part` (256 tokens x 256 features); the
@@ -540,8 +571,60 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
                     dst[(32 * mb + 8 * (v >> 2) + 4 * h + (v & 3)) * BN + nrow0 + 32 * nb] = acc[mb][nb][v];
         return;
     }
+#endif
     constexpr int OW = 32 * NF;   // outputs per staged row
     constexpr int CH = OW / 8;    // 16-byte chunks per row
+#ifdef LORS_GATED
+    // Staged in fp32, in two halves where the tile has 256 tokens, so that
+    // the eight outputs of a lane's 16-byte stores are unrounded: the
+    // gate's tile gives G (where it is kept) and act(g), the latter in H's
+    // place; the up projection's gives U and multiplies what stands there.
+    // act(g) is rounded to bf16 on the way, half a step: its fp32 values would be
+    // a second array of twice H's bytes.  A lane reads the chunks that it wrote
+    // itself.
+    constexpr int ROWS = TM == BM ? TM / 2 : TM;
+    static_assert(4 * ROWS * OW * 4 <= Lay::S * Lay::STAGE, "fp32 staging fits the stage buffers");
+    float* of = (float*)(smem + wave * (ROWS * OW * 4));
+#pragma unroll
+    for (int half = 0; half < TM / ROWS; ++half) {
+#pragma unroll
+        for (int nb = 0; nb < NF; ++nb)
+#pragma unroll
+            for (int mb = 0; mb < ROWS / 32; ++mb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    of[(32 * mb + 8 * (v >> 2) + 4 * h + (v & 3)) * OW + 32 * nb + l32] =
+                        acc[ROWS / 32 * half + mb][nb][v];
+        uint16_t* kept = seg == 0 ? pair.G : pair.U;
+#pragma unroll 4
+        for (int it = 0; it < ROWS * CH / 64; ++it) {
+            const int row = (64 / CH) * it + lane / CH, ch = lane % CH;
+            const f32x4 lo = *(const f32x4*)(of + row * OW + 8 * ch), hi = *(const f32x4*)(of + row * OW + 8 * ch + 4);
+            const int64_t gm = m0 + ROWS * half + row;
+            const int gn = n0 + OW * wave + 8 * ch;
+            if (gm < L && gn < R) {
+                const int64_t at = gm * R + gn;
+                const float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                u32x4 raw8, out;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) raw8[q] = pack_bf16x2(f[2 * q], f[2 * q + 1]);
+                if (kept != nullptr) *(u32x4*)(kept + at) = raw8;
+                if (seg == 0) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        out[q] = pack_bf16x2(activate(f[2 * q], pair.gelu), activate(f[2 * q + 1], pair.gelu));
+                } else {
+                    const u32x4 g8 = *(const u32x4*)(Y + at);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        out[q] = pack_bf16x2(__uint_as_float(g8[q] << 16) * f[2 * q],
+                                             __uint_as_float(g8[q] & 0xFFFF0000u) * f[2 * q + 1]);
+                }
+                *(u32x4*)(Y + at) = out;
+            }
+        }
+    }
+#else
     uint16_t* ol = (uint16_t*)(smem + wave * (TM * OW * 2));
 #pragma unroll
     for (int nb = 0; nb < NF; ++nb) {
@@ -561,6 +644,10 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
         const int gn = n0 + OW * wave + 8 * ch;
         if (gm < L && gn < R) *(u32x4*)(Y + gm * R + gn) = v;
     }
+#endif
+#ifdef LORS_GATED
+    }
+#endif
 }
 
 // s.B is exact in bf16 for a power-of-two s (B's exponent shifts); the folded
@@ -587,7 +674,7 @@ void launch_whole(const LayerArgs& a, hipStream_t st, int grid, int tiles_m, int
     hipLaunchKernelGGL((fwd_kernel<RK, KRAG, FOLD, BM, 2>), dim3(grid), dim3(NT), 0, st,
                        (const uint16_t*)a.X, (const uint16_t*)a.W, a.M, (const uint16_t*)a.B,
                        (const uint16_t*)a.A, (const uint16_t*)a.bias, (uint16_t*)a.Y, a.L, (int)a.R, (int)a.C,
-                       (int)a.r, a.scale, tiles_m, tiles_n, n_full, split, part, (int)a.two_four);
+                       (int)a.r, a.scale, tiles_m, tiles_n, n_full, split, part, (int)a.two_four LORS_PAIR);
 }
 
 template <int RK>
@@ -625,7 +712,7 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
                                                             part);
     }
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && tp.tm > 0) e = launch_fwd_thin_bf16(a, st, tp.n_full, tp.tail, tp.tm);
+    if (e == hipSuccess && tp.tm > 0) e = LORS_FWD_THIN(a, st, tp.n_full, tp.tail, tp.tm);
     if (e == hipSuccess && sp.split > 1)
         e = launch_split_reduce_bf16(part, sp.n_full, sp.split, tiles_m, tiles_n, fwd_group_rows(tiles_m, tiles_n), a.L,
                                      (int)a.R, a.bias, a.Y, st);
@@ -643,7 +730,7 @@ hipError_t launch_thin_tm(const LayerArgs& a, hipStream_t st, int first, int tai
                        (const uint16_t*)a.X, (const uint16_t*)a.W, a.M, (const uint16_t*)a.B,
                        (const uint16_t*)a.A, (const uint16_t*)a.bias, (uint16_t*)a.Y, a.L, (int)a.R, (int)a.C,
                        (int)a.r, a.scale, tiles_m, tiles_n, first, tail, (float*)nullptr,
-                       (int)a.two_four);
+                       (int)a.two_four LORS_PAIR);
     return hipGetLastError();
 }
 
@@ -673,9 +760,9 @@ hipError_t launch_thin_rk(const LayerArgs& a, hipStream_t st, int first, int tai
 
 #ifndef LORS_THIN_TILES
 
-hipError_t launch_fwd_bf16(const LayerArgs& a, hipStream_t st) {
+hipError_t LORS_FWD(const LayerArgs& a, hipStream_t st) {
     if (a.L == 0) return hipSuccess;
-    if (!a.sparse_mfma && fwd_few_tokens(a.L, a.R, a.C)) return launch_fwd_few_bf16(a, st);
+    if (!a.sparse_mfma && fwd_few_tokens(a.L, a.R, a.C)) return LORS_FWD_FEW(a, st);
     switch ((a.r + 15) / 16) {
         case 1: return launch_rk<1>(a, st);
         case 2: return launch_rk<2>(a, st);
@@ -693,13 +780,13 @@ hipError_t launch_fwd_bf16(const LayerArgs& a, hipStream_t st) {
     const int n = thin_only_plan(a.L, a.R, run);
     hipError_t e = hipSuccess;
     for (int i = 0; i < n && e == hipSuccess; ++i)
-        e = launch_fwd_thin_bf16(a, st, run[i].n_full, run[i].tail, run[i].tm);
+        e = LORS_FWD_THIN(a, st, run[i].n_full, run[i].tail, run[i].tm);
     return e;
 }
 
 #else
 
-hipError_t launch_fwd_thin_bf16(const LayerArgs& a, hipStream_t st, int first, int tail, int tm) {
+hipError_t LORS_FWD_THIN(const LayerArgs& a, hipStream_t st, int first, int tail, int tm) {
     if (tail <= 0) return hipSuccess;
     switch ((a.r + 15) / 16) {
         case 1: return launch_thin_rk<1>(a, st, first, tail, tm);

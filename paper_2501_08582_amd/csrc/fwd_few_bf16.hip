@@ -18,8 +18,20 @@
 // added through LDS in wave order, so results are bitwise reproducible.
 #include "gemm_common.hpp"
 #include "kernels.hpp"
+#include "gated.hpp"
 
 #include <type_traits>
+
+// The unit that instantiates the gated block's kernels defines LORS_GATED.
+#ifdef LORS_GATED
+#define LORS_PAIR Gated
+#define LORS_PAIR_OF pair_of
+#define LORS_FWD_FEW launch_gated_fwd_few_bf16
+#else
+#define LORS_PAIR Alone
+#define LORS_PAIR_OF alone_of
+#define LORS_FWD_FEW launch_fwd_few_bf16
+#endif
 
 namespace lors {
 namespace {
@@ -67,19 +79,36 @@ struct Cfg {
 // chunk and dropped by zero W' and zero X.
 // (Its bounds checks take registers that EU = 4 does not leave: 8 spilled, 8192 x
 // 4104, rank 16, 1 token 19.2 us against 15.6 without that bound.)
-template <int FT, int RK, bool KRAG, int MB, int NB>
+// Pair: one projection, or the two of a gated block: every other wave then works on
+// the second, each half of the waves shares its contraction, and the join at the end
+// forms act(g) * u of their unrounded sums.
+template <int FT, int RK, bool KRAG, int MB, int NB, class Pair>
 __global__ __launch_bounds__((64 * Cfg<FT, RK, MB, NB>::NW),
                              (KRAG ? Cfg<FT, RK, MB, NB>::NW / 4 : Cfg<FT, RK, MB, NB>::EU)) void fwd_few_kernel(
-    const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, const uint32_t* __restrict__ Mp,
-    const uint16_t* __restrict__ Bm, const uint16_t* __restrict__ Am, const uint16_t* __restrict__ bias,
-    uint16_t* __restrict__ Y, int L, int R, int C, int r, float s, int two_four) {
+    const uint16_t* __restrict__ X, const uint16_t* __restrict__ W1, const uint32_t* __restrict__ M1,
+    const uint16_t* __restrict__ B1, const uint16_t* __restrict__ A1, const uint16_t* __restrict__ bias,
+    uint16_t* __restrict__ Y, int L, int R, int C, int r, float s, int two_four, Pair pair) {
     using T = Cfg<FT, RK, MB, NB>;
+    constexpr bool kGated = std::is_same<Pair, Gated>::value;
+    constexpr int KW = kGated ? T::NW / 2 : T::NW;  // waves that share a contraction
     constexpr int NW = T::NW, G = T::G, WV = T::WV, RC = T::RC, NV = T::NV, SLOTS = T::SLOTS;
     static_assert(T::TOTAL <= kLdsBytes, "LDS budget");
     __shared__ __attribute__((aligned(1024))) uint8_t smem[T::TOTAL];
 
     const int tid = threadIdx.x, lane = tid & 63, l = lane & (FT - 1), g = lane / FT;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kwave = kGated ? wave >> 1 : wave;
+    const uint16_t* W = W1;
+    const uint32_t* Mp = M1;
+    const uint16_t *Bm = B1, *Am = A1;
+    if constexpr (kGated) {
+        if (wave & 1) {
+            W = pair.W;
+            Mp = pair.M;
+            Bm = pair.B;
+            Am = pair.A;
+        }
+    }
     const int n0 = blockIdx.x * FT * NB, m0 = blockIdx.y * FT * MB;
     const int wpr = (C + 31) >> 5;
     const int nblk = (C + BK - 1) / BK;
@@ -141,7 +170,7 @@ __global__ __launch_bounds__((64 * Cfg<FT, RK, MB, NB>::NW),
     Block ring[SLOTS];
 #pragma unroll
     for (int i = 0; i < SLOTS - 1; ++i)
-        if (wave + i * NW < nblk) load(ring[i], wave + i * NW);
+        if (kwave + i * KW < nblk) load(ring[i], kwave + i * KW);
 
     if (tid < 16) *(u32x2*)(smem + T::LUT + 8 * tid) = two_four ? select_lut16_entry<true>((uint32_t)tid)
                                                             : select_lut16_entry<false>((uint32_t)tid);
@@ -191,10 +220,10 @@ __global__ __launch_bounds__((64 * Cfg<FT, RK, MB, NB>::NW),
         for (int v = 0; v < NV; ++v) acc[i / MB][i % MB][v] = 0.f;
     lds_barrier();  // the select table
 
-    for (int base = wave; base < nblk; base += SLOTS * NW) {
+    for (int base = kwave; base < nblk; base += SLOTS * KW) {
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
-            const int blk = base + i * NW;
+            const int blk = base + i * KW;
             if (blk >= nblk) break;
             Block& cur = ring[i];
             if constexpr (!T::XA) load_x(cur, blk * BK);
@@ -202,7 +231,7 @@ __global__ __launch_bounds__((64 * Cfg<FT, RK, MB, NB>::NW),
             for (int q = 0; q < 2 * RK; ++q)
                 if (8 * q + arow < r)
                     *(u32x4*)(as + (8 * q + arow) * kRow64 + 16 * (achunk ^ tr64_swz(arow))) = cur.a[q];
-            const int ahead = blk + (SLOTS - 1) * NW;
+            const int ahead = blk + (SLOTS - 1) * KW;
             if (ahead < nblk) load(ring[(i + SLOTS - 1) % SLOTS], ahead);
             asm volatile("" ::: "memory");  // one wave's LDS operations complete in order
 #pragma unroll
@@ -256,6 +285,28 @@ __global__ __launch_bounds__((64 * Cfg<FT, RK, MB, NB>::NW),
         const int f8 = it % (FT / 8), row = it / (FT / 8) % FT, i = it / (FT * FT / 8);
         // accumulator element v of lane group gg is token row 4G(v/4) + 4gg + v%4
         const int v = 4 * (row / (4 * G)) + (row & 3), gg = (row >> 2) % G;
+        if constexpr (kGated) {
+            float sum[2][8] = {};
+#pragma unroll 4
+            for (int w = 0; w < NW; ++w) {
+                const f32x4* p = (const f32x4*)(red + ((w * NI + i) * NV + v) * 64 + FT * gg + 8 * f8);
+                const f32x4 lo = p[0], hi = p[1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sum[w & 1][e] += lo[e];
+                    sum[w & 1][4 + e] += hi[e];
+                }
+            }
+            const int gm = m0 + FT * (i % MB) + row, gn = n0 + FT * (i / MB) + 8 * f8;
+            if (pair.G != nullptr) {
+                store8(sum[0], gm, gn, L, R, nullptr, pair.G);
+                store8(sum[1], gm, gn, L, R, nullptr, pair.U);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[0][e] = activate(sum[0][e], pair.gelu) * sum[1][e];
+            store8(sum[0], gm, gn, L, R, nullptr, Y);
+            continue;
+        }
         float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int w = 0; w < NW; ++w) {
@@ -277,10 +328,10 @@ hipError_t launch(const LayerArgs& a, hipStream_t st) {
     auto run = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(64 * Cfg<FT, RK, MB, NB>::NW), 0, st, (const uint16_t*)a.X, (const uint16_t*)a.W, a.M,
                            (const uint16_t*)a.B, (const uint16_t*)a.A, (const uint16_t*)a.bias, (uint16_t*)a.Y,
-                           (int)a.L, (int)a.R, (int)a.C, (int)a.r, a.scale, (int)a.two_four);
+                           (int)a.L, (int)a.R, (int)a.C, (int)a.r, a.scale, (int)a.two_four, LORS_PAIR_OF(a));
     };
-    if (a.C % BK != 0) run(fwd_few_kernel<FT, RK, true, MB, NB>);
-    else run(fwd_few_kernel<FT, RK, false, MB, NB>);
+    if (a.C % BK != 0) run(fwd_few_kernel<FT, RK, true, MB, NB, LORS_PAIR>);
+    else run(fwd_few_kernel<FT, RK, false, MB, NB, LORS_PAIR>);
     return hipGetLastError();
 }
 
@@ -303,7 +354,7 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_fwd_few_bf16(const LayerArgs& a, hipStream_t st) {
+hipError_t LORS_FWD_FEW(const LayerArgs& a, hipStream_t st) {
     switch ((a.r + 15) / 16) {
         case 1: return launch_rk<1>(a, st);
         case 2: return launch_rk<2>(a, st);

@@ -19,6 +19,20 @@
 // be zero on entry.
 #include "gemm_common.hpp"
 #include "kernels.hpp"
+#include "gated.hpp"
+
+#include <type_traits>
+
+// The unit that instantiates the gated block's kernels defines LORS_GATED.
+#ifdef LORS_GATED
+#define LORS_PAIR GatedGrad
+#define LORS_PAIR_OF grad_pair_of
+#define LORS_G launch_gated_g_bf16
+#else
+#define LORS_PAIR Alone
+#define LORS_PAIR_OF alone_of
+#define LORS_G launch_g_bf16
+#endif
 
 namespace lors {
 namespace {
@@ -55,12 +69,16 @@ constexpr int SMEM_ALL = SMEM + 32 * kRowBytes;
 // 64).  kChecked (L < BK, or offsets beyond 32 bits): every copy checks its
 // lanes and reads the zero page outside the tensors.
 enum Tokens { kWhole, kOverlap, kChecked };
-template <int RK, Tokens TOK>
+// Pair: one projection (Alone), or the two of a gated block (GatedGrad, gated.hpp) in one
+// grid: their G's one above the other, tiles_m rows of tiles in both together, so that
+// they share one short last wave.
+template <int RK, Tokens TOK, class Pair>
 __global__ __launch_bounds__(NT, 1) void g_kernel(
-    const uint16_t* __restrict__ dY, const uint16_t* __restrict__ X,
-    const uint32_t* __restrict__ Mt, const uint16_t* __restrict__ Bm,
-    const uint16_t* __restrict__ Am, float* __restrict__ dB, float* __restrict__ dA,
-    int64_t L, int R, int C, int r, float s, int tiles_m, int tiles_n, int n_full, int split) {
+    const uint16_t* __restrict__ dY1, const uint16_t* __restrict__ X,
+    const uint32_t* __restrict__ Mt1, const uint16_t* __restrict__ B1,
+    const uint16_t* __restrict__ A1, float* __restrict__ dB1, float* __restrict__ dA1,
+    int64_t L, int R, int C, int r, float s, int tiles_m, int tiles_n, int n_full, int split, Pair pair) {
+    constexpr bool kGated = std::is_same<Pair, GatedGrad>::value;
     constexpr int JB = (RK + 1) / 2;  // 32-wide blocks of the rank
     // dA exchange: JBC rank blocks per round, one 4 KiB slot [v/4][lane][4]
     // per (wj, column block b, rank block of the round), right after the B block
@@ -87,6 +105,21 @@ __global__ __launch_bounds__(NT, 1) void g_kernel(
     work_coords(blockIdx.x, tiles_m, tiles_n, g_group_rows(tiles_m, tiles_n, nk_all), n_full, split, nk_all, tm, tn,
                 kbeg, nk32);
     const int64_t nk = nk32;
+    const uint16_t* dY = dY1;
+    const uint32_t* Mt = Mt1;
+    const uint16_t *Bm = B1, *Am = A1;
+    float *dB = dB1, *dA = dA1;
+    if constexpr (kGated) {
+        if (tm >= (tiles_m >> 1)) {
+            tm -= tiles_m >> 1;
+            dY = pair.dY;
+            Mt = pair.Mt;
+            Bm = pair.B;
+            Am = pair.A;
+            dB = pair.dB;
+            dA = pair.dA;
+        }
+    }
     const int i0 = tm * BM;
     const int j0 = tn * BN;
     // first token of K-step kt of this workgroup, and the rows of the K-step
@@ -461,7 +494,7 @@ __global__ __launch_bounds__(NT, 1) void g_kernel(
 
 template <int RK>
 hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
-    const int tiles_m = (int)((a.R + BM - 1) / BM);
+    const int tiles_m = (int)((a.R + BM - 1) / BM) * (std::is_same<LORS_PAIR, GatedGrad>::value ? 2 : 1);
     const int tiles_n = (int)((a.C + BN - 1) / BN);
     const TailSplit sp = tail_split((int64_t)tiles_m * tiles_n, (a.L + BK - 1) / BK, kNoPartials);
     dim3 grid(sp.grid), block(NT);
@@ -474,17 +507,17 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
     const bool checked = a.L < BK || (int64_t)BK * a.R * 2 >= (1ll << 31) || (int64_t)BK * a.C * 2 >= (1ll << 31);
     auto run = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, block, 0, st, dY, X, a.Mt, B, A, a.dB, a.dA, a.L, (int)a.R, (int)a.C,
-                           (int)a.r, a.scale, tiles_m, tiles_n, sp.n_full, sp.split);
+                           (int)a.r, a.scale, tiles_m, tiles_n, sp.n_full, sp.split, LORS_PAIR_OF(a));
     };
-    if (checked) run(g_kernel<RK, kChecked>);
-    else if (a.L % BK != 0) run(g_kernel<RK, kOverlap>);
-    else run(g_kernel<RK, kWhole>);
+    if (checked) run(g_kernel<RK, kChecked, LORS_PAIR>);
+    else if (a.L % BK != 0) run(g_kernel<RK, kOverlap, LORS_PAIR>);
+    else run(g_kernel<RK, kWhole, LORS_PAIR>);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_g_bf16(const LayerArgs& a, hipStream_t st) {
+hipError_t LORS_G(const LayerArgs& a, hipStream_t st) {
     if (a.L == 0) return hipSuccess;  // dB, dA stay zero
     switch ((a.r + 15) / 16) {
         case 1: return launch_rk<1>(a, st);

@@ -1,0 +1,78 @@
+// The two projections of a gated block, H = act(G) * U with G = X . Wg'^T and
+// U = X . Wu'^T, as the tile kernels see them: the gate is the kernel's own
+// projection, the other one comes in a pair.  Alone: a projection by itself.
+#pragma once
+
+#include "device_common.hpp"
+#include "kernels.hpp"
+
+namespace lors {
+
+struct Alone {};
+static inline Alone alone_of(const LayerArgs&) { return {}; }
+
+// forward: G and U may be null (serving)
+struct Gated {
+    const uint16_t* W;
+    const uint32_t* M;
+    const uint16_t *B, *A;
+    uint16_t *G, *U;
+    int gelu;
+};
+
+static inline Gated pair_of(const LayerArgs& a) {
+    const SecondArgs& q = *a.second;
+    return {(const uint16_t*)q.W, q.M, (const uint16_t*)q.B, (const uint16_t*)q.A, (uint16_t*)q.G, (uint16_t*)q.U, (int)q.gelu};
+}
+
+// backward (dX, and the adapters' gradients)
+struct GatedGrad {
+    const uint16_t *dY, *W;
+    const uint32_t* Mt;
+    const uint16_t *B, *A;
+    float *dB, *dA;
+};
+
+static inline GatedGrad grad_pair_of(const LayerArgs& a) {
+    const SecondArgs& q = *a.second;
+    return {(const uint16_t*)q.dY, (const uint16_t*)q.W, q.Mt, (const uint16_t*)q.B, (const uint16_t*)q.A, q.dB, q.dA};
+}
+
+// tanh of the GELU's argument and that argument's slope.  tanh(x) = sign(x) (1 - e) / (1 + e)
+// with e = exp(-2|x|) <= 1: no overflow, and full relative accuracy where 1 - e has
+// it; below |x| = 1/16 the series x - x^3/3 + 2x^5/15 (the next term is 4e-8 of x)
+// stands for the difference that cancels.
+__device__ __forceinline__ float gelu_tanh(float g, float& slope) {
+    constexpr float k = 0.797884560802865356f;  // sqrt(2 / pi)
+    const float g2 = g * g;
+    const float x = k * g * (1.f + 0.044715f * g2);
+    slope = k * (1.f + 0.134145f * g2);
+    const float e = __expf(-2.f * fabsf(x)), x2 = x * x;
+    const float far = copysignf((1.f - e) / (1.f + e), x);
+    return fabsf(x) < 0.0625f ? x * (1.f + x2 * (-0.333333333f + 0.133333333f * x2)) : far;
+}
+
+// SiLU g / (1 + exp(-g)), or GELU g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  Where exp(-g)
+// overflows (g below -88) SiLU is -0, as its limit is.
+__device__ __forceinline__ float activate(float g, int gelu) {
+    if (gelu) {
+        float slope;
+        return 0.5f * g * (1.f + gelu_tanh(g, slope));
+    }
+    return g / (1.f + __expf(-g));
+}
+
+// act(g), and its derivative in `d`
+__device__ __forceinline__ float activate_grad(float g, int gelu, float& d) {
+    if (gelu) {
+        float slope;
+        const float t = gelu_tanh(g, slope);
+        d = 0.5f * (1.f + t) + 0.5f * g * (1.f - t * t) * slope;
+        return 0.5f * g * (1.f + t);
+    }
+    const float y = 1.f / (1.f + __expf(-g));
+    d = y * (1.f + g * (1.f - y));
+    return g * y;
+}
+
+}  // namespace lors

@@ -167,15 +167,21 @@ __device__ __forceinline__ const T* uniform_ptr(const T* p) {
 }
 
 // The same copies addressed as a wave-uniform base (SGPR pair) plus a 32-bit
-// per-lane byte offset: no per-lane 64-bit address arithmetic.
+// per-lane byte offset: no per-lane 64-bit address arithmetic.  A base that a vector
+// instruction wrote needs five wait states, which the compiler does not add in
+// front of inline assembly: units whose kernels keep so many uniform values that bases
+// come back out of vector registers (v_readlane) define LORS_COPY_WAIT as "s_nop 3".
+#ifndef LORS_COPY_WAIT
+#define LORS_COPY_WAIT "s_nop 0"
+#endif
 __device__ __forceinline__ void copy16s_to_lds(const void* sbase, uint32_t voff, uint32_t lds_wave_base) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+    asm volatile("s_mov_b32 m0, %2\n\t" LORS_COPY_WAIT "\n\tglobal_load_lds_dwordx4 %0, %1"
                  :
                  : "v"(voff), "s"(sbase), "s"(lds_wave_base)
                  : "memory", "m0");
 }
 __device__ __forceinline__ void copy4s_to_lds(const void* sbase, uint32_t voff, uint32_t lds_wave_base) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+    asm volatile("s_mov_b32 m0, %2\n\t" LORS_COPY_WAIT "\n\tglobal_load_lds_dword %0, %1"
                  :
                  : "v"(voff), "s"(sbase), "s"(lds_wave_base)
                  : "memory", "m0");

@@ -7,6 +7,23 @@
 
 namespace lors {
 
+// The other projection (the one without activation) of a gated block, of the same
+// extents as the first.
+struct SecondArgs {
+    const void* W;       // R x C
+    const uint32_t* M;
+    const uint32_t* Mt;  // backward
+    const void* B;       // R x r
+    const void* A;       // r x C
+    const void* dY;      // L x R: the gradient of U (the first projection's dY: that of G)
+    float* dB;
+    float* dA;
+    void* b_pad;
+    void* G;             // forward: L x R each, or nullptr
+    void* U;
+    bool gelu;
+};
+
 struct LayerArgs {
     int64_t R, C, L, r;
     float scale;
@@ -33,6 +50,7 @@ struct LayerArgs {
     int64_t r_grad;         // rank of dB and dA (the caller's r; the dX passes change a.r)
     void* split_ws;         // fp32 partial sums of split tiles (forward, dX), or nullptr: no split
     int64_t split_budget;   // bytes of split_ws the partial sums may use
+    const SecondArgs* second;  // a gated block's other projection, or nullptr
 };
 
 // Split of a grid of `tiles` output tiles whose K-loop has nk steps.  Whole
@@ -131,9 +149,23 @@ hipError_t launch_ste_bf16(const LayerArgs& a, hipStream_t s);  // dB, dA of the
 size_t ste_workspace_bytes(int64_t R, int64_t L, int64_t r);
 hipError_t launch_dbias_bf16(const LayerArgs& a, hipStream_t s);
 
+// Gated block (a.second): a.Y is H, a.dY the gradient of G.  dX is the sum over both
+// projections; dB and dA are cleared by the dX launch (a.clear_grads) or the caller.
+hipError_t launch_gated_fwd_bf16(const LayerArgs& a, hipStream_t s);
+hipError_t launch_gated_fwd_thin_bf16(const LayerArgs& a, hipStream_t s, int first, int tail, int tm);
+hipError_t launch_gated_fwd_few_bf16(const LayerArgs& a, hipStream_t s);
+hipError_t launch_gated_dx_bf16(const LayerArgs& a, hipStream_t s);
+hipError_t launch_gated_dx_thin_bf16(const LayerArgs& a, hipStream_t s, int ra, int first, int tail, int tm, bool clear);
+hipError_t launch_gated_g_bf16(const LayerArgs& a, hipStream_t s);
+// H = act(G) U, and dG = dH U act'(G), dU = dH act(G): n elements
+hipError_t launch_gated_join(const void* G, const void* U, void* H, int64_t n, bool gelu, bool bf16, hipStream_t s);
+hipError_t launch_gated_split(const void* dH, const void* G, const void* U, void* dG, void* dU, int64_t n, bool gelu,
+                              bool bf16, hipStream_t s);
+
 // fp32 path
 hipError_t launch_fwd_f32(const LayerArgs& a, hipStream_t s);
 hipError_t launch_dx_f32(const LayerArgs& a, hipStream_t s);
+hipError_t launch_gated_dx_f32(const LayerArgs& a, hipStream_t s);  // the sum over a gated block's projections
 hipError_t launch_g_f32(const LayerArgs& a, hipStream_t s);
 hipError_t launch_dbias_f32(const LayerArgs& a, hipStream_t s);
 

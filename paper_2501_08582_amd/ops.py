@@ -4,19 +4,26 @@ PyTorch supplies device memory and the current HIP stream; every step of the
 layer runs in ``liblors.so``.  Tensors must live on a ROCm device, be
 contiguous, and be bf16 or fp32 (packed masks are int32 tensors holding the
 uint32 words of the layouts documented in ``include/lors.h``).
+
+The gated half of a feed-forward block, out of two such projections, is
+``gated_forward``, ``gated_backward`` and ``lors_gated`` (with autograd).
 """
 from __future__ import annotations
 
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _lib
 
 BITMAP = "bitmap"
 TWO_FOUR = "2:4"
+SILU = "silu"
+GELU = "gelu"
 
 _FMT = {BITMAP: _lib.MASK_BITMAP, TWO_FOUR: _lib.MASK_2_4}
+_ACT = {SILU: _lib.ACT_SILU, GELU: _lib.ACT_GELU}
 _DT = {torch.bfloat16: _lib.DTYPE_BF16, torch.float32: _lib.DTYPE_F32}
 
 
@@ -256,3 +263,114 @@ def lors_linear(X, W, M, B, A, scale, mask_format=BITMAP, bias=None, ste=False):
     """Sparsity-preserved LoRA linear with autograd.  ``ste=True`` selects
     the straight-through adapter gradients of Section 2.3."""
     return LoRSLinearFn.apply(X, W, M, B, A, bias, scale, mask_format, ste)
+
+
+# ---------------------------------------------------------------------------
+# the gated half of a feed-forward block
+# ---------------------------------------------------------------------------
+def _act(activation) -> int:
+    try:
+        return _ACT[activation]
+    except (KeyError, TypeError):
+        raise ValueError(f"activation must be {SILU!r} or {GELU!r}, got {activation!r}")
+
+
+def _gated(X, gate, up, scale, mask_format, activation):
+    """(problem, activation, the two projections' descriptors, device) of a call on X
+    (L x C) and gate, up: (W, M, B, A) of the same shapes and dtype."""
+    act = _act(activation)
+    if len(gate) != 4 or len(up) != 4:
+        raise ValueError("gate and up must be (W, M, B, A)")
+    dev = _dev(X, *gate, *up)
+    W, M, B, A = gate
+    if W.dim() != 2 or B.dim() != 2 or A.dim() != 2:
+        raise ValueError("W, B and A must be matrices")
+    R, C = W.shape
+    r = B.shape[1]
+    if X.dim() == 0 or X.shape[-1] != C:
+        raise ValueError(f"X has shape {tuple(X.shape)}, the projections take rows of {C}")
+    for which, (W, M, B, A) in (("gate", gate), ("up", up)):
+        for name, t, shape in (("W", W, (R, C)), ("B", B, (R, r)), ("A", A, (r, C))):
+            if t.shape != shape or t.dtype != X.dtype:
+                raise ValueError(f"{which} {name}: expected {shape} of {X.dtype}, got {tuple(t.shape)} of {t.dtype}")
+        if M.dtype != torch.int32 or M.numel() != mask_words(R, C):
+            raise ValueError(f"{which} M: expected a packed mask, int32 with R*ceil(C/32) words")
+    p = _lib.problem(R, C, X.numel() // C, r, scale, _dt(X), _fmt(mask_format))
+    return p, act, [_lib.Projection(*(t.data_ptr() for t in q)) for q in (gate, up)], dev
+
+
+def _scratch(p, backward: bool, dev):
+    need = _lib.gated_workspace_bytes(p, backward)
+    if need == 2**64 - 1:
+        raise ValueError("invalid problem")
+    return (torch.empty(need, dtype=torch.uint8, device=dev) if need else None), need
+
+
+def gated_forward(X: torch.Tensor, gate: Tuple, up: Tuple, scale: float, mask_format=BITMAP, activation: str = SILU,
+                  save: bool = True):
+    """(H, G, U): G = X . Wg'^T, U = X . Wu'^T and H = act(G) * U of two sparsity-preserved
+    LoRA projections ``gate`` and ``up``, each (W, M, B, A) as in ``forward``, of the same
+    shapes.  X may have leading dims.  ``activation``: "silu", or "gelu" (by tanh).
+    G and U are what ``gated_backward`` needs; ``save=False`` leaves them out (None)."""
+    p, act, pair, dev = _gated(X, gate, up, scale, mask_format, activation)
+    shape = (*X.shape[:-1], p.R)
+    H = X.new_empty(shape)
+    G, U = (X.new_empty(shape), X.new_empty(shape)) if save else (None, None)
+    ws, need = (None, 0) if save else _scratch(p, False, dev)
+    _call(dev, "lors_gated_forward", _lib.gated_forward, p, act, _ptr(X), *pair, _ptr(G), _ptr(U), _ptr(H), _ptr(ws), need)
+    return H, G, U
+
+
+def gated_backward(dH: torch.Tensor, X: torch.Tensor, gate: Tuple, up: Tuple, G: torch.Tensor, U: torch.Tensor,
+                   scale: float, mask_format=BITMAP, activation: str = SILU, need_dx: bool = True,
+                   grad_dtype: torch.dtype = torch.float32):
+    """(dX, (dB, dA) of the gate, (dB, dA) of the up projection): the exact, masked
+    gradients from the gradient of H, in ``grad_dtype`` (fp32, or bf16 for bf16
+    problems, rounded once more)."""
+    p, act, pair, dev = _gated(X, gate, up, scale, mask_format, activation)
+    shape = (*X.shape[:-1], p.R)
+    if _dev(dH, G, U) != dev:
+        raise ValueError("all tensors must be on the same device")
+    for name, t in (("dH", dH), ("G", G), ("U", U)):
+        if t.shape != shape or t.dtype != X.dtype:
+            raise ValueError(f"{name}: expected {shape} of {X.dtype}, got {tuple(t.shape)} of {t.dtype}")
+    if grad_dtype != torch.float32 and grad_dtype != X.dtype:
+        raise TypeError(f"grad_dtype {grad_dtype} not supported (fp32, or the problem's)")
+    dX = torch.empty_like(X) if need_dx else None
+    nB, nA = p.R * p.r, p.r * p.C  # R and C are multiples of 16 bytes: every part stays aligned
+    flat = torch.empty(2 * (nB + nA), dtype=torch.float32, device=dev)
+    parts = flat.split((nB, nA, nB, nA))
+    ws, need = _scratch(p, True, dev)
+    _call(dev, "lors_gated_backward", _lib.gated_backward, p, act, _ptr(dH), _ptr(X), *pair, _ptr(G), _ptr(U), _ptr(dX),
+          *(t.data_ptr() for t in parts), _ptr(ws), need)
+    if grad_dtype == torch.bfloat16:
+        low = torch.empty(flat.shape, dtype=torch.bfloat16, device=dev)
+        _call(dev, "lors_round_bf16", _lib.round_bf16, flat.data_ptr(), flat.numel(), low.data_ptr(), None, 0, None)
+        parts = low.split((nB, nA, nB, nA))
+    dBg, dAg, dBu, dAu = (t.view(s) for t, s in zip(parts, ((p.R, p.r), (p.r, p.C)) * 2))
+    return dX, (dBg, dAg), (dBu, dAu)
+
+
+class LoRSGatedFn(torch.autograd.Function):
+    """Autograd op: saves X, G, U and the projections' tensors, never W' or the
+    gradients of G and U."""
+
+    @staticmethod
+    def forward(ctx, X, Wg, Mg, Bg, Ag, Wu, Mu, Bu, Au, scale, mask_format, activation):
+        ctx.args = float(scale), mask_format, activation
+        H, G, U = gated_forward(X, (Wg, Mg, Bg, Ag), (Wu, Mu, Bu, Au), scale, mask_format, activation)
+        ctx.save_for_backward(X, Wg, Mg, Bg, Ag, Wu, Mu, Bu, Au, G, U)
+        return H
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dH):
+        X, Wg, Mg, Bg, Ag, Wu, Mu, Bu, Au, G, U = ctx.saved_tensors
+        dX, (dBg, dAg), (dBu, dAu) = gated_backward(dH.contiguous(), X, (Wg, Mg, Bg, Ag), (Wu, Mu, Bu, Au), G, U, *ctx.args,
+                                                    need_dx=ctx.needs_input_grad[0], grad_dtype=X.dtype)
+        return dX, None, None, dBg, dAg, None, None, dBu, dAu, None, None, None
+
+
+def lors_gated(X, gate, up, scale, mask_format=BITMAP, activation=SILU):
+    """``gated_forward``'s H with autograd, by X and both projections' B and A."""
+    return LoRSGatedFn.apply(X, *gate, *up, scale, mask_format, activation)
