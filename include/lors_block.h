@@ -87,6 +87,69 @@ lors_status_t lors_gated_backward(const lors_problem_t* p, int32_t activation, c
                                   const void* U, void* dX, float* dB_gate, float* dA_gate, float* dB_up, float* dA_up,
                                   void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------- update */
+
+#define LORS_UPDATE_MAX_SIDE 128  /* of a matrix's shorter side */
+#define LORS_UPDATE_MAX_STEPS 32
+
+/*
+ * The direction of a matrix v, with its shorter side taken as its rows:
+ *   x = v / (|v| + eps)   (|.|: the root of the sum of squares)
+ *   `steps` times:  S = x x^T,  x <- a x + (b S + c S^2) x
+ * S, the product of the steps and the direction's sums are in 64 bits; the direction is
+ * rounded once, to fp32, before the update.
+ * momentum in [0, 1], eps >= 0 and a, b, c finite, 1 <= steps <=
+ * LORS_UPDATE_MAX_STEPS; otherwise LORS_ERR_SHAPE.  In directions that v does not
+ * have, S holds its own rounding, 2^-53 of its norm, which a step raises by a^2: a
+ * larger a^(2 steps) than 2^38 is refused (LORS_ERR_UNSUPPORTED).
+ */
+typedef struct lors_update_desc {
+    double momentum;
+    double eps;
+    double a, b, c;
+    int32_t steps;
+    int32_t nesterov;     /* 0 or 1 */
+    int32_t grad_dtype;   /* lors_dtype_t */
+    int32_t param_dtype;  /* lors_dtype_t */
+    uint32_t flags;       /* 0, otherwise LORS_ERR_UNSUPPORTED */
+} lors_update_t;
+
+/*
+ * One matrix of a call, rows x cols, row-major and contiguous.
+ * 1 <= rows, cols < 2^31 and the shorter of them at most LORS_UPDATE_MAX_SIDE
+ * (LORS_ERR_UNSUPPORTED above), rows * cols < 2^40, rate and decay finite; otherwise
+ * LORS_ERR_SHAPE.  Pointers are aligned to their elements.
+ *   m     <- momentum . m + (1 - momentum) . grad           (in place)
+ *   v      = nesterov ? momentum . m + (1 - momentum) . grad : m;   grad where m is NULL
+ *   master <- (1 - decay) . master - rate . direction(v)    (in place)
+ *   param  = master, rounded; rate . direction(v) where master is NULL
+ * param may be NULL where master is not.
+ */
+typedef struct lors_update_item {
+    int64_t rows;
+    int64_t cols;
+    const void* grad;
+    float* m;
+    float* master;
+    void* param;
+    double rate;
+    double decay;
+} lors_update_item_t;
+
+/* Device scratch bytes of lors_orthogonal_update.  (size_t)-1 if the arguments are
+ * invalid. */
+size_t lors_orthogonal_workspace_bytes(const lors_update_t* p, const lors_update_item_t* items, int64_t count);
+
+/*
+ * One step of `count` matrices (0 .. 2^20, otherwise LORS_ERR_SHAPE).  `items` is a
+ * host array, read during the call.  m, master and param may not overlap anything
+ * else of the call (the same array in two items: LORS_ERR_ALIAS).  Every result is a
+ * function of the inputs alone, bit for bit; where a matrix's gradient holds an Inf
+ * or NaN, that matrix's results are NaN, no other's.
+ */
+lors_status_t lors_orthogonal_update(const lors_update_t* p, const lors_update_item_t* items, int64_t count,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -60,9 +60,12 @@ EXPORTED_TRAIN = (
 # include/lors_block.h
 ACT_SILU = 0
 ACT_GELU = 1
+UPDATE_MAX_SIDE = 128
+UPDATE_MAX_STEPS = 32
 
 EXPORTED_BLOCK = (
     "lors_block_version", "lors_gated_workspace_bytes", "lors_gated_forward", "lors_gated_backward",
+    "lors_orthogonal_workspace_bytes", "lors_orthogonal_update",
 )
 
 
@@ -159,6 +162,34 @@ class Projection(ctypes.Structure):
     ]
 
 
+class Update(ctypes.Structure):
+    _fields_ = [
+        ("momentum", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("a", ctypes.c_double),
+        ("b", ctypes.c_double),
+        ("c", ctypes.c_double),
+        ("steps", ctypes.c_int32),
+        ("nesterov", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+        ("param_dtype", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class UpdateItem(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("grad", ctypes.c_void_p),
+        ("m", ctypes.c_void_p),
+        ("master", ctypes.c_void_p),
+        ("param", ctypes.c_void_p),
+        ("rate", ctypes.c_double),
+        ("decay", ctypes.c_double),
+    ]
+
+
 class LorsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -211,6 +242,8 @@ def _declare(lib) -> None:
         "lors_gated_workspace_bytes": (_sz, [P, ctypes.c_int]),
         "lors_gated_forward": (ctypes.c_int, [P, _i32, _vp, PJ, PJ, _vp, _vp, _vp, _vp, _sz, _vp]),
         "lors_gated_backward": (ctypes.c_int, [P, _i32, _vp, _vp, PJ, PJ] + [_vp] * 8 + [_sz, _vp]),
+        "lors_orthogonal_workspace_bytes": (_sz, [ctypes.POINTER(Update), ctypes.POINTER(UpdateItem), _i64]),
+        "lors_orthogonal_update": (ctypes.c_int, [ctypes.POINTER(Update), ctypes.POINTER(UpdateItem), _i64, _vp, _sz, _vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -361,3 +394,11 @@ def gated_backward(p: Problem, activation, dH, X, gate: Projection, up: Projecti
                    dA_up, ws, ws_bytes, stream) -> int:
     return lib().lors_gated_backward(ctypes.byref(p), activation, dH, X, ctypes.byref(gate), ctypes.byref(up), G, U, dX,
                                      dB_gate, dA_gate, dB_up, dA_up, ws, ws_bytes, stream)
+
+
+def orthogonal_workspace_bytes(p: Update, items, count) -> int:
+    return lib().lors_orthogonal_workspace_bytes(ctypes.byref(p), items, count)
+
+
+def orthogonal_update(p: Update, items, count, ws, ws_bytes, stream) -> int:
+    return lib().lors_orthogonal_update(ctypes.byref(p), items, count, ws, ws_bytes, stream)

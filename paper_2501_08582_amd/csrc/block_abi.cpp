@@ -6,10 +6,14 @@
 // call is free of side effects.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <memory>
+#include <new>
 
 #include "abi_common.hpp"
+#include "block_kernels.hpp"
 #include "kernels.hpp"
 #include "lors_block.h"
 
@@ -93,6 +97,57 @@ lors::LayerArgs second_alone(const lors::LayerArgs& a) {
     b.dA = q.dA;
     b.second = nullptr;
     return b;
+}
+
+// ---------------------------------------------------------------------------
+// update
+// ---------------------------------------------------------------------------
+constexpr int64_t kMostMatrices = int64_t(1) << 20;
+
+// Checks in the documented order, up to the range of the extents.
+lors_status_t check_update(const lors_update_t* p, const lors_update_item_t* items, int64_t count) {
+    if (p == nullptr || (count > 0 && items == nullptr)) return LORS_ERR_NULL;
+    if (count > kMostMatrices) return LORS_ERR_SHAPE;
+    for (int64_t i = 0; i < count; ++i)
+        if (items[i].grad == nullptr || (items[i].master == nullptr && items[i].param == nullptr)) return LORS_ERR_NULL;
+    if (!valid_dtype(p->grad_dtype) || !valid_dtype(p->param_dtype)) return LORS_ERR_DTYPE;
+    if (count < 0 || !(p->momentum >= 0.0 && p->momentum <= 1.0) || !std::isfinite(p->eps) || p->eps < 0.0 ||
+        !std::isfinite(p->a) || !std::isfinite(p->b) || !std::isfinite(p->c) || p->steps < 1 ||
+        p->steps > LORS_UPDATE_MAX_STEPS || (p->nesterov != 0 && p->nesterov != 1))
+        return LORS_ERR_SHAPE;
+    for (int64_t i = 0; i < count; ++i) {
+        const lors_update_item_t& q = items[i];
+        if (q.rows < 1 || q.cols < 1 || q.rows > kMaxExtent || q.cols > kMaxExtent || q.rows * q.cols >= int64_t(1) << 40 ||
+            !std::isfinite(q.rate) || !std::isfinite(q.decay))
+            return LORS_ERR_SHAPE;
+    }
+    if (p->flags != 0 || 2 * p->steps * std::log2(std::fabs(p->a)) > 38.0) return LORS_ERR_UNSUPPORTED;
+    for (int64_t i = 0; i < count; ++i)
+        if (std::min(items[i].rows, items[i].cols) > LORS_UPDATE_MAX_SIDE) return LORS_ERR_UNSUPPORTED;
+    return LORS_OK;
+}
+
+int64_t scratch_of(const lors_update_item_t& q) {
+    return lors::block::update_scratch(std::min(q.rows, q.cols), std::max(q.rows, q.cols));
+}
+
+// What a call reads or writes, to find overlaps by a sort.
+struct Span {
+    uintptr_t lo, hi;
+    bool out;
+};
+
+// Whether an output overlaps anything else: in the order of their starts, a span meets an
+// earlier one where it starts before the furthest end so far.
+bool any_overlap(Span* s, int64_t n) {
+    std::sort(s, s + n, [](const Span& x, const Span& y) { return x.lo < y.lo; });
+    uintptr_t ends = 0, out_ends = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (s[i].lo < (s[i].out ? ends : out_ends)) return true;
+        ends = std::max(ends, s[i].hi);
+        if (s[i].out) out_ends = std::max(out_ends, s[i].hi);
+    }
+    return false;
 }
 
 }  // namespace
@@ -204,6 +259,58 @@ lors_status_t lors_gated_backward(const lors_problem_t* p, int32_t activation, c
     if (e == hipSuccess) e = lors::launch_g_f32(a, s);
     if (e == hipSuccess) e = lors::launch_g_f32(b, s);
     return from_hip(e);
+}
+
+size_t lors_orthogonal_workspace_bytes(const lors_update_t* p, const lors_update_item_t* items, int64_t count) {
+    if (check_update(p, items, count) != LORS_OK) return static_cast<size_t>(-1);
+    int64_t need = 0;
+    for (int64_t i = 0; i < count; ++i) need += scratch_of(items[i]);
+    return static_cast<size_t>(need);
+}
+
+lors_status_t lors_orthogonal_update(const lors_update_t* p, const lors_update_item_t* items, int64_t count,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+    const lors_status_t st = check_update(p, items, count);
+    if (st != LORS_OK || count == 0) return st;
+    const int64_t gs = elt_size(p->grad_dtype), ps = elt_size(p->param_dtype);
+    std::unique_ptr<Span[]> spans(new (std::nothrow) Span[4 * count + 1]);
+    std::unique_ptr<lors::block::Matrix[]> matrices(new (std::nothrow) lors::block::Matrix[count]);
+    if (!spans || !matrices) return LORS_ERR_HIP;
+    int64_t n = 0, need = 0;
+    auto span = [&](const void* at, int64_t bytes, bool out) {
+        const uintptr_t lo = reinterpret_cast<uintptr_t>(at);
+        if (at != nullptr && bytes > 0) spans[n++] = Span{lo, lo + static_cast<uintptr_t>(bytes), out};
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        const lors_update_item_t& q = items[i];
+        const int64_t size = q.rows * q.cols;
+        const lors_status_t at = check_alignment({{q.grad, 0, gs}, {q.m, 0, 4}, {q.master, 0, 4}, {q.param, 0, ps}});
+        if (at != LORS_OK) return at;
+        span(q.grad, size * gs, false);
+        span(q.m, size * 4, true);
+        span(q.master, size * 4, true);
+        span(q.param, size * ps, true);
+        matrices[i] = lors::block::Matrix{q.grad, q.m, q.master, q.param, std::max(q.rows, q.cols), need, static_cast<float>(q.rate),
+                                          static_cast<float>(1.0 - q.decay), static_cast<int32_t>(std::min(q.rows, q.cols)),
+                                          q.rows <= q.cols ? 1 : 0};
+        need += scratch_of(q);
+    }
+    if (check_alignment({{workspace, 0, 16}}) != LORS_OK) return LORS_ERR_ALIGN;
+    span(workspace, need, true);
+    if (any_overlap(spans.get(), n)) return LORS_ERR_ALIAS;
+    if (check_workspace(workspace, workspace_bytes, static_cast<size_t>(need)) != LORS_OK) return LORS_ERR_WORKSPACE;
+    const lors::block::UpdateArgs a{static_cast<float>(p->momentum),
+                                    static_cast<float>(1.0 - p->momentum),
+                                    p->nesterov != 0,
+                                    p->eps,
+                                    p->a,
+                                    p->b,
+                                    p->c,
+                                    p->steps,
+                                    p->grad_dtype == LORS_DTYPE_BF16,
+                                    p->param_dtype == LORS_DTYPE_BF16,
+                                    static_cast<uint8_t*>(workspace)};
+    return from_hip(lors::block::launch_update(a, matrices.get(), count, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -5,6 +5,8 @@
 ``norm``        residual + dropout(x) and its layer norm or root-mean-square norm
 ``embedding``   the scaled lookup of token rows
 ``preference``  log-probabilities of target tokens and the paired preference loss
+``orthogonal``  update directions of adapters by Newton-Schulz steps, and the
+                optimiser that steps along them
 
 As in ``ops``, PyTorch supplies device memory and the current HIP stream and
 every step runs in ``liblors.so``.  Tensors must live on a ROCm device, be
@@ -19,7 +21,8 @@ captured graph can advance its masks.
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple
+import math
+from typing import List, Optional, Sequence, Tuple, Union
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -469,3 +472,114 @@ class PreferenceLossFn(torch.autograd.Function):
 def preference_loss(logits, targets, ref=None, beta=0.1, smoothing=0.0):
     """(loss, reward, logp) with autograd: gradients flow from the loss alone."""
     return PreferenceLossFn.apply(logits, targets, ref, beta, smoothing)
+
+
+# ---------------------------------------------------------------------------
+# orthogonalised updates
+# ---------------------------------------------------------------------------
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)  # of the steps: singular values of 0.002 to 1 end between 0.7 and 1.2
+
+
+def _update(momentum, nesterov, coefficients, steps, eps, grad, param) -> _lib.Update:
+    a, b, c = coefficients
+    return _lib.Update(momentum, eps, a, b, c, steps, int(bool(nesterov)), _dt(grad), _dt(param), 0)
+
+
+def _matrices(what: str, ts: Sequence[torch.Tensor], like: Optional[Sequence[torch.Tensor]] = None,
+              dtype: Optional[torch.dtype] = None) -> None:
+    """Contiguous matrices of one device and type, of the shapes of ``like``."""
+    if like is not None and len(ts) != len(like):
+        raise ValueError(f"{what}: expected {len(like)} matrices, got {len(ts)}")
+    dtype = dtype or ts[0].dtype
+    index = (like or ts)[0].get_device()
+    for i, t in enumerate(ts):
+        if t.dim() != 2 or t.dtype != dtype or (like is not None and t.shape != like[i].shape):
+            shape = tuple(like[i].shape) if like is not None else "a matrix"
+            raise ValueError(f"{what} {i}: expected {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+        if t.get_device() != index or index < 0 or not t.is_contiguous():
+            _dev((like or ts)[0], t)  # which says what is wrong
+
+
+def _run_update(p: _lib.Update, items, count: int, ws: Optional[torch.Tensor], dev: torch.device) -> None:
+    _call(dev, "lors_orthogonal_update", _lib.orthogonal_update, p, items, count, _ptr(ws), 0 if ws is None else ws.numel())
+
+
+def orthogonalize(X: Union[torch.Tensor, Sequence[torch.Tensor]], steps: int = 5,
+                  coefficients: Tuple[float, float, float] = COEFFICIENTS, eps: float = 1e-7):
+    """The Newton-Schulz direction of a matrix, or of each of a list (as a list): x = X / (|X| + eps), then
+    ``steps`` times x <- a x + (b S + c S^2) x with S = x x^T on the shorter side, of at
+    most 128.  With the default steps every singular value above a fivehundredth of |X| comes near 1.
+    X's dtype; 64-bit steps, one rounding."""
+    one = isinstance(X, torch.Tensor)
+    Xs = [X] if one else list(X)
+    if not Xs:
+        return []
+    _matrices("matrix", Xs)
+    dev = _dev(Xs[0])
+    out = [torch.empty_like(t) for t in Xs]
+    p = _update(0.0, False, coefficients, steps, eps, Xs[0], Xs[0])
+    items = (_lib.UpdateItem * len(Xs))(*((*t.shape, t.data_ptr(), None, None, o.data_ptr(), 1.0, 0.0) for t, o in zip(Xs, out)))
+    live = [i for i, t in enumerate(Xs) if t.numel()]
+    if len(live) < len(Xs):  # matrices of no elements have nothing to do
+        items = (_lib.UpdateItem * len(live))(*(items[i] for i in live))
+    if live:
+        ws = _workspace(_lib.orthogonal_workspace_bytes(p, items, len(live)), dev)
+        _run_update(p, items, len(live), ws, dev)
+    return out[0] if one else out
+
+
+class OrthogonalUpdate:
+    """An optimiser of matrices with a short side (adapters: R x r, r x C; the shorter side is at most 128).  Of each matrix,
+
+        m      <- momentum . m + (1 - momentum) . grad
+        v       = momentum . m + (1 - momentum) . grad  (Nesterov), or m
+        master <- (1 - lr . weight_decay) . master - lr . sqrt(max(1, rows / cols)) . direction(v)
+        param   = master in the parameter's type
+
+    with the direction of ``orthogonalize``.  ``masters`` and ``momenta`` are fp32 (momenta: zeros if
+    not given) and changed in place; ``params``, of one type, receive the masters' values and may be
+    left out.  All matrices take one call of three launches for every 48 of a size of the short side
+    (up to 16, 32, 64, 128).  ``step`` may be captured into a graph; its scratch memory belongs to
+    the object, so steps of one object must not overlap."""
+
+    def __init__(self, masters: Sequence[torch.Tensor], params: Optional[Sequence[torch.Tensor]] = None,
+                 momenta: Optional[Sequence[torch.Tensor]] = None, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay: float = 0.0, steps: int = 5, coefficients: Tuple[float, float, float] = COEFFICIENTS,
+                 eps: float = 1e-7):
+        self.masters: List[torch.Tensor] = list(masters)
+        if not self.masters:
+            raise ValueError("no matrices")
+        _matrices("master", self.masters, dtype=torch.float32)
+        self.momenta = [torch.zeros_like(t) for t in self.masters] if momenta is None else list(momenta)
+        _matrices("momentum", self.momenta, self.masters, torch.float32)
+        self.params = None if params is None else list(params)
+        if self.params is not None:
+            _matrices("param", self.params, self.masters)
+        self.weight_decay = float(weight_decay)
+        self._device = _dev(self.masters[0])
+        self._rule = (momentum, nesterov, coefficients, steps, eps)
+        kept = [0] * len(self.masters) if self.params is None else [t.data_ptr() for t in self.params]
+        self._items = (_lib.UpdateItem * len(self.masters))(*(
+            (*w.shape, w.data_ptr(), m.data_ptr(), w.data_ptr(), q or None, 0.0, 0.0)
+            for w, m, q in zip(self.masters, self.momenta, kept)))
+        self._shape_rate = [math.sqrt(max(1.0, w.shape[0] / w.shape[1])) if w.numel() else 1.0 for w in self.masters]
+        self._lr: Optional[float] = None
+        p = self._descriptor(self.masters[0])
+        self._ws = _workspace(_lib.orthogonal_workspace_bytes(p, self._items, len(self.masters)), self._device)
+
+    def _descriptor(self, grad: torch.Tensor) -> _lib.Update:
+        return _update(*self._rule, grad, self.masters[0] if self.params is None else self.params[0])
+
+    def step(self, grads: Sequence[torch.Tensor], lr: float) -> None:
+        """One step along the gradients (of the masters' shapes; all bf16 or all fp32)."""
+        grads = list(grads)
+        _matrices("gradient", grads, self.masters)
+        items = self._items
+        if lr != self._lr:
+            decay = lr * self.weight_decay
+            for item, rate in zip(items, self._shape_rate):
+                item.rate, item.decay = lr * rate, decay
+            self._lr = lr
+        for item, g in zip(items, grads):
+            item.grad = g.data_ptr()
+        _run_update(self._descriptor(grads[0]), items, len(grads), self._ws, self._device)
