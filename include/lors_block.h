@@ -150,6 +150,49 @@ size_t lors_orthogonal_workspace_bytes(const lors_update_t* p, const lors_update
 lors_status_t lors_orthogonal_update(const lors_update_t* p, const lors_update_item_t* items, int64_t count,
                                      void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------- sample */
+
+/*
+ * Logits of `rows` distributions over `vocab` entries; row n starts at element
+ * n . row_stride.  0 <= rows < 2^31, 1 <= vocab < 2^31, row_stride >= 0, rows . vocab <
+ * 2^57; temperature and min_p finite and >= 0, top_p >= 0; otherwise LORS_ERR_SHAPE.
+ * Pointers are aligned to their elements.
+ *   temperature  0: the largest entry; otherwise weights w = exp((z - max z) / temperature)
+ *   top_k        keep the first top_k of the entries (<= 0: all) ...
+ *   top_p        ... the shortest run of those that holds top_p of their weight (>= 1: all)
+ *   min_p        ... and of that the entries with w >= min_p (the largest one has w = 1)
+ * Entries are ordered by logit, equal ones by index; the first is always kept.
+ */
+typedef struct lors_sample_desc {
+    int64_t rows;
+    int64_t vocab;
+    int64_t row_stride;
+    double temperature;
+    int64_t top_k;
+    double top_p;
+    double min_p;
+    int32_t dtype;   /* lors_dtype_t */
+    uint32_t flags;  /* 0, otherwise LORS_ERR_UNSUPPORTED */
+} lors_sample_t;
+
+/* Device scratch bytes of lors_sample.  (size_t)-1 if p is invalid. */
+size_t lors_sample_workspace_bytes(const lors_sample_t* p);
+
+/*
+ * token[n]: the first kept entry, by index, at which the running sum of the kept
+ * entries' weights exceeds u[n] (fp32 in [0, 1)) times their sum; the last kept one of
+ * positive weight if none does.  logp[n] (may be NULL): log of that entry's weight over
+ * the sum.  Weights and sums are in 64 bits.
+ * temperature, top_k, top_p, min_p: NULL, or device arrays of `rows` that take the
+ * place of the scalars; there, a temperature that is not above 0 counts as 0, and a
+ * top_p or min_p that is NaN as none.
+ * -Inf entries have no weight.  A row that holds a NaN, or +Inf, or nothing but -Inf,
+ * has no distribution: token -1, logp NaN.
+ */
+lors_status_t lors_sample(const lors_sample_t* p, const void* logits, const float* u, const float* temperature,
+                          const int32_t* top_k, const float* top_p, const float* min_p, int64_t* token, float* logp,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -66,6 +66,7 @@ UPDATE_MAX_STEPS = 32
 EXPORTED_BLOCK = (
     "lors_block_version", "lors_gated_workspace_bytes", "lors_gated_forward", "lors_gated_backward",
     "lors_orthogonal_workspace_bytes", "lors_orthogonal_update",
+    "lors_sample_workspace_bytes", "lors_sample",
 )
 
 
@@ -190,6 +191,20 @@ class UpdateItem(ctypes.Structure):
     ]
 
 
+class Sample(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+        ("temperature", ctypes.c_double),
+        ("top_k", ctypes.c_int64),
+        ("top_p", ctypes.c_double),
+        ("min_p", ctypes.c_double),
+        ("dtype", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
 class LorsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -244,6 +259,8 @@ def _declare(lib) -> None:
         "lors_gated_backward": (ctypes.c_int, [P, _i32, _vp, _vp, PJ, PJ] + [_vp] * 8 + [_sz, _vp]),
         "lors_orthogonal_workspace_bytes": (_sz, [ctypes.POINTER(Update), ctypes.POINTER(UpdateItem), _i64]),
         "lors_orthogonal_update": (ctypes.c_int, [ctypes.POINTER(Update), ctypes.POINTER(UpdateItem), _i64, _vp, _sz, _vp]),
+        "lors_sample_workspace_bytes": (_sz, [ctypes.POINTER(Sample)]),
+        "lors_sample": (ctypes.c_int, [ctypes.POINTER(Sample)] + [_vp] * 9 + [_sz, _vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -402,3 +419,11 @@ def orthogonal_workspace_bytes(p: Update, items, count) -> int:
 
 def orthogonal_update(p: Update, items, count, ws, ws_bytes, stream) -> int:
     return lib().lors_orthogonal_update(ctypes.byref(p), items, count, ws, ws_bytes, stream)
+
+
+def sample_workspace_bytes(p: Sample) -> int:
+    return lib().lors_sample_workspace_bytes(ctypes.byref(p))
+
+
+def sample(p: Sample, logits, u, temperature, top_k, top_p, min_p, token, logp, ws, ws_bytes, stream) -> int:
+    return lib().lors_sample(ctypes.byref(p), logits, u, temperature, top_k, top_p, min_p, token, logp, ws, ws_bytes, stream)

@@ -313,4 +313,38 @@ lors_status_t lors_orthogonal_update(const lors_update_t* p, const lors_update_i
     return from_hip(lors::block::launch_update(a, matrices.get(), count, static_cast<hipStream_t>(stream)));
 }
 
+static lors_status_t check_sample(const lors_sample_t* p) {
+    if (!valid_dtype(p->dtype)) return LORS_ERR_DTYPE;
+    if (p->rows < 0 || p->rows > kMaxExtent || p->vocab < 1 || p->vocab > kMaxExtent || p->row_stride < 0 ||
+        p->rows * p->vocab >= int64_t(1) << 57)
+        return LORS_ERR_SHAPE;
+    if (p->rows > 0 && bytes_of(p->rows, p->row_stride, 4) < 0) return LORS_ERR_SHAPE;
+    if (!std::isfinite(p->temperature) || p->temperature < 0.0 || !(p->top_p >= 0.0) || !std::isfinite(p->min_p) || p->min_p < 0.0)
+        return LORS_ERR_SHAPE;
+    return p->flags != 0 ? LORS_ERR_UNSUPPORTED : LORS_OK;
+}
+
+size_t lors_sample_workspace_bytes(const lors_sample_t* p) {
+    return p == nullptr || check_sample(p) != LORS_OK ? static_cast<size_t>(-1) : 0;
+}
+
+lors_status_t lors_sample(const lors_sample_t* p, const void* logits, const float* u, const float* temperature,
+                          const int32_t* top_k, const float* top_p, const float* min_p, int64_t* token, float* logp,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    if (p == nullptr) return LORS_ERR_NULL;
+    if (p->rows != 0 && (logits == nullptr || u == nullptr || token == nullptr)) return LORS_ERR_NULL;
+    lors_status_t st = check_sample(p);
+    if (st != LORS_OK) return st;
+    const int64_t es = elt_size(p->dtype), n = p->rows;
+    const int64_t z = n == 0 ? 0 : ((n - 1) * p->row_stride + p->vocab) * es;
+    const size_t need = lors_sample_workspace_bytes(p);
+    st = check_arrays({{logits, z, es}, {u, 4 * n, 4}, {temperature, 4 * n, 4}, {top_k, 4 * n, 4}, {top_p, 4 * n, 4}, {min_p, 4 * n, 4}},
+                      {{token, 8 * n, 8}, {logp, 4 * n, 4}, {workspace, static_cast<int64_t>(need), 16}});
+    if (st == LORS_OK) st = check_workspace(workspace, workspace_bytes, need);
+    if (st != LORS_OK) return st;
+    const lors::block::SampleArgs a{n,           p->vocab, p->row_stride, p->temperature, p->top_k, p->top_p, p->min_p, logits,
+                                    u,           temperature, top_k,      top_p,          min_p,    token,    logp,     workspace};
+    return from_hip(lors::block::launch_sample(a, p->dtype == LORS_DTYPE_BF16, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

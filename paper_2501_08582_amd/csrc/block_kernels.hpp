@@ -36,5 +36,22 @@ struct UpdateArgs {
 int64_t update_scratch(int64_t d, int64_t n);
 hipError_t launch_update(const UpdateArgs& a, const Matrix* matrices, int64_t count, hipStream_t s);
 
+struct SampleArgs {
+    int64_t rows, vocab, row_stride;
+    double temperature;
+    int64_t top_k;
+    double top_p, min_p;
+    const void* logits;
+    const float* u;
+    const float* temperatures;  // or nullptr each
+    const int32_t* top_ks;
+    const float* top_ps;
+    const float* min_ps;
+    int64_t* token;
+    float* logp;                // or nullptr
+    void* workspace;
+};
+hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t s);
+
 }  // namespace block
 }  // namespace lors

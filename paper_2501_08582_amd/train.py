@@ -7,6 +7,7 @@
 ``preference``  log-probabilities of target tokens and the paired preference loss
 ``orthogonal``  update directions of adapters by Newton-Schulz steps, and the
                 optimiser that steps along them
+``sample``      tokens drawn from logits: temperature, top-k, top-p, min-p
 
 As in ``ops``, PyTorch supplies device memory and the current HIP stream and
 every step runs in ``liblors.so``.  Tensors must live on a ROCm device, be
@@ -583,3 +584,59 @@ class OrthogonalUpdate:
         for item, g in zip(items, grads):
             item.grad = g.data_ptr()
         _run_update(self._descriptor(grads[0]), items, len(grads), self._ws, self._device)
+
+
+# ---------------------------------------------------------------------------
+# sampling
+# ---------------------------------------------------------------------------
+def _per_row(value, what: str, shape, dtype: torch.dtype, dev: torch.device):
+    """(scalar, tensor or None) of a parameter that is one number or one a row."""
+    if not isinstance(value, torch.Tensor):
+        return value, None
+    if value.shape != shape or value.dtype != dtype:
+        raise ValueError(f"{what}: expected {tuple(shape)} of {dtype}, got {tuple(value.shape)} of {value.dtype}")
+    if _dev(value) != dev:
+        raise ValueError("all tensors must be on the same device")
+    return 0, value
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Union[float, torch.Tensor] = 1.0,
+           top_k: Union[int, torch.Tensor] = 0, top_p: Union[float, torch.Tensor] = 1.0,
+           min_p: Union[float, torch.Tensor] = 0.0) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(token, logp): a token of each row of logits (... x vocab, contiguous in the last dimension;
+    rows of a matrix may be strided), int64, and the log of its probability among what is kept, fp32.
+    Entries are ordered by logit, equal ones by index.  top_k keeps the first top_k of them (0: all), top_p the
+    shortest run of those that holds top_p of their probability (1: all), min_p those of at least
+    min_p times the largest probability; the first is always kept.  The token is the first kept one, by
+    index, at which the running sum of probabilities exceeds u (fp32 in [0, 1), one a row) times their
+    whole.  temperature 0: the first.  Each parameter may be a tensor of one value a row (fp32; top_k
+    int32).  A row with a NaN or +Inf, or of -Inf alone, gives token -1 and logp NaN."""
+    if not logits.is_cuda:
+        raise ValueError("all tensors must be on the GPU")
+    if logits.dim() == 0 or logits.shape[-1] == 0:
+        raise ValueError("expected a last dimension of at least one element")
+    shape, vocab = logits.shape[:-1], logits.shape[-1]
+    if logits.stride(-1) != 1 and vocab > 1:
+        raise ValueError("logits must be contiguous in their last dimension")
+    if logits.dim() == 2:
+        stride = logits.stride(0)
+    elif logits.is_contiguous():
+        stride = vocab
+    else:
+        raise ValueError("logits must be contiguous, or a matrix with strided rows")
+    _fp32(shape, "u", u)
+    dev = _place(u)
+    if dev != logits.device:
+        raise ValueError("all tensors must be on the same device")
+    T, Ts = _per_row(temperature, "temperature", shape, torch.float32, dev)
+    k, ks = _per_row(top_k, "top_k", shape, torch.int32, dev)
+    p, ps = _per_row(top_p, "top_p", shape, torch.float32, dev)
+    low, lows = _per_row(min_p, "min_p", shape, torch.float32, dev)
+    d = _lib.Sample(u.numel(), vocab, stride, T, k, p, low, _dt(logits), 0)
+    token = torch.empty(shape, dtype=torch.int64, device=dev)
+    logp = torch.empty(shape, dtype=torch.float32, device=dev)
+    need = _lib.sample_workspace_bytes(d)
+    ws = _workspace(need, dev)
+    _call(dev, "lors_sample", _lib.sample, d, logits.data_ptr(), u.data_ptr(), _ptr(Ts), _ptr(ks), _ptr(ps), _ptr(lows),
+          token.data_ptr(), logp.data_ptr(), _ptr(ws), need)
+    return token, logp
