@@ -48,66 +48,134 @@ struct Shared {
 };
 
 // Inclusive sums over the workgroup's threads of a and b.
-__device__ __forceinline__ void scan2(uint64_t& a, uint64_t& b, Shared& s) {
+template <class A>
+__device__ __forceinline__ void scan2(A& a, uint64_t& b, Shared& s) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t x = __shfl_up(a, o), y = __shfl_up(b, o);
+        const A x = __shfl_up(a, o);
+        const uint64_t y = __shfl_up(b, o);
         if (lane >= o) {
             a += x;
             b += y;
         }
     }
     __syncthreads();
+    A* wa = (A*)s.wave64;
     if (lane == 63) {
-        s.wave64[wave] = a;
+        wa[wave] = a;
         s.wave64[kWaves + wave] = b;
     }
     __syncthreads();
     for (int w = 0; w < wave; ++w) {
-        a += s.wave64[w];
+        a += wa[w];
         b += s.wave64[kWaves + w];
     }
+}
+
+// s.list descending; n entries, the others 0 and at its end.
+__device__ __forceinline__ void sort_list(Shared& s, uint32_t n) {
+    const int tid = threadIdx.x;
+    if (tid >= (int)n) s.list[tid] = 0;
+    const uint32_t size = n <= 2 ? 2 : 1u << (32 - __clz((int)(n - 1)));
+    for (uint32_t w = 2; w <= size; w <<= 1)
+        for (uint32_t o = w >> 1; o > 0; o >>= 1) {
+            __syncthreads();
+            const int j = tid ^ (int)o;
+            if (j > tid && tid < (int)size) {
+                const uint64_t x = s.list[tid], y = s.list[j];
+                if ((x < y) == (w == size || (tid & w) == 0)) {
+                    s.list[tid] = y;
+                    s.list[j] = x;
+                }
+            }
+        }
+    __syncthreads();
+}
+
+// 2^t for t <= 0, to 2^-46 of its value: 2^f on |f| <= 1/2 by its Taylor series (the next
+// term is 2^-47).  A weight takes this many 64-bit operations, 14, of about 45 that a
+// division and the library's exp take.
+__device__ __forceinline__ double power_of_two(double t) {
+    if (!(t > -1000.)) return 0.;
+    const double n = rint(t), x = (t - n) * 0.693147180559945309417;
+    double y = 1. / 39916800.;
+    y = fma(y, x, 1. / 3628800.);
+    y = fma(y, x, 1. / 362880.);
+    y = fma(y, x, 1. / 40320.);
+    y = fma(y, x, 1. / 5040.);
+    y = fma(y, x, 1. / 720.);
+    y = fma(y, x, 1. / 120.);
+    y = fma(y, x, 1. / 24.);
+    y = fma(y, x, 1. / 6.);
+    y = fma(y, x, 0.5);
+    y = fma(y, x, 1.);
+    y = fma(y, x, 1.);
+    return ldexp(y, (int)n);
 }
 
 template <typename T>
 struct Row {
     static constexpr int U = train::kUnit<T>;
+    static constexpr int AHEAD = 4;  // units in flight in a lane
     const T* at;
     uint32_t V;
-    // f(logit, index) over the elements of this thread
+    // f(logit, index, whether it exists) over the elements of this thread, every lane of a
+    // wave at the same time
     template <class F>
     __device__ __forceinline__ void each(F f) const {
-        for (uint64_t i = (uint64_t)threadIdx.x * U; i < V; i += (uint64_t)NT * U) {
-            const int n = V - i < U ? (int)(V - i) : U;
-            const train::F<U> z = train::widen<T, U>(train::load_unit<T, U>(at + i, n));
+        const uint32_t wave0 = (threadIdx.x & ~63u) * U;
+        for (uint64_t i0 = 0; i0 + wave0 < V; i0 += (uint64_t)AHEAD * NT * U) {
+            train::Raw<T, U> raw[AHEAD];
+            int n[AHEAD];
 #pragma unroll
-            for (int e = 0; e < U; ++e)
-                if (e < n) f(z.v[e], (uint32_t)i + e);
+            for (int q = 0; q < AHEAD; ++q) {
+                const uint64_t i = i0 + (uint64_t)(q * NT + threadIdx.x) * U;
+                n[q] = i < V ? (V - i < U ? (int)(V - i) : U) : 0;
+                raw[q] = train::load_unit<T, U>(n[q] ? at + i : at, n[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                const uint64_t i = i0 + (uint64_t)(q * NT + threadIdx.x) * U;
+                const train::F<U> z = train::widen<T, U>(raw[q]);
+#pragma unroll
+                for (int e = 0; e < U; ++e) f(z.v[e], (uint32_t)i + e, e < n[q]);
+            }
         }
     }
 };
 
+// Appends q of the lanes that hold one: one addition a wave.  s.listed counts all, the
+// list holds the first kSorted.
+__device__ __forceinline__ void append(Shared& s, bool some, uint64_t q) {
+    const uint64_t mask = __ballot(some);
+    if (mask == 0) return;
+    const int lane = threadIdx.x & 63, leader = __ffsll((unsigned long long)mask) - 1;
+    uint32_t at = 0;
+    if (lane == leader) at = atomicAdd(&s.listed, (uint32_t)__popcll(mask));
+    at = __shfl(at, leader) + __popcll(mask & ((1ull << lane) - 1));
+    if (some && at < kSorted) s.list[at] = q;
+}
+
+// Any logits: passes as above.
 template <typename T>
-__global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
-    __shared__ Shared s;
+__device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Shared& s) {
     constexpr int U = Row<T>::U;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t n = train::block_id();
-    if (n >= a.rows) return;
     const Row<T> row{(const T*)a.logits + n * a.row_stride, (uint32_t)a.vocab};
     const double T0 = a.temperatures != nullptr ? (double)a.temperatures[n] : a.temperature;
     const int64_t k0 = a.top_ks != nullptr ? a.top_ks[n] : a.top_k;
     const double p0 = a.top_ps != nullptr ? (double)a.top_ps[n] : a.top_p;
     const double low0 = a.min_ps != nullptr ? (double)a.min_ps[n] : a.min_p;
     const double low = low0 > 0. ? low0 : 0.;  // (NaN: none)
+    const double u = (double)a.u[n];
 
     // ---- pass 1
     uint64_t best = 0;
     bool broken = false;  // NaN or +Inf
-    row.each([&](float z, uint32_t i) {
-        broken |= !(z < INFINITY);
-        const uint64_t q = place_of(z, i);
+    row.each([&](float z, uint32_t i, bool some) {
+        broken |= some && !(z < INFINITY);
+        const uint64_t q = some ? place_of(z, i) : 0;
         best = q > best ? q : best;
     });
     if (broken) best = ~0ull;
@@ -129,8 +197,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
         }
         return;
     }
-    const double topd = (double)top;
-    auto weight = [&](float z) { return exp(((double)z - topd) / T0); };
+    // (bounded: the largest logit itself has the weight 1 at any temperature)
+    const double topd = (double)top, rate = fmin(1.44269504088896340736 / T0, 1e300);
+    // (finite z; T0 of Inf gives every one the same)
+    auto weight = [&](float z) { return power_of_two(((double)z - topd) * rate); };
 
     // ---- passes 2 and 3: the last kept place
     uint64_t last = 0;  // everything
@@ -141,7 +211,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
         const double unit = ldexp(1., bits);
         auto fixed = [&](float z) { return z > -INFINITY ? (uint64_t)(weight(z) * unit + 0.5) : 0ull; };
         const float per = (float)(kBinsPerNat / T0);
-        // a level of bins: the entries in (lo, hi], those before it, the shift of the later levels
+        // the entries in [lo, hi] by a level of bins; the first level goes by the logits
         uint64_t lo = 0, hi = ~0ull;
         auto bin_of = [&](float z, uint64_t q, int shift) {
             if (shift < 0) {
@@ -152,14 +222,17 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
         };
         uint64_t total = 0;  // of what the filter before kept
         for (int filter = k != 0 ? 0 : 1; filter < (by_mass ? 2 : 1); ++filter) {
-            // the border: of the entries in their order, the first `rank`, or those before
-            // which less than `goal` lies
-            const uint64_t floor_ = last;
+            // the border: of the entries in their order, the first k, or those before which
+            // less than `goal` lies.  The second filter needs no counts: bins of no
+            // weight hold nothing that it keeps.
+            const bool counts = filter == 0;
+            const uint64_t from = last;
             lo = 0;
             hi = ~0ull;
             int shift = -1;
             uint64_t count0 = 0, mass0 = 0;
             double goal = 0.;
+            uint32_t listed = 0;
             for (;;) {
                 for (int b = tid; b < kBins; b += NT) {
                     s.mass[b] = 0;
@@ -172,11 +245,11 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
                     s.found[1] = 0;
                 }
                 __syncthreads();
-                row.each([&](float z, uint32_t i) {
+                row.each([&](float z, uint32_t i, bool some) {
                     const uint64_t q = place_of(z, i);
-                    if (q < lo || q > hi || q < floor_) return;
+                    if (!some || q < lo || q > hi || q < from) return;
                     const int b = bin_of(z, q, shift);
-                    atomicAdd(&s.count[b], 1u);
+                    if (counts) atomicAdd(&s.count[b], 1u);
                     if (by_mass) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)fixed(z));
                 });
                 __syncthreads();
@@ -195,12 +268,9 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
                 }
                 // the border's bin: the last that is not empty and in front of which too little lies
                 const uint64_t cb[2] = {count0 + c - c0 - c1, count0 + c - c1}, mb[2] = {mass0 + m - m0 - m1, mass0 + m - m1};
-                const uint32_t cs[2] = {c0, c1};
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const bool in = cs[e] != 0 && (filter == 0 ? cb[e] < k : (double)mb[e] < goal || cb[e] == 0);
-                    if (in) atomicMax(&s.bin, 2 * tid + e);
-                }
+                const bool in0 = counts ? c0 != 0 && cb[0] < k : m0 != 0 && ((double)mb[0] < goal || mb[0] == 0);
+                const bool in1 = counts ? c1 != 0 && cb[1] < k : m1 != 0 && ((double)mb[1] < goal || mb[1] == 0);
+                if (in0 || in1) atomicMax(&s.bin, 2 * tid + (in1 ? 1 : 0));
                 __syncthreads();
                 const int bin = s.bin;
                 if (2 * tid == (bin & ~1)) {
@@ -208,22 +278,79 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
                     s.found[3] = mb[bin & 1];
                 }
                 __syncthreads();
-                const uint32_t inside = s.count[bin];
+                const uint64_t inside = counts ? s.count[bin] : 0;
+                // top-k of few: all up to the border, which the rest is found among
+                const bool whole = counts && shift < 0 && s.found[2] + inside <= kSorted;
+                row.each([&](float z, uint32_t i, bool some) {
+                    const uint64_t q = place_of(z, i);
+                    bool in = some && q >= lo && q <= hi && q >= from;
+                    if (in) {
+                        const int b = bin_of(z, q, shift);
+                        in = whole ? b <= bin : b == bin;
+                    }
+                    append(s, in, q);
+                });
+                __syncthreads();
+                listed = s.listed;
+                if (whole) {
+                    sort_list(s, listed);
+                    // entry `tid` of the order; what top-k, top-p and min-p keep of it
+                    const uint64_t q = s.list[tid];
+                    const float z = logit_of((uint32_t)(q >> 32));
+                    const bool first_k = tid < (int)listed && (uint64_t)tid < k && z > -INFINITY;
+                    const double w = first_k ? weight(z) : 0.;
+                    uint64_t sum = first_k && by_mass ? fixed(z) : 0, rank = first_k ? 1 : 0;
+                    const uint64_t own = sum;
+                    scan2(rank, sum, s);
+                    __syncthreads();
+                    if (tid == NT - 1) s.found[2] = sum;
+                    __syncthreads();
+                    const double limit = p0 * (double)s.found[2];
+                    const bool in = first_k && w >= low && (!by_mass || (double)(sum - own) < limit || tid == 0);
+                    if (tid == 0) s.bin = NT;
+                    __syncthreads();
+                    if (!in) atomicMin(&s.bin, tid);
+                    s.runs[tid] = w;
+                    __syncthreads();
+                    const int kept_n = s.bin;  // the first entries of the order
+                    // by index: the list holds the inverted index above the place in the order
+                    s.list[tid] = (q & 0xFFFFFFFFull) << 32 | (uint32_t)tid;
+                    __syncthreads();
+                    sort_list(s, (uint32_t)kept_n);
+                    const uint64_t e = s.list[tid];
+                    const bool some = tid < kept_n;
+                    const double mine = some ? s.runs[(uint32_t)e] : 0.;
+                    double upto = mine;
+                    uint64_t nothing = 0;
+                    scan2(upto, nothing, s);
+                    __syncthreads();
+                    if (tid == NT - 1) s.runs[0] = upto;
+                    if (tid == 0) s.bin = kSorted;
+                    __syncthreads();
+                    const double all = s.runs[0];
+                    if (some && mine > 0. && upto > u * all) atomicMin(&s.bin, tid);
+                    __syncthreads();
+                    if (s.bin == kSorted) {  // none exceeds it: the last of positive weight
+                        __syncthreads();
+                        if (tid == 0) s.bin = -1;
+                        __syncthreads();
+                        if (mine > 0.) atomicMax(&s.bin, tid);
+                        __syncthreads();
+                    }
+                    if (tid == s.bin) {
+                        a.token[n] = (int64_t)(uint32_t)~(uint32_t)(e >> 32);
+                        if (a.logp != nullptr) a.logp[n] = (float)log(mine / all);
+                    }
+                    return;
+                }
                 count0 = s.found[2];
                 mass0 = s.found[3];
-                if (inside <= kSorted) {
-                    row.each([&](float z, uint32_t i) {
-                        const uint64_t q = place_of(z, i);
-                        if (q < lo || q > hi || q < floor_ || bin_of(z, q, shift) != bin) return;
-                        s.list[atomicAdd(&s.listed, 1u)] = q;
-                    });
-                    break;
-                }
+                if (listed <= kSorted) break;
                 // too many: their range, and another level
                 uint64_t least = ~0ull, most = 0;
-                row.each([&](float z, uint32_t i) {
+                row.each([&](float z, uint32_t i, bool some) {
                     const uint64_t q = place_of(z, i);
-                    if (q < lo || q > hi || q < floor_ || bin_of(z, q, shift) != bin) return;
+                    if (!some || q < lo || q > hi || q < from || bin_of(z, q, shift) != bin) return;
                     least = q < least ? q : least;
                     most = q > most ? q : most;
                 });
@@ -237,29 +364,13 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
                 if (shift < 0) shift = 0;
                 __syncthreads();
             }
-            __syncthreads();
-            const uint32_t listed = s.listed;
-            if (tid >= (int)listed) s.list[tid] = 0;
-            // descending
-            for (int w = 2; w <= kSorted; w <<= 1)
-                for (int o = w >> 1; o > 0; o >>= 1) {
-                    __syncthreads();
-                    const int j = tid ^ o;
-                    if (j > tid) {
-                        const uint64_t x = s.list[tid], y = s.list[j];
-                        if ((x < y) == ((tid & w) == 0)) {
-                            s.list[tid] = y;
-                            s.list[j] = x;
-                        }
-                    }
-                }
-            __syncthreads();
+            sort_list(s, listed);
             const uint64_t q = s.list[tid];
             const bool some = tid < (int)listed;
             uint64_t c = some ? 1 : 0, m = some && by_mass ? fixed(logit_of((uint32_t)(q >> 32))) : 0;
             const uint64_t own = m;
             scan2(c, m, s);
-            const bool in = some && (filter == 0 ? count0 + c - 1 < k : (double)(mass0 + m - own) < goal || count0 + c == 1);
+            const bool in = some && (counts ? count0 + c - 1 < k : (double)(mass0 + m - own) < goal || mass0 + m - own == 0);
             if (tid == 0) s.bin = -1;
             __syncthreads();
             if (in) atomicMax(&s.bin, tid);
@@ -276,6 +387,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
     }
 
     // ---- pass 4
+    constexpr int AHEAD = Row<T>::AHEAD;
     const uint64_t blocks = ((uint64_t)row.V + 64 * U - 1) / (64 * U);
     const uint32_t reps = (uint32_t)((blocks + kRuns - 1) / kRuns);  // blocks of a run
     const int runs = (int)((blocks + reps - 1) / reps);
@@ -284,26 +396,42 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
         const double w = weight(z);
         return w >= low ? w : 0.;
     };
-    // this lane's U elements of a block: their weights
-    auto load = [&](uint64_t block, double (&w)[U]) {
+    // this lane's U elements of a block, and their weights
+    auto load = [&](uint64_t block, int& m) {
         const uint64_t i = (block * 64 + lane) * U;
-        const int m = i < row.V ? (row.V - i < U ? (int)(row.V - i) : U) : 0;
-        train::F<U> z{};
-        if (m > 0) z = train::widen<T, U>(train::load_unit<T, U>(row.at + i, m));
-#pragma unroll
-        for (int e = 0; e < U; ++e) w[e] = e < m ? kept(z.v[e], (uint32_t)i + e) : 0.;
+        m = i < row.V ? (row.V - i < U ? (int)(row.V - i) : U) : 0;
+        return train::load_unit<T, U>(m ? row.at + i : row.at, m);
     };
-    for (int r = wave; r < runs; r += kWaves) {
-        double sum = 0.;
-        for (uint32_t b = 0; b < reps; ++b) {
-            double w[U];
-            load((uint64_t)r * reps + b, w);
+    auto weigh = [&](const train::Raw<T, U>& raw, int m, uint64_t block, double (&w)[U]) {
+        const train::F<U> z = train::widen<T, U>(raw);
 #pragma unroll
-            for (int e = 0; e < U; ++e) sum += w[e];
+        for (int e = 0; e < U; ++e) w[e] = e < m ? kept(z.v[e], (uint32_t)((block * 64 + lane) * U) + e) : 0.;
+    };
+    for (int r0 = wave; r0 < runs; r0 += AHEAD * kWaves) {
+        double sum[AHEAD] = {};
+        for (uint32_t b = 0; b < reps; ++b) {
+            train::Raw<T, U> raw[AHEAD];
+            int m[AHEAD];
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                const int r = r0 + q * kWaves;
+                raw[q] = load(r < runs ? (uint64_t)r * reps + b : blocks, m[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                double w[U];
+                weigh(raw[q], m[q], (uint64_t)(r0 + q * kWaves) * reps + b, w);
+#pragma unroll
+                for (int e = 0; e < U; ++e) sum[q] += w[e];
+            }
         }
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) s.runs[r] = sum;
+        for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) sum[q] += __shfl_xor(sum[q], o);
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q)
+            if (lane == 0 && r0 + q * kWaves < runs) s.runs[r0 + q * kWaves] = sum[q];
     }
     __syncthreads();
     if (wave != 0) return;
@@ -320,7 +448,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
         if (lane >= o) upto_lane += x;
     }
     const double whole = __shfl(upto_lane, 63);
-    const double goal = (double)a.u[n] * whole;
+    const double goal = u * whole;
     // the first run at whose end the sum exceeds the goal; else the last of positive weight
     int first = runs, positive = -1;
     double base = 0., run = __shfl_up(upto_lane, 1);
@@ -352,8 +480,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
     double weight_of = 0.;
     for (uint32_t b = 0; b < reps; ++b) {
         double w[U];
+        int m;
         const uint64_t block = (uint64_t)chosen * reps + b;
-        load(block, w);
+        const train::Raw<T, U> raw = load(block, m);
+        weigh(raw, m, block, w);
         double sum = 0.;
 #pragma unroll
         for (int e = 0; e < U; ++e) sum += w[e];
@@ -396,6 +526,408 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
     if (lane == 0) {
         a.token[n] = token;
         if (a.logp != nullptr) a.logp[n] = (float)log(weight_of / whole);
+    }
+}
+
+// bf16 logits of 2^-30 <= |z| < 2^16, 0 and -Inf: few enough values to count the entries of
+// each, which takes no arithmetic an entry, no search and no sort:
+//   A  counts by value; with them the largest, the weights, the borders of every filter and
+//      the kept weight, all on the values; a border that cuts a value's entries keeps the
+//      first of them by index
+//   B  sums of the kept entries' weights (out of a table) by runs, and the token
+struct Values {
+    static constexpr int kLeast = (127 - 30) << 7, kSpan = 46 << 7;  // magnitudes' bits
+    static constexpr int kZero = kSpan, kEach = (2 * kSpan + NT) / NT, kCount = kEach * NT;
+    double weight[kCount];
+    uint32_t count[kCount];
+    double runs[kRuns];
+    uint32_t ties[kRuns];
+    uint64_t wave64[2 * kWaves];
+    double mass;
+    uint32_t before;
+    int first, border, quota, odd;
+    // descending: the larger values first; -1: -Inf, -2: not one of these values
+    static __device__ __forceinline__ int bin_of(uint32_t b) {
+        const uint32_t m = b & 0x7FFFu, d = m - kLeast;
+        if (d < (uint32_t)kSpan) return (b & 0x8000u) ? kZero + 1 + (int)d : kZero - 1 - (int)d;
+        return m == 0 ? kZero : b == 0xFF80u ? -1 : -2;
+    }
+    static __device__ __forceinline__ float value_of(int bin) {
+        const uint32_t m = bin == kZero ? 0u : bin < kZero ? (uint32_t)(kLeast + kZero - 1 - bin) : 0x8000u | (uint32_t)(kLeast + bin - kZero - 1);
+        return bf16_bits_to_f32(m);
+    }
+};
+static_assert(Values::kCount > 2 * Values::kSpan, "every value has a bin");
+static_assert(sizeof(Values) <= 160 * 1024, "LDS");
+
+template <class V>
+__device__ __forceinline__ void scan_values(double& a, uint64_t& b, V& s) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const double x = __shfl_up(a, o);
+        const uint64_t y = __shfl_up(b, o);
+        if (lane >= o) {
+            a += x;
+            b += y;
+        }
+    }
+    __syncthreads();
+    double* wa = (double*)s.wave64;
+    if (lane == 63) {
+        wa[wave] = a;
+        s.wave64[kWaves + wave] = b;
+    }
+    __syncthreads();
+    double pa = 0.;
+    for (int w = 0; w < wave; ++w) {
+        pa += wa[w];
+        b += s.wave64[kWaves + w];
+    }
+    a += pa;
+}
+
+// false (every thread): the row holds other values
+__device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Values& s) {
+    using R = Row<uint16_t>;
+    constexpr int U = R::U, AHEAD = R::AHEAD, E = Values::kEach;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t V = (uint32_t)a.vocab;
+    const uint16_t* at = (const uint16_t*)a.logits + n * a.row_stride;
+    const double T0 = a.temperatures != nullptr ? (double)a.temperatures[n] : a.temperature;
+    const int64_t k0 = a.top_ks != nullptr ? a.top_ks[n] : a.top_k;
+    const double p0 = a.top_ps != nullptr ? (double)a.top_ps[n] : a.top_p;
+    const double low0 = a.min_ps != nullptr ? (double)a.min_ps[n] : a.min_p;
+    const double u = (double)a.u[n];
+
+    // ---- A
+    for (int e = tid; e < Values::kCount; e += NT) s.count[e] = 0;
+    if (tid == 0) {
+        s.odd = 0;
+        s.first = Values::kCount;
+        s.border = -1;
+    }
+    __syncthreads();
+    bool odd = false;
+    for (uint64_t i0 = 0; i0 + (uint64_t)tid * U < V; i0 += (uint64_t)AHEAD * NT * U) {
+        train::Raw<uint16_t, U> raw[AHEAD];
+        int m[AHEAD];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            const uint64_t i = i0 + (uint64_t)(q * NT + tid) * U;
+            m[q] = i < V ? (V - i < U ? (int)(V - i) : U) : 0;
+            raw[q] = train::load_unit<uint16_t, U>(m[q] ? at + i : at, m[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+            for (int e = 0; e < U; ++e)
+                if (e < m[q]) {
+                    const int bin = Values::bin_of(raw[q].w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu);
+                    if (bin >= 0) atomicAdd(&s.count[bin], 1u);
+                    odd |= bin == -2;
+                }
+    }
+    if (odd) s.odd = 1;
+    __syncthreads();
+    if (s.odd) return false;
+    // the largest value
+    uint32_t c[E];
+    int first = Values::kCount;
+#pragma unroll
+    for (int e = E - 1; e >= 0; --e) {
+        c[e] = s.count[E * tid + e];
+        if (c[e] != 0) first = E * tid + e;
+    }
+    if (first < Values::kCount) atomicMin(&s.first, first);
+    __syncthreads();
+    first = s.first;
+    if (first == Values::kCount) {  // -Inf alone
+        if (tid == 0) {
+            a.token[n] = -1;
+            if (a.logp != nullptr) a.logp[n] = NAN;
+        }
+        return true;
+    }
+    const bool greedy = !(T0 > 0.) || k0 == 1 || low0 > 1.;
+    const double top = (double)Values::value_of(first), rate = greedy ? 0. : fmin(1.44269504088896340736 / T0, 1e300);
+    double w[E], mass = 0.;
+    uint64_t count = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        w[e] = c[e] != 0 ? power_of_two(((double)Values::value_of(E * tid + e) - top) * rate) : 0.;
+        s.weight[E * tid + e] = w[e];
+        mass += (double)c[e] * w[e];
+        count += c[e];
+    }
+    const double own_mass = mass;
+    const uint64_t own_count = count;
+    scan_values(mass, count, s);
+    const double mass0 = mass - own_mass;  // before this thread's values (the same sums in every pass over them)
+    const uint64_t count0 = count - own_count;
+    // top-k: the value that holds the k-th entry
+    const uint64_t k = greedy ? 1 : k0 > 0 && k0 < (int64_t)V ? (uint64_t)k0 : ~0ull;
+    auto find = [&](auto test) {  // the last value with entries that passes, and what lies before it
+        double m = mass0;
+        uint64_t t = count0;
+        int mine = -1;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (c[e] != 0 && test(m, t, w[e])) mine = e;
+            m += (double)c[e] * w[e];
+            t += c[e];
+        }
+        if (mine >= 0) atomicMax(&s.border, E * tid + mine);
+        __syncthreads();
+        if (s.border / E == tid) {
+            m = mass0;
+            t = count0;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (E * tid + e < s.border) {
+                    m += (double)c[e] * w[e];
+                    t += c[e];
+                }
+            s.mass = m;
+            s.before = (uint32_t)t;
+        }
+        __syncthreads();
+    };
+    find([&](double, uint64_t t, double) { return t < k; });
+    int border = s.border;
+    uint64_t quota = k - s.before < s.count[border] ? k - s.before : s.count[border];
+    if (p0 < 1. && !greedy) {
+        const double goal = p0 * (s.mass + (double)quota * s.weight[border]);
+        const int last = border;
+        __syncthreads();
+        if (tid == 0) s.border = -1;
+        __syncthreads();
+        find([&](double m, uint64_t t, double) { return m < goal || t == 0; });
+        if (s.border < last) {
+            border = s.border;
+            quota = s.count[border];
+        }
+        if (s.border <= last) {  // the entries i of it with mass + i w < goal
+            const double wb = s.weight[border], m = s.mass;
+            double q = ceil((goal - m) / wb);  // right to one entry: its rounding is 2^-52 of at most 2^31
+            if (!(m + (q - 1.) * wb < goal)) q -= 1.;
+            else if (m + q * wb < goal) q += 1.;
+            if (!(q >= 1.)) q = 1.;
+            if (q < (double)quota) quota = (uint64_t)q;
+        }
+    }
+    if (low0 > 0. && !greedy) {
+        const int last = border;
+        __syncthreads();
+        if (tid == 0) s.border = -1;
+        __syncthreads();
+        find([&](double, uint64_t t, double x) { return x >= low0 || t == 0; });
+        if (s.border < last) {
+            border = s.border;
+            quota = s.count[border];
+        }
+    }
+    __syncthreads();
+    // entries of the values before `border`, and the first `quota` of its own
+    const double wb = s.weight[border];
+    if (quota == s.count[border]) {
+        ++border;
+        quota = 0;
+    }
+
+    // ---- B
+    const uint64_t blocks = ((uint64_t)V + 64 * U - 1) / (64 * U);
+    const uint32_t reps = (uint32_t)((blocks + kRuns - 1) / kRuns);  // blocks of a run
+    const int runs = (int)((blocks + reps - 1) / reps);
+    auto load = [&](uint64_t block, int& m) {
+        const uint64_t i = (block * 64 + lane) * U;
+        m = i < V ? (V - i < U ? (int)(V - i) : U) : 0;
+        return train::load_unit<uint16_t, U>(m ? at + i : at, m);
+    };
+    auto bin_at = [&](const train::Raw<uint16_t, U>& raw, int e, int m) {
+        return e < m ? Values::bin_of(raw.w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu) : -1;
+    };
+    for (int r0 = wave; r0 < runs; r0 += AHEAD * kWaves) {
+        double sum[AHEAD] = {};
+        uint32_t ties[AHEAD] = {};
+        for (uint32_t b = 0; b < reps; ++b) {
+            train::Raw<uint16_t, U> raw[AHEAD];
+            int m[AHEAD];
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                const int r = r0 + q * kWaves;
+                raw[q] = load(r < runs ? (uint64_t)r * reps + b : blocks, m[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+                for (int e = 0; e < U; ++e) {
+                    const int bin = bin_at(raw[q], e, m[q]);
+                    if (bin >= 0 && bin < border) sum[q] += s.weight[bin];
+                    ties[q] += bin == border ? 1 : 0;
+                }
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                sum[q] += __shfl_xor(sum[q], o);
+                ties[q] += __shfl_xor(ties[q], o);
+            }
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q)
+            if (lane == 0 && r0 + q * kWaves < runs) {
+                s.runs[r0 + q * kWaves] = sum[q];
+                s.ties[r0 + q * kWaves] = ties[q];
+            }
+    }
+    __syncthreads();
+    if (wave != 0) return true;
+    // sums before each run: 16 consecutive ones a lane; a run's ties count while the quota lasts
+    constexpr int EACH = kRuns / 64;
+    uint32_t tied = 0;
+    for (int e = 0; e < EACH; ++e) tied += lane * EACH + e < runs ? s.ties[lane * EACH + e] : 0;
+    uint64_t ties0 = tied;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint64_t x = __shfl_up(ties0, o);
+        if (lane >= o) ties0 += x;
+    }
+    ties0 -= tied;
+    auto of_run = [&](int r, uint64_t& t) {
+        const uint64_t left = t < quota ? quota - t : 0, here = s.ties[r];
+        t += here;
+        return s.runs[r] + (double)(left < here ? left : here) * wb;
+    };
+    double part = 0.;
+    uint64_t t = ties0;
+    for (int e = 0; e < EACH; ++e)
+        if (lane * EACH + e < runs) part += of_run(lane * EACH + e, t);
+    double upto_lane = part;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const double x = __shfl_up(upto_lane, o);
+        if (lane >= o) upto_lane += x;
+    }
+    const double whole = __shfl(upto_lane, 63), goal = u * whole;
+    double run = __shfl_up(upto_lane, 1), base = 0.;
+    if (lane == 0) run = 0.;
+    int chosen = runs, positive = -1;
+    double at_first = 0.;
+    uint64_t ties_first = 0, ties_last = 0;
+    t = ties0;
+    for (int e = 0; e < EACH; ++e) {
+        const int r = lane * EACH + e;
+        if (r >= runs) break;
+        const uint64_t before = t;
+        const double x = of_run(r, t);
+        if (x > 0.) {
+            positive = r;
+            ties_last = before;
+            if (chosen == runs && run + x > goal) {
+                chosen = r;
+                at_first = run;
+                ties_first = before;
+            }
+        }
+        run += x;
+    }
+    int best = chosen, end_run = positive;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_xor(best, o), y = __shfl_xor(end_run, o);
+        best = x < best ? x : best;
+        end_run = y > end_run ? y : end_run;
+    }
+    const bool over = best == runs;  // u times the whole is not below it: the last entry of weight
+    const uint64_t owner = __ballot(over ? positive == end_run : chosen == best);
+    const int who = __ffsll((unsigned long long)owner) - 1;
+    base = __shfl(at_first, who);
+    uint64_t seen = __shfl(over ? ties_last : ties_first, who);
+    if (over) best = end_run;
+    int64_t token = -1;
+    double weight_of = 0.;
+    for (uint32_t b = 0; b < reps; ++b) {
+        int m;
+        const uint64_t block = (uint64_t)best * reps + b;
+        const train::Raw<uint16_t, U> raw = load(block, m);
+        uint32_t own = 0;
+#pragma unroll
+        for (int e = 0; e < U; ++e) own += bin_at(raw, e, m) == border ? 1 : 0;
+        uint32_t upto_ties = own;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t x = __shfl_up(upto_ties, o);
+            if (lane >= o) upto_ties += x;
+        }
+        uint64_t rank = seen + upto_ties - own;
+        double x[U], sum = 0.;
+#pragma unroll
+        for (int e = 0; e < U; ++e) {
+            const int bin = bin_at(raw, e, m);
+            x[e] = bin >= 0 && bin < border ? s.weight[bin] : bin == border && rank < quota ? wb : 0.;
+            rank += bin == border ? 1 : 0;
+            sum += x[e];
+        }
+        seen += __shfl(upto_ties, 63);
+        double upto = sum;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const double y = __shfl_up(upto, o);
+            if (lane >= o) upto += y;
+        }
+        const double end = __shfl(upto, 63);
+        double run2 = base + (upto - sum);
+        int mine = -1, final_ = -1;
+        double wm = 0., wf = 0.;
+#pragma unroll
+        for (int e = 0; e < U; ++e) {
+            run2 += x[e];
+            if (x[e] > 0.) {
+                final_ = e;
+                wf = x[e];
+                if (mine < 0 && run2 > goal) {
+                    mine = e;
+                    wm = x[e];
+                }
+            }
+        }
+        const uint64_t hit = over ? 0 : __ballot(mine >= 0), some = __ballot(final_ >= 0);
+        if (hit != 0) {
+            const int l = __ffsll((unsigned long long)hit) - 1;
+            token = (int64_t)((block * 64 + l) * U) + __shfl(mine, l);
+            weight_of = __shfl(wm, l);
+            break;
+        }
+        if (some != 0) {  // where no entry exceeds the goal, the last one
+            const int l = 63 - __clzll((long long)some);
+            token = (int64_t)((block * 64 + l) * U) + __shfl(final_, l);
+            weight_of = __shfl(wf, l);
+        }
+        base += end;
+    }
+    if (lane == 0) {
+        a.token[n] = token;
+        if (a.logp != nullptr) a.logp[n] = (float)log(weight_of / whole);
+    }
+    return true;
+}
+
+template <typename T>
+__global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
+    const int64_t n = train::block_id();
+    if (n >= a.rows) return;
+    if constexpr (sizeof(T) == 2) {
+        __shared__ union {
+            Values v;
+            Shared s;
+        } m;
+        if (sample_values(a, n, m.v)) return;
+        __syncthreads();
+        sample_row<T>(a, n, m.s);
+    } else {
+        __shared__ Shared s;
+        sample_row<T>(a, n, s);
     }
 }
 
