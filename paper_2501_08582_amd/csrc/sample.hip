@@ -540,8 +540,9 @@ struct Values {
     static constexpr int kZero = kSpan, kEach = (2 * kSpan + NT) / NT, kCount = kEach * NT;
     double weight[kCount];
     uint32_t count[kCount];
-    double runs[kRuns];
-    uint32_t ties[kRuns];
+    double runs[kRuns + kRuns / 16];  // run r at r + r / 16: 16 consecutive ones a lane, on other banks
+    uint32_t ties[kRuns + kRuns / 16];
+    static __device__ __forceinline__ int place(int r) { return r + (r >> 4); }
     uint64_t wave64[2 * kWaves];
     double mass;
     uint32_t before;
@@ -552,6 +553,17 @@ struct Values {
         if (d < (uint32_t)kSpan) return (b & 0x8000u) ? kZero + 1 + (int)d : kZero - 1 - (int)d;
         return m == 0 ? kZero : b == 0xFF80u ? -1 : -2;
     }
+    // The same of two logits, 16 bits each, where both lie in the span; false otherwise.  Packed
+    // 16-bit integers: four instructions an entry, of which the passes over a row consist.
+    typedef short two __attribute__((ext_vector_type(2)));
+    typedef unsigned short utwo __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ bool bins_of(uint32_t b, uint32_t& bins) {
+        const utwo m = __builtin_bit_cast(utwo, b & 0x7FFF7FFFu), d = m - (utwo)(unsigned short)kLeast;
+        const two neg = __builtin_bit_cast(two, b) >> (two)15;  // -1 for negative ones
+        const two t = __builtin_bit_cast(two, d) ^ ~neg;        // ~d or d: kZero - 1 - d, kZero + 1 + d
+        bins = __builtin_bit_cast(uint32_t, t - neg + (two)(short)kZero);
+        return d[0] < kSpan && d[1] < kSpan;
+    }
     static __device__ __forceinline__ float value_of(int bin) {
         const uint32_t m = bin == kZero ? 0u : bin < kZero ? (uint32_t)(kLeast + kZero - 1 - bin) : 0x8000u | (uint32_t)(kLeast + bin - kZero - 1);
         return bf16_bits_to_f32(m);
@@ -559,6 +571,7 @@ struct Values {
 };
 static_assert(Values::kCount > 2 * Values::kSpan, "every value has a bin");
 static_assert(sizeof(Values) <= 160 * 1024, "LDS");
+static_assert(train::kUnit<uint16_t> == 8, "sums of a unit");
 
 template <class V>
 __device__ __forceinline__ void scan_values(double& a, uint64_t& b, V& s) {
@@ -587,10 +600,36 @@ __device__ __forceinline__ void scan_values(double& a, uint64_t& b, V& s) {
     a += pa;
 }
 
+// Sums over a wave's lanes of four values at a time: lane l gets that of value l / 16.  Seven
+// exchanges, of which four stay in rows of 16 lanes, against 24 one by one.
+template <typename A>
+__device__ __forceinline__ A other_lane(A v, int ctrl_step) {  // 0 .. 3: the rows' butterfly
+    uint32_t w[sizeof(A) / 4];
+    __builtin_memcpy(w, &v, sizeof(A));
+#pragma unroll
+    for (uint32_t& x : w)
+        x = (uint32_t)(ctrl_step == 0   ? __builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true)
+                       : ctrl_step == 1 ? __builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true)
+                       : ctrl_step == 2 ? __builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true)
+                                        : __builtin_amdgcn_mov_dpp((int)x, 0x140, 0xF, 0xF, true));
+    __builtin_memcpy(&v, w, sizeof(A));
+    return v;
+}
+template <typename A>
+__device__ __forceinline__ A sum_of_four(const A (&v)[4]) {
+    const bool upper = threadIdx.x & 32, odd = threadIdx.x & 16;
+    A x = (upper ? v[2] : v[0]) + __shfl_xor(upper ? v[0] : v[2], 32);
+    A y = (upper ? v[3] : v[1]) + __shfl_xor(upper ? v[1] : v[3], 32);
+    A z = (odd ? y : x) + __shfl_xor(odd ? x : y, 16);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) z += other_lane(z, k);
+    return z;
+}
+
 // false (every thread): the row holds other values
 __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Values& s) {
     using R = Row<uint16_t>;
-    constexpr int U = R::U, AHEAD = R::AHEAD, E = Values::kEach;
+    constexpr int U = R::U, AHEAD = 8, E = Values::kEach;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t V = (uint32_t)a.vocab;
     const uint16_t* at = (const uint16_t*)a.logits + n * a.row_stride;
@@ -600,6 +639,10 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
     const double low0 = a.min_ps != nullptr ? (double)a.min_ps[n] : a.min_p;
     const double u = (double)a.u[n];
 
+    auto bits_at = [](const train::Raw<uint16_t, U>& raw, int e) {  // (e need not be known: no indexing of registers)
+        const uint32_t lo = e & 2 ? raw.w[1] : raw.w[0], hi = e & 2 ? raw.w[3] : raw.w[2];
+        return (e & 4 ? hi : lo) >> (16 * (e & 1)) & 0xFFFFu;
+    };
     // ---- A
     for (int e = tid; e < Values::kCount; e += NT) s.count[e] = 0;
     if (tid == 0) {
@@ -619,14 +662,25 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
             raw[q] = train::load_unit<uint16_t, U>(m[q] ? at + i : at, m[q]);
         }
 #pragma unroll
-        for (int q = 0; q < AHEAD; ++q)
+        for (int q = 0; q < AHEAD; ++q) {
+            uint32_t bins[U / 2];
+            bool plain = m[q] == U;
 #pragma unroll
-            for (int e = 0; e < U; ++e)
-                if (e < m[q]) {
-                    const int bin = Values::bin_of(raw[q].w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu);
+            for (int e = 0; e < U / 2; ++e) plain &= Values::bins_of(raw[q].w[e], bins[e]);
+            if (plain) {
+#pragma unroll
+                for (int e = 0; e < U / 2; ++e) {
+                    atomicAdd(&s.count[bins[e] & 0xFFFFu], 1u);
+                    atomicAdd(&s.count[bins[e] >> 16], 1u);
+                }
+            } else {
+                for (int e = 0; e < m[q]; ++e) {
+                    const int bin = Values::bin_of(bits_at(raw[q], e));
                     if (bin >= 0) atomicAdd(&s.count[bin], 1u);
                     odd |= bin == -2;
                 }
+            }
+        }
     }
     if (odd) s.odd = 1;
     __syncthreads();
@@ -734,6 +788,12 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
         ++border;
         quota = 0;
     }
+    // what is not kept weighs nothing, so that pass B asks no questions
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (E * tid + e >= border) s.weight[E * tid + e] = 0.;
+    __syncthreads();
 
     // ---- B
     const uint64_t blocks = ((uint64_t)V + 64 * U - 1) / (64 * U);
@@ -744,49 +804,61 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
         m = i < V ? (V - i < U ? (int)(V - i) : U) : 0;
         return train::load_unit<uint16_t, U>(m ? at + i : at, m);
     };
-    auto bin_at = [&](const train::Raw<uint16_t, U>& raw, int e, int m) {
-        return e < m ? Values::bin_of(raw.w[e >> 1] >> (16 * (e & 1)) & 0xFFFFu) : -1;
-    };
-    for (int r0 = wave; r0 < runs; r0 += AHEAD * kWaves) {
-        double sum[AHEAD] = {};
-        uint32_t ties[AHEAD] = {};
+    auto bin_at = [&](const train::Raw<uint16_t, U>& raw, int e, int m) { return e < m ? Values::bin_of(bits_at(raw, e)) : -1; };
+    constexpr int BEHIND = 4;  // runs of a wave at a time (sum_of_four)
+    for (int r0 = wave; r0 < runs; r0 += BEHIND * kWaves) {
+        double sum[BEHIND] = {};
+        uint32_t ties[BEHIND] = {};
         for (uint32_t b = 0; b < reps; ++b) {
-            train::Raw<uint16_t, U> raw[AHEAD];
-            int m[AHEAD];
+            train::Raw<uint16_t, U> raw[BEHIND];
+            int m[BEHIND];
 #pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
+            for (int q = 0; q < BEHIND; ++q) {
                 const int r = r0 + q * kWaves;
                 raw[q] = load(r < runs ? (uint64_t)r * reps + b : blocks, m[q]);
             }
 #pragma unroll
-            for (int q = 0; q < AHEAD; ++q)
+            for (int q = 0; q < BEHIND; ++q) {
+                uint32_t bins[U / 2];
+                bool plain = m[q] == U;
 #pragma unroll
-                for (int e = 0; e < U; ++e) {
-                    const int bin = bin_at(raw[q], e, m[q]);
-                    if (bin >= 0 && bin < border) sum[q] += s.weight[bin];
-                    ties[q] += bin == border ? 1 : 0;
+                for (int e = 0; e < U / 2; ++e) plain &= Values::bins_of(raw[q].w[e], bins[e]);
+                if (plain) {
+                    // most entries lie behind the border: a unit of those alone is left out
+                    Values::utwo least = __builtin_bit_cast(Values::utwo, bins[0]);
+#pragma unroll
+                    for (int e = 1; e < U / 2; ++e) least = __builtin_elementwise_min(least, __builtin_bit_cast(Values::utwo, bins[e]));
+                    if (least[0] > border && least[1] > border) continue;
+                    double x[U];
+#pragma unroll
+                    for (int e = 0; e < U; ++e) x[e] = s.weight[bins[e >> 1] >> (16 * (e & 1)) & 0xFFFFu];
+                    sum[q] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+                    if (quota != 0)
+#pragma unroll
+                        for (int e = 0; e < U; ++e) ties[q] += (int)(bins[e >> 1] >> (16 * (e & 1)) & 0xFFFFu) == border ? 1 : 0;
+                } else {
+                    for (int e = 0; e < m[q]; ++e) {
+                        const int bin = Values::bin_of(bits_at(raw[q], e));
+                        if (bin >= 0) sum[q] += s.weight[bin];
+                        ties[q] += bin == border ? 1 : 0;
+                    }
                 }
+            }
         }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1)
-#pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
-                sum[q] += __shfl_xor(sum[q], o);
-                ties[q] += __shfl_xor(ties[q], o);
-            }
-#pragma unroll
-        for (int q = 0; q < AHEAD; ++q)
-            if (lane == 0 && r0 + q * kWaves < runs) {
-                s.runs[r0 + q * kWaves] = sum[q];
-                s.ties[r0 + q * kWaves] = ties[q];
-            }
+        const int mine = r0 + (lane >> 4) * kWaves;
+        const double all = sum_of_four(sum);
+        const uint32_t tied = quota != 0 ? sum_of_four(ties) : 0;
+        if ((lane & 15) == 0 && mine < runs) {
+            s.runs[Values::place(mine)] = all;
+            s.ties[Values::place(mine)] = tied;
+        }
     }
     __syncthreads();
     if (wave != 0) return true;
     // sums before each run: 16 consecutive ones a lane; a run's ties count while the quota lasts
     constexpr int EACH = kRuns / 64;
     uint32_t tied = 0;
-    for (int e = 0; e < EACH; ++e) tied += lane * EACH + e < runs ? s.ties[lane * EACH + e] : 0;
+    for (int e = 0; e < EACH; ++e) tied += lane * EACH + e < runs ? s.ties[Values::place(lane * EACH + e)] : 0;
     uint64_t ties0 = tied;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -795,9 +867,9 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
     }
     ties0 -= tied;
     auto of_run = [&](int r, uint64_t& t) {
-        const uint64_t left = t < quota ? quota - t : 0, here = s.ties[r];
+        const uint64_t left = t < quota ? quota - t : 0, here = s.ties[Values::place(r)];
         t += here;
-        return s.runs[r] + (double)(left < here ? left : here) * wb;
+        return s.runs[Values::place(r)] + (double)(left < here ? left : here) * wb;
     };
     double part = 0.;
     uint64_t t = ties0;
