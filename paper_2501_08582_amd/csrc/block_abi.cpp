@@ -265,7 +265,7 @@ size_t lors_orthogonal_workspace_bytes(const lors_update_t* p, const lors_update
     if (check_update(p, items, count) != LORS_OK) return static_cast<size_t>(-1);
     int64_t need = 0;
     for (int64_t i = 0; i < count; ++i) need += scratch_of(items[i]);
-    return static_cast<size_t>(need);
+    return static_cast<size_t>(need + lors::block::update_table(count));
 }
 
 lors_status_t lors_orthogonal_update(const lors_update_t* p, const lors_update_item_t* items, int64_t count,
@@ -295,6 +295,8 @@ lors_status_t lors_orthogonal_update(const lors_update_t* p, const lors_update_i
                                           q.rows <= q.cols ? 1 : 0};
         need += scratch_of(q);
     }
+    const int64_t table = lors::block::update_table(count), at = need;
+    need += table;
     if (check_alignment({{workspace, 0, 16}}) != LORS_OK) return LORS_ERR_ALIGN;
     span(workspace, need, true);
     if (any_overlap(spans.get(), n)) return LORS_ERR_ALIAS;
@@ -310,7 +312,8 @@ lors_status_t lors_orthogonal_update(const lors_update_t* p, const lors_update_i
                                     p->grad_dtype == LORS_DTYPE_BF16,
                                     p->param_dtype == LORS_DTYPE_BF16,
                                     static_cast<uint8_t*>(workspace)};
-    return from_hip(lors::block::launch_update(a, matrices.get(), count, static_cast<hipStream_t>(stream)));
+    return from_hip(lors::block::launch_update(a, matrices.get(), count, table ? a.workspace + at : nullptr,
+                                               static_cast<hipStream_t>(stream)));
 }
 
 static lors_status_t check_sample(const lors_sample_t* p) {

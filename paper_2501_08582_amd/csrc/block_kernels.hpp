@@ -34,7 +34,9 @@ struct UpdateArgs {
 
 // Bytes of a matrix's scratch (a multiple of 256).
 int64_t update_scratch(int64_t d, int64_t n);
-hipError_t launch_update(const UpdateArgs& a, const Matrix* matrices, int64_t count, hipStream_t s);
+// Bytes of the descriptors of many matrices, in the workspace behind their scratch.
+int64_t update_table(int64_t count);
+hipError_t launch_update(const UpdateArgs& a, const Matrix* matrices, int64_t count, void* table, hipStream_t s);
 
 struct SampleArgs {
     int64_t rows, vocab, row_stride;

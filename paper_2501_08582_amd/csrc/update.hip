@@ -22,6 +22,8 @@
 //
 // Bound by HBM for many matrices: 10 bytes an element in the first pass (bf16 gradient), 16
 // in the second.  One matrix alone is bound by the steps' chain of products.
+#include <type_traits>
+
 #include "block_kernels.hpp"
 #include "train_common.hpp"
 
@@ -32,19 +34,31 @@ namespace {
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 constexpr int NT = 256;
-constexpr int kBatch = 48;        // matrices of a launch: their descriptors are kernel arguments
-constexpr int kPiece = 512;       // least columns (along the long side) of a workgroup
+constexpr int kBatch = 48;        // matrices whose descriptors are kernel arguments
+constexpr int kPiece = 256;       // least columns (along the long side) of a workgroup
 constexpr int kMostPieces = 256;
 
 struct Batch {
     int count;
-    int first[kBatch + 1];  // first workgroup of each matrix
+    int first[kBatch];  // first workgroup of each matrix
     Matrix m[kBatch];
+};
+
+// The matrices of a launch: a batch, or more of them in the workspace (table_kernel).
+struct Table {
+    int* first;
+    Matrix* m;
+};
+struct Source {
+    Table table;
+    int count;
+    bool many;
+    Batch batch;
 };
 
 __host__ __device__ inline int64_t piece_cols(int64_t n) {
     const int64_t most = (n + kMostPieces - 1) / kMostPieces;
-    const int64_t c = (most + 127) / 128 * 128;
+    const int64_t c = (most + 255) / 256 * 256;  // turns of 64 columns of four waves
     return c < kPiece ? kPiece : c;
 }
 __host__ __device__ inline int64_t pieces_of(int64_t n) { return (n + piece_cols(n) - 1) / piece_cols(n); }
@@ -54,11 +68,32 @@ __device__ __forceinline__ f64x4 mfma64(double a, double b, f64x4 c) {
     return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0);
 }
 
+// Pointers out of a descriptor: the compiler is told that they are to global memory (it
+// would use flat accesses, which wait for LDS operations too).
+#ifdef __HIP_DEVICE_COMPILE__
+#define LORS_GLOBAL __attribute__((address_space(1)))
+#else
+#define LORS_GLOBAL
+#endif
+template <typename T>
+using Global = LORS_GLOBAL T*;
+
+// Where a run of elements starts: FULL ones at an element that the whole wave shares and 32 bits
+// of a lane's own (one register for all runs of a turn), others anywhere.
+struct Place {
+    int64_t base;
+    uint32_t lane;
+};
+template <typename T>
+__device__ __forceinline__ Global<T> at_place(T* p, const Place& at) {
+    return (Global<T>)((LORS_GLOBAL char*)(Global<T>)(p + at.base) + (uint64_t)(at.lane * (uint32_t)sizeof(T)));
+}
+
 // The first n of N elements at p as fp32, the others 0.
 template <typename T, int N>
-__device__ __forceinline__ void read_some(const T* p, int n, float (&f)[N]) {
+__device__ __forceinline__ void read_some(Global<const T> p, int n, float (&f)[N]) {
     if (n >= N) {
-        const train::Packed<T, N> v = *(const train::Packed<T, N>*)p;
+        const train::Packed<T, N> v = *(Global<const train::Packed<T, N>>)p;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             if constexpr (sizeof(T) == 2) f[e] = bf16_bits_to_f32(v.v[e]);
@@ -76,7 +111,7 @@ __device__ __forceinline__ void read_some(const T* p, int n, float (&f)[N]) {
     }
 }
 template <typename T, int N>
-__device__ __forceinline__ void write_some(T* p, int n, const float (&f)[N]) {
+__device__ __forceinline__ void write_some(Global<T> p, int n, const float (&f)[N]) {
     train::Packed<T, N> v;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
@@ -84,7 +119,7 @@ __device__ __forceinline__ void write_some(T* p, int n, const float (&f)[N]) {
         else v.v[e] = f[e];
     }
     if (n >= N) {
-        *(train::Packed<T, N>*)p = v;
+        *(Global<train::Packed<T, N>>)p = v;
         return;
     }
 #pragma unroll
@@ -94,119 +129,189 @@ __device__ __forceinline__ void write_some(T* p, int n, const float (&f)[N]) {
 
 __device__ __forceinline__ int most(int64_t left, int n) { return left >= n ? n : left > 0 ? (int)left : 0; }
 
-// Matrix of this workgroup.
-__device__ __forceinline__ int find(const Batch& b, int block) {
-    int lo = 0, hi = b.count - 1;
+// Matrix of this workgroup, and the workgroup's number in it.
+__device__ __forceinline__ int find(const int* first, int count, int block) {
+    int lo = 0, hi = count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (b.first[mid] <= block) lo = mid;
+        if (first[mid] <= block) lo = mid;
         else hi = mid - 1;
     }
     return lo;
 }
+// A workgroup's descriptor, which all lanes load alike, into scalar registers.
+__device__ __forceinline__ Matrix uniform(const Matrix& x) {
+    uint32_t w[sizeof(Matrix) / 4];
+    __builtin_memcpy(w, &x, sizeof(Matrix));
+#pragma unroll
+    for (uint32_t& e : w) e = __builtin_amdgcn_readfirstlane(e);
+    Matrix out;
+    __builtin_memcpy(&out, w, sizeof(Matrix));
+    return out;
+}
+__device__ __forceinline__ Matrix matrix_of(const Source& s, int block, int& piece) {
+    if (s.many) {
+        const int i = find(s.table.first, s.count, block);
+        piece = __builtin_amdgcn_readfirstlane(block - s.table.first[i]);
+        return uniform(s.table.m[i]);
+    }
+    const int i = find(s.batch.first, s.count, block);
+    piece = block - s.batch.first[i];
+    return s.batch.m[i];
+}
+__device__ __forceinline__ Matrix matrix_at(const Source& s, int i) { return uniform(s.many ? s.table.m[i] : s.batch.m[i]); }
+
+__global__ __launch_bounds__(64) void table_kernel(Batch b, int at, Table t) {
+    const int i = threadIdx.x;
+    if (i >= b.count) return;
+    t.first[at + i] = b.first[i];
+    t.m[at + i] = b.m[i];
+}
 
 struct Rule {
     float beta, fresh;
-    int nesterov;
+    int nesterov, grad_bf16, param_bf16;
     // m <- beta m + fresh g, and v.  The second pass forms v from the m that the first
     // one stored, by the same operations: the same bits.
     __device__ __forceinline__ float moment(float m, float g) const { return fmaf(beta, m, fresh * g); }
     __device__ __forceinline__ float direction(float m, float g) const { return nesterov ? fmaf(beta, m, fresh * g) : m; }
 };
 
-// DT: 16-row blocks of the short side.  Short index i of row p of block t: 16 t + p of a
-// wide matrix, DT p + t of a tall one (consecutive in memory over t).  The steps
-// work on rows in the order (t, p) whatever that is.
+// DT: 16-row blocks of the short side.  Row p = 4c + h of block t is the short index i = 16 t + p of a
+// wide matrix and 4 DT h + DT c + t of a tall one: there a lane of the second pass (h its
+// row of 16 lanes) holds 4 DT consecutive elements, one of the first pass DT.  The
+// steps work on rows in the order (t, p), whatever that is.
 template <int DT>
 constexpr int kTiles = DT * (DT + 1) / 2;
+// Columns of a lane in a turn of the first pass (the widest short side has registers for four).
+template <int DT>
+constexpr int kEach = DT == 8 ? 4 : 8;
 
-// v of 32 columns from j0 on: lane l holds, of row l % 16 of every block, the columns
-// 8 (l / 16) + e (wide) or 4 e + l / 16 (tall); any assignment does that is the same
-// for every row.
-template <typename T, int DT, bool WIDE>
-__device__ __forceinline__ void gram_piece(const Matrix& x, const Rule& rule, int64_t j0, int64_t j1, f64x4 (&acc)[kTiles<DT>]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = lane & 15, h = lane >> 4;
-    const T* grad = (const T*)x.grad;
-    for (int64_t jb = j0 + 32 * wave; jb < j1; jb += 32 * (NT / 64)) {
-        float g[DT][8], m[DT][8];
-        if constexpr (WIDE) {
-            const int64_t j = jb + 8 * h;
+// FULL: the turn's columns exist and rows are read in whole vectors (read_whole): every
+// lane loads, from the last row that exists where its own does not, and takes 0 instead.
+// Without branches around them all loads of a turn are in flight together.
+template <typename T, int N>
+__device__ __forceinline__ void read_whole(Global<const T> p, bool some, float (&f)[N]) {
+    const train::Packed<T, N> v = *(Global<const train::Packed<T, N>>)p;
+    if constexpr (sizeof(T) * N == 2) {
+        // (else the load writes the upper half of a register, and waits for what it held)
+        uint32_t w = v.v[0];
+        asm("" : "+v"(w));
+        f[0] = some ? bf16_bits_to_f32(w) : 0.f;
+        return;
+    }
 #pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                const int i = 16 * t + p, n = i < x.d ? most(j1 - j, 8) : 0;
-                read_some<T, 8>(grad + (n ? (int64_t)i * x.n + j : 0), n, g[t]);
-                if (x.m != nullptr) read_some<float, 8>(x.m + (n ? (int64_t)i * x.n + j : 0), n, m[t]);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int64_t j = jb + 4 * e + h;
-                const int n = j < j1 ? most(x.d - DT * p, DT) : 0;
-                float a[DT], b[DT];
-                read_some<T, DT>(grad + (n ? j * x.d + DT * p : 0), n, a);
-                if (x.m != nullptr) read_some<float, DT>(x.m + (n ? j * x.d + DT * p : 0), n, b);
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    g[t][e] = a[t];
-                    m[t][e] = x.m != nullptr ? b[t] : 0.f;
-                }
-            }
-        }
-        if (x.m != nullptr) {
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) m[t][e] = rule.moment(m[t][e], g[t][e]);
-            if constexpr (WIDE) {
-                const int64_t j = jb + 8 * h;
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    const int i = 16 * t + p, n = i < x.d ? most(j1 - j, 8) : 0;
-                    if (n) write_some<float, 8>(x.m + (int64_t)i * x.n + j, n, m[t]);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int64_t j = jb + 4 * e + h;
-                    const int n = j < j1 ? most(x.d - DT * p, DT) : 0;
-                    float b[DT];
-#pragma unroll
-                    for (int t = 0; t < DT; ++t) b[t] = m[t][e];
-                    if (n) write_some<float, DT>(x.m + j * x.d + DT * p, n, b);
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[t][e] = rule.direction(m[t][e], g[t][e]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            double v[DT];
-#pragma unroll
-            for (int t = 0; t < DT; ++t) v[t] = (double)g[t][e];
-            int k = 0;
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int u = t; u < DT; ++u, ++k) acc[k] = mfma64(v[t], v[u], acc[k]);
-        }
+    for (int e = 0; e < N; ++e) {
+        if constexpr (sizeof(T) == 2) f[e] = some ? bf16_bits_to_f32(v.v[e]) : 0.f;
+        else f[e] = some ? v.v[e] : 0.f;
+    }
+}
+// The gradient's, of either type.
+template <int N, bool FULL>
+__device__ __forceinline__ void read_grad(const void* p, bool bf16, const Place& at, int n, float (&f)[N]) {
+    if (bf16) {
+        if constexpr (FULL) read_whole<uint16_t, N>(at_place((const uint16_t*)p, at), n > 0, f);
+        else read_some<uint16_t, N>(at_place((const uint16_t*)p, at), n, f);
+    } else {
+        if constexpr (FULL) read_whole<float, N>(at_place((const float*)p, at), n > 0, f);
+        else read_some<float, N>(at_place((const float*)p, at), n, f);
     }
 }
 
-template <typename T, int DT>
-__global__ __launch_bounds__(NT, DT == 8 ? 1 : 2) void gram_kernel(Batch batch, Rule rule, uint8_t* __restrict__ ws) {
+template <int DT, bool WIDE, bool FULL>
+__device__ __forceinline__ void gram_turn(const Matrix& x, const Rule& rule, int64_t jb, int64_t j1, f64x4 (&acc)[kTiles<DT>]) {
+    const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 4;
+    // run k of a lane: where it starts and how many of its elements exist
+    constexpr int N = kEach<DT>, K = WIDE ? DT : N, E = WIDE ? N : DT;
+    auto run = [&](int k, int& n) -> Place {
+        if constexpr (WIDE) {  // k: block; N columns
+            const int i = 16 * k + p;
+            const int64_t j = jb + N * h;
+            n = i < x.d ? (FULL ? N : most(j1 - j, N)) : 0;
+            if (FULL) return {(16 * k < x.d ? 16 * k * x.n : 0) + jb, (i < x.d ? (uint32_t)(p * x.n) : 0u) + N * h};
+            return {n ? (int64_t)i * x.n + j : 0, 0};
+        } else {  // k: column; DT rows
+            const int64_t j = jb + 4 * k + h;
+            const int i = 4 * DT * (p & 3) + DT * (p >> 2);
+            n = FULL ? (i < x.d ? DT : 0) : j < j1 ? most(x.d - i, DT) : 0;
+            if (FULL) return {(jb + 4 * k) * x.d, (uint32_t)(h * x.d + (i < x.d ? i : 0))};
+            return {n ? j * x.d + i : 0, 0};
+        }
+    };
+    // (the branches on what a matrix has stand around whole loops of loads, not inside)
+    float g[K][E];
+    auto gradients = [&](bool bf16) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            int n;
+            const Place at = run(k, n);
+            read_grad<E, FULL>(x.grad, bf16, at, n, g[k]);
+        }
+    };
+    if (rule.grad_bf16) gradients(true);
+    else gradients(false);
+    if (x.m != nullptr) {
+        float m[K][E];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            int n;
+            const Place at = run(k, n);
+            if constexpr (FULL) read_whole<float, E>(at_place(x.m, at), n > 0, m[k]);
+            else read_some<float, E>(at_place(x.m, at), n, m[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                m[k][e] = rule.moment(m[k][e], g[k][e]);
+                g[k][e] = rule.direction(m[k][e], g[k][e]);
+            }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            int n;
+            const Place at = run(k, n);
+            if (n > 0) write_some<float, E>(at_place(x.m, at), FULL ? E : n, m[k]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        double v[DT];
+#pragma unroll
+        for (int t = 0; t < DT; ++t) v[t] = (double)g[WIDE ? t : e][WIDE ? e : t];
+        int k = 0;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int u = t; u < DT; ++u, ++k) acc[k] = mfma64(v[t], v[u], acc[k]);
+    }
+}
+
+// v of 4 N columns a turn: lane l holds, of row l % 16 of every block, the columns N (l / 16) + e
+// (wide) or 4 e + l / 16 (tall); any assignment does that is the same for every row.
+template <int DT, bool WIDE>
+__device__ __forceinline__ void gram_piece(const Matrix& x, const Rule& rule, int64_t j0, int64_t j1, f64x4 (&acc)[kTiles<DT>]) {
+    const bool whole = WIDE ? x.n < (int64_t)1 << 26 : x.d % DT == 0;  // (a lane's own offset fits 32 bits)
+    constexpr int C = 4 * kEach<DT>;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll 1
+    for (int64_t jb = j0 + C * wave; jb < j1; jb += C * (NT / 64)) {
+        if (whole && jb + C <= j1) gram_turn<DT, WIDE, true>(x, rule, jb, j1, acc);
+        else gram_turn<DT, WIDE, false>(x, rule, jb, j1, acc);
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(NT, DT == 8 ? 1 : 2) void gram_kernel(Source src, Rule rule, uint8_t* __restrict__ ws) {
     constexpr int G = kTiles<DT> < 8 ? kTiles<DT> : 8;  // tiles joined at a time
     __shared__ double red[NT / 64][G][256];
-    const int item = find(batch, (int)blockIdx.x);
-    const Matrix x = batch.m[item];
-    const int piece = (int)blockIdx.x - batch.first[item];
+    int piece;
+    const Matrix x = matrix_of(src, (int)blockIdx.x, piece);
     const int64_t cols = piece_cols(x.n), j0 = piece * cols, j1 = j0 + cols < x.n ? j0 + cols : x.n;
     f64x4 acc[kTiles<DT>];
 #pragma unroll
     for (int k = 0; k < kTiles<DT>; ++k) acc[k] = f64x4{0., 0., 0., 0.};
-    if (x.wide) gram_piece<T, DT, true>(x, rule, j0, j1, acc);
-    else gram_piece<T, DT, false>(x, rule, j0, j1, acc);
+    if (x.wide) gram_piece<DT, true>(x, rule, j0, j1, acc);
+    else gram_piece<DT, false>(x, rule, j0, j1, acc);
     // the waves' sums, in wave order
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     double* out = (double*)(ws + x.scratch) + (int64_t)piece * (kTiles<DT> * 256);
@@ -230,6 +335,19 @@ __global__ __launch_bounds__(NT, DT == 8 ? 1 : 2) void gram_kernel(Batch batch, 
     }
 }
 
+// The pieces' sum, in their order, into the first piece's place: one entry a thread.
+__global__ __launch_bounds__(NT) void sum_kernel(Source src, int entries, uint8_t* __restrict__ ws) {
+    const Matrix x = matrix_at(src, (int)blockIdx.y);
+    const int e = blockIdx.x * NT + threadIdx.x;
+    double* part = (double*)(ws + x.scratch) + e;
+    const int64_t pieces = pieces_of(x.n);
+    if (pieces == 1) return;
+    double s = 0.;
+#pragma unroll 16
+    for (int64_t q = 0; q < pieces; ++q) s += part[q * entries];
+    part[0] = s;
+}
+
 // ---------------------------------------------------------------------------
 // the steps: wave w holds the columns 16 w .. of every matrix
 // ---------------------------------------------------------------------------
@@ -243,17 +361,26 @@ struct Square {
 // part must not be transposed from step to step: it then grows (2^-53 to 2^-18 in ten
 // steps, against 2^-39).
 template <int DT>
+__device__ __forceinline__ void read_left(const double* L, int group, double (&l)[DT]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) l[t] = L[(4 * group + (lane >> 4)) * Square<DT>::PITCH + 16 * t + (lane & 15)];
+}
+// (The left operands of four columns of L are read while the products of the four before run; the
+// barriers keep the compiler from reading all of L ahead, for which there are no registers.)
+template <int DT>
 __device__ __forceinline__ void times(const double* L, const f64x4 (&B)[DT], f64x4 (&out)[DT]) {
-    const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 4;
+    double l[2][DT];
+    read_left<DT>(L, 0, l[0]);
 #pragma unroll
     for (int t = 0; t < DT; ++t) out[t] = f64x4{0., 0., 0., 0.};
 #pragma unroll
-    for (int kb = 0; kb < DT; ++kb)
+    for (int g = 0; g < 4 * DT; ++g) {
+        if (g + 1 < 4 * DT) read_left<DT>(L, g + 1, l[(g + 1) & 1]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-                out[t] = mfma64(L[(16 * kb + 4 * c + h) * Square<DT>::PITCH + 16 * t + p], B[kb][c], out[t]);
+        for (int t = 0; t < DT; ++t) out[t] = mfma64(l[g & 1][t], B[g >> 2][g & 3], out[t]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 template <int DT>
@@ -269,19 +396,17 @@ template <int DT>
 constexpr int kStepThreads = 64 * DT < NT ? NT : 64 * DT;
 
 template <int DT>
-__global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Batch batch, double eps, double a, double b, double c, int steps,
+__global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, double eps, double a, double b, double c, int steps,
                                                                   uint8_t* __restrict__ ws) {
     constexpr int D = Square<DT>::D, PITCH = Square<DT>::PITCH, N = kStepThreads<DT>;
     __shared__ double L[D * PITCH];
     __shared__ double trace[2];
-    const Matrix x = batch.m[blockIdx.x];
+    const Matrix x = matrix_at(src, (int)blockIdx.x);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, p = lane & 15, h = lane >> 4;
     const double* part = (const double*)(ws + x.scratch);
     const int64_t pieces = pieces_of(x.n);
     for (int e = tid; e < kTiles<DT> * 256; e += N) {
-        double s = 0.;
-#pragma unroll 8
-        for (int64_t q = 0; q < pieces; ++q) s += part[q * (kTiles<DT> * 256) + e];
+        const double s = part[e];
         int t = 0, k = e >> 8;  // tile k is (t, u)
         while (k >= DT - t) k -= DT - t++;
         const int u = t + k, row = 16 * t + 4 * ((e >> 6) & 3) + ((e >> 4) & 3), col = 16 * u + (e & 15);
@@ -299,7 +424,7 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Batch batch, do
     __syncthreads();
     const double inv = 1. / (sqrt(trace[0]) + eps);
     const bool works = wave < DT;
-    f64x4 S[DT], P[DT], Q[DT], W[DT];
+    f64x4 S[DT], Q[DT], W[DT];
     if (works) {
 #pragma unroll
         for (int t = 0; t < DT; ++t)
@@ -310,22 +435,24 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Batch batch, do
         __syncthreads();  // every wave is done with the left operand
         if (works) put<DT>(L, S, wave);
         __syncthreads();
-        if (works) {
-            times<DT>(L, S, P);
+        if (works) {  // W = P
+            times<DT>(L, S, W);
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    P[t][v] = fma(c, P[t][v], fma(b, S[t][v], t == wave && 4 * v + h == p ? a : 0.));
+                    W[t][v] = fma(c, W[t][v], fma(b, S[t][v], t == wave && 4 * v + h == p ? a : 0.));
         }
         __syncthreads();
-        if (works) put<DT>(L, P, wave);
+        if (works) {
+            put<DT>(L, W, wave);
+            if (k == 0)
+#pragma unroll
+                for (int t = 0; t < DT; ++t) Q[t] = W[t];
+        }
         __syncthreads();
         if (works) {
-            if (k == 0) {
-#pragma unroll
-                for (int t = 0; t < DT; ++t) Q[t] = P[t];
-            } else {
+            if (k > 0) {
                 times<DT>(L, Q, W);
 #pragma unroll
                 for (int t = 0; t < DT; ++t) Q[t] = W[t];
@@ -349,134 +476,244 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Batch batch, do
 // the direction and the update
 // ---------------------------------------------------------------------------
 
-// 64 columns from jb on: lane l holds, of the rows k = 4c + l / 16 of every block, the
+// 64 columns from jb on: lane l holds, of the rows p = 4c + l / 16 of every block, the
 // columns 4 (l % 16) + e (wide) or 16 e + l % 16 (tall).  Results come out where the
-// operands lay.
-template <typename T, typename TP, int DT, bool WIDE>
-__device__ __forceinline__ void apply_piece(const Matrix& x, const Rule& rule, int64_t j0, int64_t j1, const double* L) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = lane & 15, h = lane >> 4;
-    const T* grad = (const T*)x.grad;
-    for (int64_t jb = j0 + 64 * wave; jb < j1; jb += 64 * (NT / 64)) {
-        float v[DT][4][4];  // [block][c][e]
-        // where (c, t or e)'s run of elements starts, and how many of it exist
-        auto run = [&](int c, int k, int& n) {
-            if constexpr (WIDE) {  // k: block; 4 columns
-                const int i = 16 * k + 4 * c + h;
-                n = i < x.d ? most(j1 - (jb + 4 * p), 4) : 0;
-                return n ? (int64_t)i * x.n + jb + 4 * p : 0;
-            } else {  // k: e; DT rows
-                const int64_t j = jb + 16 * k + p;
-                const int i = DT * (4 * c + h);
-                n = j < j1 ? most(x.d - i, DT) : 0;
-                return n ? j * x.d + i : 0;
-            }
-        };
-        constexpr int K = WIDE ? DT : 4, E = WIDE ? 4 : DT;
+// operands lay.  FULL as above; where there are registers for them (AHEAD), the
+// master's values are on their way during the products.
+template <int DT, bool WIDE, bool FULL>
+__device__ __forceinline__ void apply_turn(const Matrix& x, const Rule& rule, int64_t jb, int64_t j1, const double* L) {
+    const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 4;
+    float v[DT][4][4];  // [block][c][e]
+    // runs of E consecutive elements: (block k, c) over e, or column e = k over c and the block
+    constexpr int K = WIDE ? 4 * DT : 4, E = WIDE ? 4 : 4 * DT;
+    auto run = [&](int k, int& n) -> Place {
+        if constexpr (WIDE) {
+            const int i0 = 16 * (k >> 2) + 4 * (k & 3), i = i0 + h;
+            const int64_t j = jb + 4 * p;
+            n = i < x.d ? (FULL ? 4 : most(j1 - j, 4)) : 0;
+            if (FULL) return {(i0 < x.d ? i0 * x.n : 0) + jb, (uint32_t)(h * x.n) + 4 * p};
+            return {n ? (int64_t)i * x.n + j : 0, 0};
+        } else {
+            const int64_t j = jb + 16 * k + p;
+            const int i = 4 * DT * h;
+            n = FULL ? (i < x.d ? E : 0) : j < j1 ? most(x.d - i, E) : 0;
+            if (FULL) return {(jb + 16 * k) * x.d, (uint32_t)(p * x.d + (i < x.d ? i : 0))};
+            return {n ? j * x.d + i : 0, 0};
+        }
+    };
+    auto value = [&](int k, int e) -> float& {
+        if constexpr (WIDE) return v[k >> 2][k & 3][e];
+        else return v[e % DT][e / DT][k];
+    };
+    auto gradients = [&](bool bf16) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k) {
+            int n;
+            const Place at = run(k, n);
+            float g[E];
+            read_grad<E, FULL>(x.grad, bf16, at, n, g);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int e = 0; e < E; ++e) value(k, e) = g[e];
+        }
+    };
+    if (rule.grad_bf16) gradients(true);
+    else gradients(false);
+    if (x.m != nullptr)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            int n;
+            const Place at = run(k, n);
+            float m[E];
+            if constexpr (FULL) read_whole<float, E>(at_place(x.m, at), n > 0, m);
+            else read_some<float, E>(at_place(x.m, at), n, m);
+#pragma unroll
+            for (int e = 0; e < E; ++e) value(k, e) = rule.direction(m[e], value(k, e));
+        }
+    constexpr bool AHEAD = FULL && DT < 4;
+    float old[AHEAD ? K : 1][E];
+    if constexpr (AHEAD)
+        if (x.master != nullptr)
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
                 int n;
-                const int64_t at = run(c, k, n);
-                float g[E], m[E];
-                read_some<T, E>(grad + at, n, g);
-                if (x.m != nullptr) {
-                    read_some<float, E>(x.m + at, n, m);
+                const Place at = run(k, n);
+                read_whole<float, E>(at_place(x.master, at), true, old[k]);
+            }
+    constexpr int EG = DT == 8 ? 1 : DT == 4 ? 2 : 4;  // sets of columns at a time, for the registers
 #pragma unroll
-                    for (int e = 0; e < E; ++e) g[e] = rule.direction(m[e], g[e]);
+    for (int e0 = 0; e0 < 4; e0 += EG) {
+        f64x4 o[EG][DT];
+#pragma unroll
+        for (int e = 0; e < EG; ++e)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) o[e][t] = f64x4{0., 0., 0., 0.};
+        double l[2][DT];
+        read_left<DT>(L, 0, l[0]);
+#pragma unroll
+        for (int g = 0; g < 4 * DT; ++g) {
+            if (g + 1 < 4 * DT) read_left<DT>(L, g + 1, l[(g + 1) & 1]);
+            double r[EG];
+#pragma unroll
+            for (int e = 0; e < EG; ++e) r[e] = (double)v[g >> 2][g & 3][e0 + e];
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int e = 0; e < EG; ++e) o[e][t] = mfma64(l[g & 1][t], r[e], o[e][t]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // (the other sets need their own columns only)
+#pragma unroll
+        for (int e = 0; e < EG; ++e)
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[t][c][e0 + e] = (float)o[e][t][c];
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) value(k, e) *= x.rate;
+    if (x.master != nullptr) {
+        constexpr int RUNS = WIDE ? 4 : DT == 8 ? 1 : 2;  // runs of the master in flight
+#pragma unroll
+        for (int k0 = 0; k0 < K; k0 += RUNS) {
+            float before[RUNS][E];
+#pragma unroll
+            for (int q = 0; q < RUNS; ++q) {
+                int n;
+                const Place at = run(k0 + q, n);
+                if constexpr (AHEAD) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) before[q][e] = old[AHEAD ? k0 + q : 0][e];
+                } else if constexpr (FULL) {
+                    read_whole<float, E>(at_place(x.master, at), true, before[q]);
+                } else {
+                    read_some<float, E>(at_place(x.master, at), n, before[q]);
                 }
+            }
+#pragma unroll
+            for (int q = 0; q < RUNS; ++q) {
+                int n;
+                const Place at = run(k0 + q, n);
+                float w[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    if constexpr (WIDE) v[k][c][e] = g[e];
-                    else v[e][c][k] = g[e];
+                    w[e] = fmaf(x.keep, before[q][e], -value(k0 + q, e));
+                    value(k0 + q, e) = w[e];
                 }
+                if (n > 0) write_some<float, E>(at_place(x.master, at), FULL ? E : n, w);
             }
-        constexpr int EG = DT == 8 ? 2 : 4;  // columns sets at a time
-#pragma unroll
-        for (int e0 = 0; e0 < 4; e0 += EG) {
-            f64x4 o[EG][DT];
-#pragma unroll
-            for (int e = 0; e < EG; ++e)
-#pragma unroll
-                for (int t = 0; t < DT; ++t) o[e][t] = f64x4{0., 0., 0., 0.};
-#pragma unroll
-            for (int kb = 0; kb < DT; ++kb)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    double r[EG];
-#pragma unroll
-                    for (int e = 0; e < EG; ++e) r[e] = (double)v[kb][c][e0 + e];
-#pragma unroll
-                    for (int t = 0; t < DT; ++t) {
-                        const double l = L[(16 * kb + 4 * c + h) * Square<DT>::PITCH + 16 * t + p];
-#pragma unroll
-                        for (int e = 0; e < EG; ++e) o[e][t] = mfma64(l, r[e], o[e][t]);
-                    }
-                }
-            // the later sets still need their own operands: only these columns change
-#pragma unroll
-            for (int e = 0; e < EG; ++e)
-#pragma unroll
-                for (int t = 0; t < DT; ++t)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) v[t][c][e0 + e] = (float)o[e][t][c];
         }
+    }
+    auto params = [&](auto* to) {
+        using TP = std::remove_pointer_t<decltype(to)>;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k) {
+            int n;
+            const Place at = run(k, n);
+            float w[E];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                int n;
-                const int64_t at = run(c, k, n);
-                float d[E], w[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) d[e] = v[WIDE ? k : e][c][WIDE ? e : k];
-                if (n == 0) continue;
-                if (x.master != nullptr) {
-                    read_some<float, E>(x.master + at, n, w);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) w[e] = fmaf(-x.rate, d[e], x.keep * w[e]);
-                    write_some<float, E>(x.master + at, n, w);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) w[e] = x.rate * d[e];
-                }
-                if (x.param != nullptr) write_some<TP, E>((TP*)x.param + at, n, w);
-            }
+            for (int e = 0; e < E; ++e) w[e] = value(k, e);
+            if (n > 0) write_some<TP, E>(at_place(to, at), FULL ? E : n, w);
+        }
+    };
+    if (x.param != nullptr) {
+        if (rule.param_bf16) params((uint16_t*)x.param);
+        else params((float*)x.param);
     }
 }
 
-template <typename T, typename TP, int DT>
-__global__ __launch_bounds__(NT, DT == 8 ? 1 : 2) void apply_kernel(Batch batch, Rule rule, const uint8_t* __restrict__ ws) {
+// Whether the whole turns of a matrix are FULL ones: rows four by four (tall: vectors of 4 DT) exist or do
+// not, and a lane's own offset fits 32 bits.  All else are edges, which another launch takes.
+__host__ __device__ inline bool whole_rows(bool wide, int64_t d, int64_t n, int dt) {
+    return wide ? d % 4 == 0 && n < (int64_t)1 << 26 : d % (4 * dt) == 0;
+}
+
+template <int DT, bool WIDE, bool FULL>
+__global__ __launch_bounds__(NT, DT == 8 ? 1 : 2) void apply_kernel(Source src, Rule rule, int64_t cols, const uint8_t* __restrict__ ws) {
     constexpr int D = Square<DT>::D, PITCH = Square<DT>::PITCH;
-    __shared__ double L[D * PITCH];
-    const int item = find(batch, (int)blockIdx.x);
-    const Matrix x = batch.m[item];
-    const int piece = (int)blockIdx.x - batch.first[item];
-    const int64_t cols = piece_cols(x.n), j0 = piece * cols, j1 = j0 + cols < x.n ? j0 + cols : x.n;
+    __shared__ __attribute__((aligned(16))) double L[D * PITCH];
+    int piece;
+    const Matrix x = matrix_of(src, (int)blockIdx.x, piece);
+    const int64_t end = FULL ? x.n / 64 * 64 : x.n;
+    int64_t j0 = piece * cols;
+    if (!FULL && whole_rows(WIDE, x.d, x.n, DT)) j0 += x.n / 64 * 64;
+    const int64_t j1 = j0 + cols < end ? j0 + cols : end;
     const double* Q = (const double*)(ws + x.scratch) + pieces_of(x.n) * (kTiles<DT> * 256);
-    for (int e = threadIdx.x; e < D * D; e += NT) L[e / D * PITCH + e % D] = Q[e];
+    typedef double f64x2 __attribute__((ext_vector_type(2)));
+    for (int e = 2 * threadIdx.x; e < D * D; e += 2 * NT) *(f64x2*)(L + e / D * PITCH + e % D) = *(const f64x2*)(Q + e);
     __syncthreads();
-    if (x.wide) apply_piece<T, TP, DT, true>(x, rule, j0, j1, L);
-    else apply_piece<T, TP, DT, false>(x, rule, j0, j1, L);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll 1
+    for (int64_t jb = j0 + 64 * wave; jb < j1; jb += 64 * (NT / 64))
+        apply_turn<DT, WIDE, FULL>(x, rule, jb, j1, L);
 }
 
 int blocks_of(int64_t d) { return d <= 16 ? 1 : d <= 32 ? 2 : d <= 64 ? 4 : 8; }
 
-template <int DT>
-hipError_t launch_batch(const UpdateArgs& a, const Batch& b, hipStream_t s) {
-    const Rule rule{a.momentum, a.fresh, (int)a.nesterov};
-    const dim3 grid((unsigned)b.first[b.count]);
-    if (a.grad_bf16) hipLaunchKernelGGL((gram_kernel<uint16_t, DT>), grid, dim3(NT), 0, s, b, rule, a.workspace);
-    else hipLaunchKernelGGL((gram_kernel<float, DT>), grid, dim3(NT), 0, s, b, rule, a.workspace);
-    hipLaunchKernelGGL((steps_kernel<DT>), dim3(b.count), dim3(kStepThreads<DT>), 0, s, b, a.eps, a.a, a.b, a.c, a.steps, a.workspace);
-    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, s, b, rule, (const uint8_t*)a.workspace); };
-    if (a.grad_bf16) {
-        if (a.param_bf16) run(apply_kernel<uint16_t, uint16_t, DT>);
-        else run(apply_kernel<uint16_t, float, DT>);
-    } else {
-        if (a.param_bf16) run(apply_kernel<float, uint16_t, DT>);
-        else run(apply_kernel<float, float, DT>);
+// The chosen ones of the matrices, whose workgroups f counts, as a launch's source; `table` has
+// room for all of them.
+template <class Choose, class Count>
+Source collect(const Matrix* matrices, int64_t count, Table table, hipStream_t s, int& blocks, Choose choose, Count f) {
+    Source src{};
+    src.table = table;
+    for (int64_t i = 0; i < count; ++i) src.count += choose(matrices[i]) ? 1 : 0;
+    src.many = src.count > kBatch;
+    Batch& b = src.batch;
+    int at = 0;
+    blocks = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (!choose(matrices[i])) continue;
+        b.m[b.count] = matrices[i];
+        b.first[b.count++] = blocks;
+        blocks += f(matrices[i]);
+        if (src.many && (b.count == kBatch || at + b.count == src.count)) {
+            hipLaunchKernelGGL(table_kernel, dim3(1), dim3(64), 0, s, b, at, table);
+            at += b.count;
+            b.count = 0;
+        }
     }
+    return src;
+}
+
+// The matrices of one size of the short side.
+template <int DT>
+hipError_t launch_size(const UpdateArgs& a, const Matrix* matrices, int64_t count, Table table, hipStream_t s) {
+    const Rule rule{a.momentum, a.fresh, (int)a.nesterov, (int)a.grad_bf16, (int)a.param_bf16};
+    auto mine = [](const Matrix& x) { return blocks_of(x.d) == DT; };
+    int blocks = 0;
+    const Source all = collect(matrices, count, table, s, blocks, mine, [](const Matrix& x) { return (int)pieces_of(x.n); });
+    if (all.count == 0) return hipSuccess;
+    hipLaunchKernelGGL((gram_kernel<DT>), dim3(blocks), dim3(NT), 0, s, all, rule, a.workspace);
+    hipLaunchKernelGGL(sum_kernel, dim3(kTiles<DT>, all.count), dim3(NT), 0, s, all, kTiles<DT> * 256, a.workspace);
+    hipLaunchKernelGGL((steps_kernel<DT>), dim3(all.count), dim3(kStepThreads<DT>), 0, s, all, a.eps, a.a, a.b, a.c, a.steps,
+                       a.workspace);
+    auto apply = [&](auto wide_tag, auto full_tag) {
+        constexpr bool WIDE = decltype(wide_tag)::value, FULL = decltype(full_tag)::value;
+        auto cols_of = [](const Matrix& x) {
+            const bool whole = whole_rows(WIDE, x.d, x.n, DT);
+            return FULL ? (whole ? x.n / 64 * 64 : 0) : whole ? x.n % 64 : x.n;
+        };
+        auto some = [&](const Matrix& x) { return mine(x) && (x.wide != 0) == WIDE && cols_of(x) > 0; };
+        // Columns of a workgroup: its copy of Q is worth several turns of them where there are
+        // workgroups enough.
+        int64_t turns = 0;
+        for (int64_t i = 0; i < count; ++i)
+            if (some(matrices[i])) turns += (cols_of(matrices[i]) + kPiece - 1) / kPiece;
+        if (turns == 0) return;
+        int64_t each = turns / 512;
+        each = each < 1 ? 1 : each > 8 ? 8 : each;
+        while (turns / each + count > (int64_t)1 << 30) each *= 2;  // (they are counted in 32 bits)
+        const int64_t cols = each * kPiece;
+        int grid = 0;
+        const Source src = collect(matrices, count, table, s, grid, some,
+                                   [&](const Matrix& x) { return (int)((cols_of(x) + cols - 1) / cols); });
+        hipLaunchKernelGGL((apply_kernel<DT, WIDE, FULL>), dim3(grid), dim3(NT), 0, s, src, rule, cols, (const uint8_t*)a.workspace);
+    };
+    apply(std::true_type{}, std::true_type{});
+    apply(std::false_type{}, std::true_type{});
+    apply(std::true_type{}, std::false_type{});
+    apply(std::false_type{}, std::false_type{});
     return hipGetLastError();
 }
 
@@ -487,24 +724,16 @@ int64_t update_scratch(int64_t d, int64_t n) {
     return 8 * (pieces_of(n) * (dt * (dt + 1) / 2 * 256) + 256 * dt * dt);
 }
 
-hipError_t launch_update(const UpdateArgs& a, const Matrix* matrices, int64_t count, hipStream_t s) {
-    hipError_t e = hipSuccess;
-    for (int dt = 1; dt <= 8 && e == hipSuccess; dt *= 2) {
-        Batch b{};
-        for (int64_t i = 0; i <= count && e == hipSuccess; ++i) {
-            const bool fits = i < count && blocks_of(matrices[i].d) == dt;
-            if (fits) {
-                b.m[b.count] = matrices[i];
-                b.first[b.count + 1] = b.first[b.count] + (int)pieces_of(matrices[i].n);
-                ++b.count;
-            }
-            if (b.count == kBatch || (i == count && b.count > 0)) {
-                e = dt == 1 ? launch_batch<1>(a, b, s) : dt == 2 ? launch_batch<2>(a, b, s) : dt == 4 ? launch_batch<4>(a, b, s)
-                                                                                               : launch_batch<8>(a, b, s);
-                b.count = 0;
-            }
-        }
-    }
+int64_t update_table(int64_t count) { return count > kBatch ? count * (int64_t)(sizeof(Matrix) + sizeof(int)) : 0; }
+
+hipError_t launch_update(const UpdateArgs& a, const Matrix* matrices, int64_t count, void* table, hipStream_t s) {
+    Table t{};
+    t.m = (Matrix*)table;
+    t.first = (int*)(t.m + (table != nullptr ? count : 0));
+    hipError_t e = launch_size<1>(a, matrices, count, t, s);
+    if (e == hipSuccess) e = launch_size<2>(a, matrices, count, t, s);
+    if (e == hipSuccess) e = launch_size<4>(a, matrices, count, t, s);
+    if (e == hipSuccess) e = launch_size<8>(a, matrices, count, t, s);
     return e;
 }
 
