@@ -37,16 +37,19 @@ lors_status_t check_gated(const lors_problem_t* p, int32_t activation, uint32_t 
     return LORS_OK;
 }
 
-// The backward's scratch: both transposed masks, both padded B's, dG, dU.
+// The backward's scratch: both transposed masks, both padded B's, dG, dU, and the fp32
+// partial sums of dX's tiles that are cut over the K-steps of both projections (whole
+// tiles, so ranks up to 64).
 struct GatedScratch {
-    int64_t mt, pad, grad, total;
+    int64_t mt, pad, grad, split, total;
     explicit GatedScratch(const lors_problem_t* p) {
         const bool bf16 = p->dtype == LORS_DTYPE_BF16;
         const int64_t rp = (p->r + 7) / 8 * 8;
         mt = bf16 ? round256(p->C * ((p->R + 31) / 32) * 4) : 0;
         pad = bf16 && rp != p->r ? round256(2 * p->R * rp) : 0;
         grad = round256(p->L * p->R * elt_size(p->dtype));
-        total = 2 * (mt + pad + grad);
+        split = bf16 && rp <= 64 ? lors::split_part_bytes(lors::gated_dx_split(p->L, p->R, p->C)) : 0;
+        total = 2 * (mt + pad + grad) + split;
     }
 };
 
@@ -234,6 +237,7 @@ lors_status_t lors_gated_backward(const lors_problem_t* p, int32_t activation, c
     void* dU = static_cast<uint8_t*>(dG) + ws.grad;
     a.dY = dG;
     second.dY = dU;
+    a.split_ws = ws.split ? static_cast<uint8_t*>(dU) + ws.grad : nullptr;
     hipError_t e = hipSuccess;
     // the bf16 dX launch clears dB and dA of both projections for the atomics of the
     // adapters' gradients

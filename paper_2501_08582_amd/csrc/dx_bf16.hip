@@ -39,12 +39,14 @@
 #define LORS_FIRST(name) name##_gate
 #define LORS_MORE , GatedGrad pair
 #define LORS_PAIR , grad_pair_of(a)
+#define LORS_TERMS 2
 #define LORS_DX launch_gated_dx_bf16
 #define LORS_DX_THIN launch_gated_dx_thin_bf16
 #else
 #define LORS_FIRST(name) name
 #define LORS_MORE
 #define LORS_PAIR
+#define LORS_TERMS 1
 #define LORS_DX launch_dx_bf16
 #define LORS_DX_THIN launch_dx_thin_bf16
 #endif
@@ -119,7 +121,8 @@ struct Layout {
 // the forward kernel.
 // LORS_GATED: the two projections of a gated block (GatedGrad, gated.hpp): the
 // accumulators take the second's products after the first's, so that dX is their
-// unrounded sum.  The pipeline drains and fills once between them.
+// unrounded sum.  The pipeline drains and fills once between them.  A piece of a
+// split tile takes a range of the K-steps of both, numbered one after the other.
 template <int RK, bool KRAG, bool FOLD, int TM, int NF>
 __global__ __launch_bounds__(NT, 1) void dx_kernel(
     const uint16_t* __restrict__ LORS_FIRST(dY), const uint16_t* __restrict__ LORS_FIRST(W),
@@ -170,14 +173,15 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
     int64_t m0;
     int n0;
     if constexpr (TM == BM && NF == 2) {
-        work_coords(blockIdx.x, tiles_m, tiles_n, GROUP_M, n_full, split, (R + BK - 1) / BK, tm, tn, kbeg, nk);
+        work_coords(blockIdx.x, tiles_m, tiles_n, GROUP_M, n_full, split, LORS_TERMS * ((R + BK - 1) / BK), tm, tn, kbeg,
+                    nk);
         m0 = (int64_t)tm * BM;
         n0 = tn * BN;
     } else {
         int u;
         thin_coords(blockIdx.x, tiles_m, tiles_n, GROUP_M, n_full, split, (SPAN / TM) * (2 / NF), tm, tn, u);
         kbeg = 0;
-        nk = (R + BK - 1) / BK;
+        nk = LORS_TERMS * ((R + BK - 1) / BK);
         m0 = (int64_t)tm * SPAN + (int64_t)(u % (SPAN / TM)) * TM;
         n0 = tn * BN + (u / (SPAN / TM)) * Lay::FT;
         if (m0 >= L || n0 >= C) return;  // a part of an edge tile that holds no output
@@ -185,7 +189,9 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
     // last row of the dY slab, last column chunk and last column that exist
     const int lastm = (int)min(L - 1 - m0, (int64_t)(TM - 1));
     const int lastc = C - 8 - n0, lastn = C - 1 - n0;
+#ifndef LORS_GATED
     const int kofs = kbeg * BK;
+#endif
     const int wprT = (R + 31) >> 5;  // words per row of M^T
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
     const uint8_t* zsrc = (const uint8_t*)g_zero_page + 16 * lane;
@@ -219,8 +225,13 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
     const int ncol0 = 32 * NF * wave + l32;
     // the projections of a gated block: the gate's contraction, then the up
     // projection's
+    const int ksteps = (R + BK - 1) / BK, kend = kbeg + nk;
 #pragma unroll 1
     for (int seg = 0; seg < 2; ++seg) {
+    const int kfirst = max(kbeg - seg * ksteps, 0);
+    const int nk = min(kend - seg * ksteps, ksteps) - kfirst;
+    if (nk <= 0) continue;
+    const int kofs = kfirst * BK;
     const uint16_t* dY = seg == 0 ? dY_gate : pair.dY;
     const uint16_t* W = seg == 0 ? W_gate : pair.W;
     const uint32_t* Mt = seg == 0 ? Mt_gate : pair.Mt;
@@ -620,7 +631,6 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
     // (rows of 32 NF outputs), then 16-byte stores of whole rows.
     wait_vmcnt<0>();
     lds_barrier();  // every wave's copies landed and every read of the stages done
-#ifndef LORS_GATED
     if (TM == BM && NF == 2 && (int)blockIdx.x >= n_full) {
         // a piece of a split tile: its unrounded fp32 partial sums go to slice
         // blockIdx.x - n_full of `part` (256 tokens x 256 features); the
@@ -635,7 +645,6 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
                     dst[(32 * mb + 8 * (v >> 2) + 4 * h + (v & 3)) * BN + ncol0 + 32 * nb] = acc[mb][nb][v];
         return;
     }
-#endif
     constexpr int OW = 32 * NF;   // outputs per staged row
     constexpr int CH = OW / 8;    // 16-byte chunks per row
     uint16_t* ol = (uint16_t*)(smem + wave * (TM * OW * 2));
@@ -694,8 +703,12 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st, int ra) {
     // backward at rank 64 (us): 65792 x 2048, 200 tokens (8 tiles in 8 pieces)
     // 1100 / 545; 4096 x 11008, 1531 tokens (2 in 8) 406 / 378.
     TailSplit sp{tiles, 1, tiles};
+#ifdef LORS_GATED
+    if (a.split_ws != nullptr) sp = gated_dx_split(a.L, a.R, a.C);
+#else
     if (a.split_ws != nullptr && !dx_whole_tiles(a.L, a.R, a.C))
         sp = tail_split(tiles, (a.R + BK - 1) / BK, a.split_budget);
+#endif
     const ThinPlan tp = sp.split == 1 ? thin_plan(a.L, a.C) : ThinPlan{tiles, 0, 0};
     float* part = sp.split > 1 ? (float*)a.split_ws : nullptr;
     // with thin tiles the whole-tile grid is exactly the first n_full tiles

@@ -67,6 +67,15 @@ struct TailSplit {
 constexpr int64_t kNoPartials = INT64_MAX;
 constexpr int64_t kPieceBytes = 256 * 256 * 4;  // fp32 partials of one piece
 TailSplit tail_split(int64_t tiles, int64_t nk, int64_t max_part_bytes);
+// The gated block's dX (L x C over both projections' R): cut whatever the shape, since
+// its workspace holds dG and dU as it is and its K is twice as long -- from 32 K-steps on.
+// Thin tiles against pieces, the whole backward (us): 4096 tokens of 13824 x 5120, rank 64
+// (64 of 320 tiles in 4 pieces) 2511 / 2340; 128 of 11008 x 4096, rank 16, 347 / 195; 300 of
+// 1000 x 520 (32 K-steps) 61.5 / 53.6; 512 of 512 x 512 (16 K-steps) 44.5 / 47.1.
+inline TailSplit gated_dx_split(int64_t L, int64_t R, int64_t C) {
+    const int64_t tiles = ((L + 255) / 256) * ((C + 255) / 256), nk = 2 * ((R + 63) / 64);
+    return nk >= 32 ? tail_split(tiles, nk, kNoPartials) : TailSplit{(int)tiles, 1, (int)tiles};
+}
 // Bytes of fp32 partial sums a split grid of 256 x 256 tiles writes.
 inline int64_t split_part_bytes(const TailSplit& t) {
     return t.split > 1 ? (int64_t)(t.grid - t.n_full) * kPieceBytes : 0;

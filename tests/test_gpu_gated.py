@@ -102,7 +102,10 @@ def test_forward(i, shape):
 
 BACK = [(1, 8, 8, 1), (5, 72, 40, 3), (64, 264, 136, 16), (65, 520, 200, 12), (200, 264, 512, 64), (577, 1032, 200, 100),
         (333, 72, 1032, 128), (3328, 64, 2560, 16), (3328, 128, 2560, 64), (3300, 72, 2552, 33), (3299, 64, 2560, 48),
-        (4352, 64, 4096, 30), (130, 2560, 2560, 17)]
+        (4352, 64, 4096, 30), (130, 2560, 2560, 17),
+        # dX's last wave cut over both projections' K-steps: three pieces a tile, the middle one
+        # with steps of both (ragged, and whole tiles); six pieces behind a wave of whole tiles
+        (260, 1032, 10000, 5), (512, 1088, 10240, 64), (2100, 1032, 8200, 33)]
 
 
 @pytest.mark.parametrize("i,shape", list(enumerate(BACK)))
