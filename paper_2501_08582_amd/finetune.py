@@ -1,18 +1,24 @@
 """Preference fine-tuning of a small sparse model, with every operator in its place.
 
-The model is a stack of gateless feed-forward blocks over single tokens (no
-attention, so it learns which token follows which): embedding, then in each block
+The model is a stack of feed-forward blocks over single tokens (no attention, so
+it learns which token follows which): embedding, then in each block
 residual + dropout(branch) and its norm, a sparse up projection with adapters,
-SiLU and a sparse down projection, at last a norm and a sparse head.  All
-projections are ``ops.lors_linear``; embedding, norms, dropout and the loss are
-those of ``train``.  The weights are pruned and frozen; adapters, norm weights and
-the embedding train.
+SiLU and a sparse down projection, at last a norm and a sparse head.  With
+``gated`` a second projection of the same input, through SiLU, multiplies the up
+projection instead (``ops.lors_gated``).  The other projections are
+``ops.lors_linear``; embedding, norms, dropout and the loss are those of
+``train``.  The weights are pruned and frozen; adapters, norm weights and the
+embedding train: by descent with momentum, or the adapters along orthogonalised
+momenta (``update="orthogonal"``, ``train.OrthogonalUpdate``).
 
 The loss prefers continuations that follow a rule over random ones.  Its
 reference is the model before training: the adapters start at B = 0, so it is the
 sparse model alone, and its log-probabilities are taken once.
 
-``python -m paper_2501_08582_amd.finetune --steps 30``
+After training the model continues prompts greedily, or by ``train.sample`` at a
+temperature.
+
+``python -m paper_2501_08582_amd.finetune --steps 30 --gated --update orthogonal``
 """
 from __future__ import annotations
 
@@ -42,6 +48,9 @@ class Config:
     prompt: int = 16
     lr: float = 3e-4
     seed: int = 0
+    gated: bool = False
+    update: str = "momentum"  # or "orthogonal": the adapters' rule, whose matrix_lr is of another kind
+    matrix_lr: float = 0.02
 
 
 class Projection:
@@ -63,6 +72,10 @@ class Projection:
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
         return ops.lors_linear(x, self.W, self.M, self.B, self.A, self.cfg.scale, self.cfg.mask)
 
+    def parts(self):
+        """(W, M, B, A), as the gated block takes a projection."""
+        return self.W, self.M, self.B, self.A
+
     def serve(self, x: torch.Tensor) -> torch.Tensor:
         return ops.forward(x, self.W, self.M, self.B.detach(), self.A.detach(), self.cfg.scale, self.cfg.mask)
 
@@ -77,13 +90,29 @@ class Model:
         self.head = Projection(cfg.vocab, cfg.width, cfg, g)
         self.norms = [torch.ones(cfg.width, dtype=torch.bfloat16, device="cuda", requires_grad=True)
                       for _ in range(cfg.layers + 1)]
+        self.gates = [Projection(cfg.hidden, cfg.width, cfg, g) for _ in range(cfg.layers if cfg.gated else 0)]
 
     def parameters(self) -> Dict[str, torch.Tensor]:
         out = {"table": self.table, "head.A": self.head.A, "head.B": self.head.B}
         for i, (up, down) in enumerate(self.blocks):
             out.update({f"{i}.up.A": up.A, f"{i}.up.B": up.B, f"{i}.down.A": down.A, f"{i}.down.B": down.B})
+        for i, gate in enumerate(self.gates):
+            out.update({f"{i}.gate.A": gate.A, f"{i}.gate.B": gate.B})
         out.update({f"norm.{i}": w for i, w in enumerate(self.norms)})
         return out
+
+    def inner(self, i: int, x: torch.Tensor) -> torch.Tensor:
+        """What block i's down projection takes."""
+        up, _ = self.blocks[i]
+        if self.cfg.gated:
+            return ops.lors_gated(x, self.gates[i].parts(), up.parts(), self.cfg.scale, self.cfg.mask)
+        return torch.nn.functional.silu(up(x))
+
+    def inner_serve(self, i: int, x: torch.Tensor) -> torch.Tensor:
+        up, _ = self.blocks[i]
+        if self.cfg.gated:
+            return ops.gated_forward(x, self.gates[i].parts(), up.parts(), self.cfg.scale, self.cfg.mask, save=False)[0]
+        return torch.nn.functional.silu(up.serve(x))
 
     def logits(self, ids: torch.Tensor, p: float = 0.0, offset: int = 0) -> torch.Tensor:
         """Logits of the token after each of ``ids``.  Every dropout of a pass takes an
@@ -91,26 +120,33 @@ class Model:
         cfg = self.cfg
         table_scale = cfg.width**0.5
         branch, stream = train.embedding(ids, self.table, table_scale), None
-        for i, (up, down) in enumerate(self.blocks):
+        for i, (_, down) in enumerate(self.blocks):
             x, stream = train.norm(branch, self.norms[i], kind=cfg.kind, residual=stream, p=p, seed=cfg.seed,
                                    offset=offset * (cfg.layers + 1) + i)
-            branch = down(torch.nn.functional.silu(up(x)))
+            branch = down(self.inner(i, x))
         x, _ = train.norm(branch, self.norms[-1], kind=cfg.kind, residual=stream, p=p, seed=cfg.seed,
                           offset=offset * (cfg.layers + 1) + cfg.layers)
         return self.head(x)
 
     @torch.no_grad()
-    def generate(self, ids: torch.Tensor, tokens: int) -> torch.Tensor:
-        """Greedy continuation of the last token of each sequence, one token a pass:
-        the forms without gradients and statistics."""
+    def generate(self, ids: torch.Tensor, tokens: int, temperature: float = 0.0, top_k: int = 0, top_p: float = 1.0,
+                 generator: Optional[torch.Generator] = None) -> torch.Tensor:
+        """Continuation of the last token of each sequence, one token a pass: greedy, or sampled
+        at a temperature with ``generator``'s numbers.  The forms without gradients and
+        statistics."""
         cfg, out = self.cfg, [ids]
         for _ in range(tokens):
             branch, stream = train.embedding_forward(out[-1][:, -1:].contiguous(), self.table, cfg.width**0.5), None
-            for i, (up, down) in enumerate(self.blocks):
+            for i, (_, down) in enumerate(self.blocks):
                 x, stream, _, _ = train.norm_forward(branch, self.norms[i], kind=cfg.kind, residual=stream, need_stats=False)
-                branch = down.serve(torch.nn.functional.silu(up.serve(x)))
+                branch = down.serve(self.inner_serve(i, x))
             x, _, _, _ = train.norm_forward(branch, self.norms[-1], kind=cfg.kind, residual=stream, need_stats=False)
-            out.append(self.head.serve(x).argmax(dim=-1))
+            logits = self.head.serve(x)
+            if temperature == 0.0:
+                out.append(logits.argmax(dim=-1))
+                continue
+            u = torch.rand(logits.shape[:-1], generator=generator, device="cuda")
+            out.append(train.sample(logits, u, temperature, top_k, top_p)[0])
         return torch.cat(out, dim=1)
 
 
@@ -145,7 +181,8 @@ def batch(cfg: Config, seed: int) -> Tuple[torch.Tensor, torch.Tensor]:
 
 class Trainer:
     """Descent with momentum on fp32 copies of the trained parameters, every array's step
-    of the same root mean square."""
+    of the same root mean square; with ``update="orthogonal"`` all adapters take one
+    ``train.OrthogonalUpdate`` instead."""
 
     def __init__(self, cfg: Optional[Config] = None):
         self.cfg = cfg = cfg or Config()
@@ -153,6 +190,13 @@ class Trainer:
         self.params = self.model.parameters()
         self.master = {k: p.detach().float() for k, p in self.params.items()}
         self.speed = {k: torch.zeros_like(m) for k, m in self.master.items()}
+        self.matrices: List[str] = []
+        if cfg.update == "orthogonal":
+            self.matrices = [k for k in self.params if k.endswith((".A", ".B"))]
+            kept = [[of[k] for k in self.matrices] for of in (self.master, self.params, self.speed)]
+            self.rule = train.OrthogonalUpdate(kept[0], [p.detach() for p in kept[1]], kept[2])
+        elif cfg.update != "momentum":
+            raise ValueError(f"unknown update {cfg.update!r} (momentum, orthogonal)")
         self.count = 0
 
     @torch.no_grad()
@@ -167,7 +211,12 @@ class Trainer:
         loss, reward, _ = train.preference_loss(logits, targets, ref, cfg.beta)
         grads = torch.autograd.grad(loss, list(self.params.values()))
         with torch.no_grad():
+            if self.matrices:
+                by_name = dict(zip(self.params, grads))
+                self.rule.step([by_name[k] for k in self.matrices], cfg.matrix_lr)
             for (k, p), grad in zip(self.params.items(), grads):
+                if k in self.matrices:
+                    continue
                 self.speed[k].mul_(0.9).add_(grad.float(), alpha=0.1)
                 rms = self.speed[k].square().mean().sqrt() + 1e-12
                 self.master[k].sub_(self.speed[k] / rms, alpha=cfg.lr)
@@ -181,8 +230,11 @@ def main(argv=None) -> None:
     ap.add_argument("--steps", type=int, default=30)
     ap.add_argument("--kind", choices=(train.LAYER, train.RMS), default=train.RMS)
     ap.add_argument("--mask", choices=(ops.BITMAP, ops.TWO_FOUR), default=ops.TWO_FOUR)
+    ap.add_argument("--gated", action="store_true", help="gated blocks")
+    ap.add_argument("--update", choices=("momentum", "orthogonal"), default="momentum", help="the adapters' rule")
+    ap.add_argument("--temperature", type=float, default=0.0, help="also sample continuations at it")
     a = ap.parse_args(argv)
-    trainer = Trainer(Config(kind=a.kind, mask=a.mask))
+    trainer = Trainer(Config(kind=a.kind, mask=a.mask, gated=a.gated, update=a.update))
     cfg = trainer.cfg
     batches = [batch(cfg, 100 + i) for i in range(4)]
     refs = [trainer.reference(*b) for b in batches]
@@ -196,6 +248,10 @@ def main(argv=None) -> None:
     told = trainer.model.generate(start, 4)
     hits = (told[:, 1:] == rule(told[:, :-1], cfg.vocab)).float().mean()
     print(f"greedy continuations that follow the rule: {float(hits):.2f}", flush=True)
+    if a.temperature > 0.0:
+        told = trainer.model.generate(start, 4, a.temperature, top_p=0.95, generator=torch.Generator(device="cuda").manual_seed(1))
+        hits = (told[:, 1:] == rule(told[:, :-1], cfg.vocab)).float().mean()
+        print(f"sampled ones: {float(hits):.2f}", flush=True)
 
 
 if __name__ == "__main__":

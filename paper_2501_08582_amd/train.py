@@ -539,8 +539,8 @@ class OrthogonalUpdate:
 
     with the direction of ``orthogonalize``.  ``masters`` and ``momenta`` are fp32 (momenta: zeros if
     not given) and changed in place; ``params``, of one type, receive the masters' values and may be
-    left out.  All matrices take one call of three launches for every 48 of a size of the short side
-    (up to 16, 32, 64, 128).  ``step`` may be captured into a graph; its scratch memory belongs to
+    left out.  A step is one call, whatever the count: its launches are a few for each size of the
+    short side (up to 16, 32, 64, 128).  ``step`` may be captured into a graph; its scratch memory belongs to
     the object, so steps of one object must not overlap."""
 
     def __init__(self, masters: Sequence[torch.Tensor], params: Optional[Sequence[torch.Tensor]] = None,

@@ -1,0 +1,137 @@
+"""The gated block, the orthogonalised updates and the sampling together: training a
+gated model and serving it, as the fine-tuning example uses them."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block as ob
+from paper_2501_08582_amd import finetune, ops, train
+from tests.gpu_helpers import dev_to_f64
+
+pytestmark = pytest.mark.gpu
+
+
+def small(**over):
+    return finetune.Config(**{**dict(vocab=512, width=128, hidden=256, pairs=6, length=33, prompt=5, gated=True,
+                                     update="orthogonal"), **over})
+
+
+@pytest.mark.parametrize("mask,kind", [(ops.TWO_FOUR, train.RMS), (ops.BITMAP, train.LAYER)])
+def test_training_steps_and_samples(mask, kind):
+    cfg = small(mask=mask, kind=kind)
+    trainer = finetune.Trainer(cfg)
+    names = list(trainer.params)
+    assert "0.gate.A" in names and trainer.matrices == [k for k in names if k[-2:] in (".A", ".B")]
+    ids, targets = finetune.batch(cfg, 3)
+    ref = trainer.reference(ids, targets)
+    rule, taken = trainer.rule.step, []
+
+    def watched_step(grads, lr):
+        taken.append([g.clone() for g in grads])
+        rule(grads, lr)
+
+    trainer.rule.step = watched_step
+    for _ in range(3):
+        before = [(dev_to_f64(trainer.master[k]), dev_to_f64(trainer.speed[k])) for k in trainer.matrices]
+        loss, _ = trainer.step(ids, targets, ref)
+        assert torch.isfinite(loss)
+        for k, g, (w, m) in zip(trainer.matrices, taken[-1], before):
+            g = dev_to_f64(g)
+            rate = cfg.matrix_lr * max(1.0, w.shape[0] / w.shape[1]) ** 0.5
+            rm, rw = ob.update(g, m, w, 0.95, True, rate, 0.0, 5, *train.COEFFICIENTS, 1e-7)
+            size = 0.95 * np.abs(m) + 0.05 * np.abs(g)
+            assert (np.abs(dev_to_f64(trainer.speed[k]) - rm) <= 2 * 2.0**-24 * size + 2.0**-24 * np.abs(rm)).all(), k
+            # v off by four roundings, the steps' gain 485; one rounding of the direction, two of the master
+            err = np.linalg.norm(dev_to_f64(trainer.master[k]) - rw)
+            assert err <= rate * (485 * 4 * 2.0**-24 + 2.0**-24 * np.sqrt(min(g.shape)) * 1.3) + 2 * 2.0**-24 * np.linalg.norm(np.abs(w) + rate), k
+            assert torch.equal(trainer.params[k].detach(), trainer.master[k].bfloat16())
+    assert any(g.any() for k, g in zip(trainer.matrices, taken[-1]) if k.endswith("gate.A"))
+    # serving the trained model, sampled: every token is the oracle's on the same logits
+    start = torch.arange(7, device="cuda").unsqueeze(1)
+    seen = []
+    plain = train.sample
+
+    def watched(logits, u, *rest):
+        out = plain(logits, u, *rest)
+        seen.append((logits.clone(), u.clone(), out))
+        return out
+
+    g = torch.Generator(device="cuda").manual_seed(5)
+    try:
+        train.sample = watched
+        told = trainer.model.generate(start, 3, 0.8, top_k=40, top_p=0.9, generator=g)
+    finally:
+        train.sample = plain
+    again = trainer.model.generate(start, 3, 0.8, top_k=40, top_p=0.9, generator=torch.Generator(device="cuda").manual_seed(5))
+    assert told.shape == (7, 4) and torch.equal(told, again) and len(seen) == 3
+    for step, (logits, u, (token, logp)) in enumerate(seen):
+        assert torch.equal(told[:, step + 1:step + 2], token) and logits.shape == (7, 1, cfg.vocab)
+        for row in range(7):
+            want, low = ob.sample(dev_to_f64(logits[row, 0]), float(u[row, 0]), 0.8, 40, 0.9, 0.0)
+            assert int(token[row, 0]) == want and abs(float(logp[row, 0]) - low) <= 2.0**-24 * abs(low) + 2.0**-40
+
+
+def test_a_gated_model_serves_what_it_trains():
+    """The logits of the serving forms and of the training forms, on the same tokens."""
+    cfg = small(update="momentum")
+    trainer = finetune.Trainer(cfg)
+    ids, targets = finetune.batch(cfg, 4)
+    trainer.step(ids, targets, trainer.reference(ids, targets))
+    start = torch.arange(9, device="cuda").unsqueeze(1)
+    told = trainer.model.generate(start, 3)
+    with torch.no_grad():
+        logits = trainer.model.logits(told[:, :-1].contiguous())
+    picked = logits.gather(2, told[:, 1:].unsqueeze(2)).squeeze(2)
+    # the greedy token is the largest, up to the rounding of logits by calls of other lengths
+    assert (picked >= logits.amax(2) - 2.0**-6 * logits.abs().amax(2)).all()
+
+
+def plain_logits(model, ids, leaves):
+    """The model in 64 bits, W' rounded to bf16 as its definition has it (the rounding passes
+    the gradient on)."""
+    cfg = model.cfg
+
+    def project(q, name, x):
+        W = q.W.double().cpu()
+        merged = W + cfg.scale * (W != 0) * (leaves[name + ".B"] @ leaves[name + ".A"])
+        return x @ (merged + (merged.bfloat16().double() - merged).detach()).T
+
+    def norm(x, w):
+        return x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-5) * w
+
+    branch, stream = leaves["table"][ids.cpu()] * cfg.width**0.5, 0.0
+    for i, (up, down) in enumerate(model.blocks):
+        stream = stream + branch
+        x = norm(stream, leaves[f"norm.{i}"])
+        inner = torch.nn.functional.silu(project(model.gates[i], f"{i}.gate", x)) * project(up, f"{i}.up", x)
+        branch = project(down, f"{i}.down", inner)
+    return project(model.head, "head", norm(stream + branch, leaves[f"norm.{len(model.blocks)}"]))
+
+
+def test_the_gated_model_s_gradients():
+    """Gradients of a weighted sum of the logits by every parameter, against the model in 64
+    bits.  Between a parameter and its gradient lie at most 16 tensors that are rounded to
+    bf16 (embedding; norm; G, U, H twice; down; stream; norm; and on the way back the head's dX, the
+    norm's, down's, dG and dU, the G tile, dX, the norm's, the gradient), each off by at most
+    2^-8 of itself; relative Frobenius errors of a chain of products add."""
+    cfg = small(dropout=0.0, layers=1)
+    model = finetune.Model(cfg)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    with torch.no_grad():
+        for k, p in model.parameters().items():
+            if k.endswith(".B"):
+                p.copy_(0.05 * torch.randn(p.shape, generator=g, device="cuda"))
+    ids = torch.randint(0, cfg.vocab, (2, 32), generator=g, device="cuda")
+    weight = torch.randn((2, 32, cfg.vocab), generator=g, device="cuda").bfloat16()
+    params = model.parameters()
+    got = torch.autograd.grad((model.logits(ids) * weight).float().sum(), list(params.values()))
+    leaves = {k: p.detach().double().cpu().requires_grad_(True) for k, p in params.items()}
+    want = torch.autograd.grad((plain_logits(model, ids, leaves) * weight.double().cpu()).sum(), list(leaves.values()))
+    for k, a, b in zip(params, got, want):
+        e = float((a.double().cpu() - b).norm() / b.norm())
+        assert e <= 16 * 2.0**-8, (k, e)
+
+
+def test_unknown_rule_is_refused():
+    with pytest.raises(ValueError):
+        finetune.Trainer(small(update="other"))
