@@ -55,8 +55,8 @@ typedef struct lors_projection {
  *
  * Scratch bytes of lors_gated_forward (without G and U) and, with backward != 0,
  * of lors_gated_backward: the two transposed masks, padded copies of B where r is
- * no multiple of 8, and dG and dU (L x R each).  (size_t)-1 if p is invalid for
- * the call.
+ * no multiple of 8, dG and dU (L x R each), and at most 64 MiB of fp32 partial sums of dX's
+ * tiles that are cut over their contraction.  (size_t)-1 if p is invalid for the call.
  */
 size_t lors_gated_workspace_bytes(const lors_problem_t* p, int backward);
 
