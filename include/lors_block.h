@@ -65,8 +65,9 @@ size_t lors_gated_workspace_bytes(const lors_problem_t* p, int backward);
  * rounded to the dtype, as in lors_forward.  G and U: where the projections'
  * results are kept for the backward, both or neither (LORS_ERR_NULL); NULL for
  * serving.  G and U are rounded once.  H is computed from their fp32 sums in
- * bf16 (in batches of tiles act(G) is rounded to bf16 before the product), and
- * from the stored G and U in fp32.  p->flags: 0, otherwise LORS_ERR_UNSUPPORTED.
+ * bf16 (in batches of tiles above rank 48 act(G) is rounded to bf16 before the
+ * product), and from the stored G and U in fp32.  p->flags: 0, otherwise
+ * LORS_ERR_UNSUPPORTED.
  */
 lors_status_t lors_gated_forward(const lors_problem_t* p, int32_t activation, const void* X,
                                  const lors_projection_t* gate, const lors_projection_t* up, void* G, void* U, void* H,

@@ -22,7 +22,8 @@ LIB = os.path.join(PKG, "liblors.so")
 ARCH = "gfx950"
 SOURCES = ["abi.cpp", "fwd_bf16.hip", "fwd_thin_bf16.hip", "fwd_few_bf16.hip", "fwd24_bf16.hip", "dx_bf16.hip", "dx_thin_bf16.hip",
            "g_bf16.hip", "ste_bf16.hip", "f32_path.hip", "misc.hip",
-           "gated_fwd_bf16.hip", "gated_fwd_thin_bf16.hip", "gated_fwd_few_bf16.hip", "gated_dx_bf16.hip", "gated_dx_thin_bf16.hip",
+           "gated_fwd_bf16.hip", "gated_fwd_thin_bf16.hip", "gated_pair_fwd_bf16.hip",
+           "gated_pair_fwd_thin_bf16.hip", "gated_fwd_few_bf16.hip", "gated_dx_bf16.hip", "gated_dx_thin_bf16.hip",
            "gated_g_bf16.hip", "gated_act.hip", "block_abi.cpp", "update.hip", "sample.hip",
            "train_abi.cpp", "norm.hip", "dropout.hip", "embedding.hip", "preference.hip"]
 

@@ -32,8 +32,9 @@ lors_status_t check_gated(const lors_problem_t* p, int32_t activation, uint32_t 
     if (activation != LORS_ACT_SILU && activation != LORS_ACT_GELU) return LORS_ERR_UNSUPPORTED;
     if (st != LORS_OK) return st;
     if ((p->flags & ~flags) != 0u) return LORS_ERR_UNSUPPORTED;
-    // both projections' G tiles in one grid
-    if (2 * ((p->R + 255) / 256) * ((p->C + 255) / 256) > kMaxExtent) return LORS_ERR_UNSUPPORTED;
+    // both projections' tiles in one grid: the forward's, the adapters' gradients'
+    const int64_t rt = (p->R + 255) / 256;
+    if (2 * rt * ((p->C + 255) / 256) > kMaxExtent || 2 * rt * ((p->L + 255) / 256) > kMaxExtent) return LORS_ERR_UNSUPPORTED;
     return LORS_OK;
 }
 

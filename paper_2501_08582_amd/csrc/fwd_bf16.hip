@@ -48,14 +48,20 @@
 #include <cmath>
 #include <type_traits>
 
-// The units that instantiate the gated block's kernels define LORS_GATED.
+// The units that instantiate the gated block's kernels define LORS_GATED: 1, the two
+// projections' tiles one after the other; 2, side by side in one tile (see fwd_kernel).
 #ifdef LORS_GATED
 #define LORS_FIRST(name) name##_gate
 #define LORS_MORE , Gated pair
 #define LORS_PAIR , pair_of(a)
+#define LORS_FWD_FEW launch_gated_fwd_few_bf16
+#if LORS_GATED == 2
+#define LORS_FWD launch_gated_pair_fwd_bf16
+#define LORS_FWD_THIN launch_gated_pair_fwd_thin_bf16
+#else
 #define LORS_FWD launch_gated_fwd_bf16
 #define LORS_FWD_THIN launch_gated_fwd_thin_bf16
-#define LORS_FWD_FEW launch_gated_fwd_few_bf16
+#endif
 #else
 #define LORS_FIRST(name) name
 #define LORS_MORE
@@ -72,7 +78,14 @@ constexpr int NT = 256;
 constexpr int BM = 256;   // tokens per tile
 constexpr int BN = 256;   // output features per whole tile (64 per wave)
 constexpr int BK = 64;    // input features per K-step
+#if LORS_GATED == 2
+constexpr int kSides = 2;   // projections in a tile
+constexpr int kEarly = 13;
+#else
+constexpr int kSides = 1;
 constexpr int kEarly = 12;  // copies of a stage issued right after the barrier; the rest a sub-step later
+#endif
+constexpr int HN = BN / kSides;  // columns of the output a whole tile holds
 
 // TM: tokens per tile, NF: 32-feature blocks per wave -- BM and 2 for a whole
 // tile; a thin tile of a short last wave has half the features (NF = 1) and
@@ -83,17 +96,18 @@ struct Layout {
     static constexpr int XB = TM * kRow64;        // X slab: TM rows of 64 k
     static constexpr int WB = FT * kRow64;        // W slab: FT rows of 64 k
     static constexpr int MB = FT * 2 * 4;         // 2 mask words per row of W
-    static constexpr int AB = 16 * RK * kRow64;   // A slab: 16*RK rows of 64 k
+    static constexpr int AB1 = 16 * RK * kRow64;  // A slab: 16*RK rows of 64 k, of each projection in the tile
+    static constexpr int AB = kSides * AB1;
     static constexpr int X = 0, W = XB, A = XB + WB, M = XB + WB + AB;
     static constexpr int STAGE = XB + WB + AB + MB;
-    static constexpr int PAD = 2 * RK % 4 ? 1024 : 0;  // target of the A slab's padding copies, where it has any
+    static constexpr int PAD = kSides == 1 && 2 * RK % 4 ? 1024 : 0;  // target of the A slab's padding copies, where it has any
     static constexpr int S = stages_that_fit(STAGE, 256 + PAD);
     static constexpr int LUT = S * STAGE;         // select table: 16 x 8 B
     static constexpr int SINK = LUT + 256;
     static constexpr int TOTAL = SINK + PAD;
     static constexpr int NX = TM / 32;            // X-slab copies per wave
     static constexpr int NWC = 4 * NF;            // W-slab copies per wave
-    static constexpr int NAW = (2 * RK + 3) / 4;  // A-slab copies per wave
+    static constexpr int NAW = kSides == 2 ? RK : (2 * RK + 3) / 4;  // A-slab copies per wave
     static constexpr int NMC = NF;                // mask copies per wave
     static constexpr int COPIES = NX + NWC + NAW + NMC;  // copies per wave per stage
     static constexpr int EARLY = COPIES < kEarly ? COPIES : kEarly;
@@ -119,8 +133,11 @@ struct Layout {
 // accumulators, merges 32 NF rows of W', and the MFMA slots, X reads and
 // merge pieces of the missing token and feature blocks drop out of the
 // schedule.
-// LORS_GATED: the two projections of a gated block (Gated, gated.hpp), whose tiles a
+// LORS_GATED 1: the two projections of a gated block (Gated, gated.hpp), whose tiles a
 // workgroup computes one after the other; see the epilogue.
+// LORS_GATED 2: a tile holds half as many columns of H, waves 0 and 1 form the gate's
+// features of them and waves 2 and 3 the up projection's: X is read once for both, and the sums
+// meet in LDS, unrounded.  Its stages hold two A slabs, which fit up to rank 48.
 template <int RK, bool KRAG, bool FOLD, int TM, int NF>
 __global__ __launch_bounds__(NT, 1) void fwd_kernel(
     const uint16_t* __restrict__ X, const uint16_t* __restrict__ LORS_FIRST(W),
@@ -155,7 +172,7 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
         work_coords(blockIdx.x, tiles_m, tiles_n, fwd_group_rows(tiles_m, tiles_n), n_full, split, (C + BK - 1) / BK, tm,
                     tn, kbeg, nk);
         m0 = (int64_t)tm * BM;
-        n0 = tn * BN;
+        n0 = tn * HN;
     } else {
         int u;
         thin_coords(blockIdx.x, tiles_m, tiles_n, fwd_group_rows(tiles_m, tiles_n), n_full, split, (SPAN / TM) * (2 / NF),
@@ -163,10 +180,21 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
         kbeg = 0;
         nk = (C + BK - 1) / BK;
         m0 = (int64_t)tm * SPAN + (int64_t)(u % (SPAN / TM)) * TM;
-        n0 = tn * BN + (u / (SPAN / TM)) * Lay::FT;
+        n0 = tn * HN + (u / (SPAN / TM)) * (Lay::FT / kSides);
         if (m0 >= L || n0 >= R) return;  // a part of an edge tile that holds no output
     }
-#ifdef LORS_GATED
+#if LORS_GATED == 2
+    const int side = wave >> 1, wside = wave & 1;  // the wave's projection, and its place there
+    const uint16_t* W = side == 0 ? W_gate : pair.W;
+    const uint32_t* Mp = side == 0 ? Mp_gate : pair.M;
+    const uint16_t* Bm = side == 0 ? Bm_gate : pair.B;
+    const uint16_t* Am = side == 0 ? Am_gate : pair.A;
+#else
+    constexpr int side = 0;
+    const int wside = wave;
+#endif
+    const int nback = side * (Lay::FT / kSides);  // a feature's row in the slabs, less its place in the tile
+#if LORS_GATED == 1
     // the projections of a gated block: the gate's tile, then the up projection's
 #pragma unroll 1
     for (int seg = 0; seg < 2; ++seg) {
@@ -178,7 +206,7 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
 #endif
     // last rows of the X and W slabs that exist
     const int lastm = (int)min(L - 1 - m0, (int64_t)(TM - 1));
-    const int lastn = min(R - 1 - n0, Lay::FT - 1);
+    const int lastn = min(R - 1 - n0, Lay::FT / kSides - 1);
     const int kofs = kbeg * BK;
     const int wpr = (C + 31) >> 5;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
@@ -193,7 +221,7 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
     bf16x8 bfr[NF][RK];
 #pragma unroll
     for (int nb = 0; nb < NF; ++nb) {
-        const int gn = n0 + 32 * NF * wave + 32 * nb + l32;
+        const int gn = n0 + 32 * NF * wside + 32 * nb + l32;
 #pragma unroll
         for (int c = 0; c < RK; ++c) {
             u32x4 v = zero_u32x4();
@@ -232,14 +260,15 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
     for (int q = 0; q < Lay::NWC; ++q) {
         const int row = 8 * (Lay::NWC * wave + q) + (lane >> 3);
         const int lc = (lane & 7) ^ ((row >> 1) & 7);
-        offW[q] = (uint32_t)((min(row, lastn) * C + 8 * lc) * 2);
+        offW[q] = (uint32_t)((min(row - nback, lastn) * C + 8 * lc) * 2);
     }
     // A slab: copy q of wave w is slab block 4q + w (rows 8 blk .. +7) when
-    // that block exists; rows at or past r read zeros
+    // that block exists (two projections: block 2q + w of the wave's own); rows at or
+    // past r read zeros
     const uint16_t* aptr[Lay::NAW];
 #pragma unroll
     for (int q = 0; q < Lay::NAW; ++q) {
-        const int row = 8 * (4 * q + wave) + (lane >> 3);
+        const int row = 8 * (4 / kSides * q + wside) + (lane >> 3);
         const int lc = (lane & 7) ^ tr64_swz(row);
         aptr[q] = Am + (int64_t)row * C + 8 * lc;
     }
@@ -248,7 +277,7 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
 #pragma unroll
     for (int q = 0; q < Lay::NMC; ++q) {
         const int e = 64 * (Lay::NMC * wave + q) + lane;
-        offM[q] = (uint32_t)((min(e >> 1, lastn) * wpr + (e & 1)) * 4);
+        offM[q] = (uint32_t)((min((e >> 1) - nback, lastn) * wpr + (e & 1)) * 4);
     }
     const uint16_t* Xt = uniform_ptr(X + m0 * C);
     const uint16_t* Wt = uniform_ptr(W + (int64_t)n0 * C);
@@ -267,19 +296,20 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
             } else {
                 const int row = 8 * blk + (lane >> 3);
                 const int lc = (lane & 7) ^ ((row >> 1) & 7);
-                const bool ok = (isx ? m0 + row < L : n0 + row < R) && k0 + 8 * lc < C;
-                const uint16_t* src = (isx ? Xt : Wt) + (int64_t)row * C + k0 + 8 * lc;
+                const int from = isx ? row : row - nback;
+                const bool ok = (isx ? m0 + from < L : n0 + from < R) && k0 + 8 * lc < C;
+                const uint16_t* src = (isx ? Xt : Wt) + (int64_t)from * C + k0 + 8 * lc;
                 copy16_to_lds(ok ? (const void*)src : (const void*)zsrc, dst);
             }
         } else if (j < Lay::NX + Lay::NWC + Lay::NAW) {
             // every wave issues NAW copies; those past the A slab go to the sink
-            const int q = j - Lay::NX - Lay::NWC, blk = 4 * q + wave;
+            const int q = j - Lay::NX - Lay::NWC, blk = 4 / kSides * q + wside;
             const bool has = blk < 2 * RK;
             const int row = 8 * blk + (lane >> 3);
             const int lc = (lane & 7) ^ tr64_swz(row);
             const bool ok = has && row < r && (!KRAG || k0 + 8 * lc < C);
             copy16_to_lds(ok ? (const void*)(aptr[q] + k0) : (const void*)zsrc,
-                          has ? sb + Lay::A + 1024 * blk : lds0 + Lay::SINK);
+                          has ? sb + Lay::A + Lay::AB1 * side + 1024 * blk : lds0 + Lay::SINK);
         } else {
             const int q = j - Lay::NX - Lay::NWC - Lay::NAW;
             const uint32_t dst = sb + Lay::M + 256 * (Lay::NMC * wave + q);
@@ -287,8 +317,9 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
                 copy4s_to_lds(uniform_ptr(Mt + (k0 >> 5)), offM[q], dst);
             } else {
                 const int e = 64 * (Lay::NMC * wave + q) + lane;
-                const bool ok = n0 + (e >> 1) < R && (k0 >> 5) + (e & 1) < wpr;
-                const uint32_t* src = Mt + (int64_t)(e >> 1) * wpr + (k0 >> 5) + (e & 1);
+                const int from = (e >> 1) - nback;
+                const bool ok = n0 + from < R && (k0 >> 5) + (e & 1) < wpr;
+                const uint32_t* src = Mt + (int64_t)from * wpr + (k0 >> 5) + (e & 1);
                 copy4_to_lds(ok ? (const void*)src : (const void*)zsrc, dst);
             }
         }
@@ -307,7 +338,7 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
             for (int t = 0; t < 2; ++t) {
                 const int row = 8 * (g >> 1) + 4 * t + (jj >> 2);
                 const int col = 32 * kb + 16 * (g & 1) + 4 * sig;
-                offAt[kb][t] = Lay::A + tr64_elem_off(row, col);
+                offAt[kb][t] = Lay::A + Lay::AB1 * side + tr64_elem_off(row, col);
             }
     }
     const int nrow0 = 32 * NF * wave + l32;
@@ -574,7 +605,59 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
 #endif
     constexpr int OW = 32 * NF;   // outputs per staged row
     constexpr int CH = OW / 8;    // 16-byte chunks per row
-#ifdef LORS_GATED
+#if LORS_GATED == 2
+    // Staged in fp32, in two halves where the tile has 256 tokens; waves w and w + 2
+    // then take half of the rows each of the features that w summed for the gate and
+    // w + 2 for the up projection, and write H = act(g) * u out of the unrounded sums.
+    constexpr int ROWS = TM == BM ? TM / 2 : TM;
+    static_assert(4 * ROWS * OW * 4 <= Lay::S * Lay::STAGE, "fp32 staging fits the stage buffers");
+    float* of = (float*)(smem + wave * (ROWS * OW * 4));
+    const float* og = (const float*)(smem + wside * (ROWS * OW * 4));
+    const float* ou = (const float*)(smem + (wside + 2) * (ROWS * OW * 4));
+#pragma unroll
+    for (int half = 0; half < TM / ROWS; ++half) {
+        if (half > 0) lds_barrier();  // the first half has been read
+#pragma unroll
+        for (int nb = 0; nb < NF; ++nb)
+#pragma unroll
+            for (int mb = 0; mb < ROWS / 32; ++mb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    of[(32 * mb + 8 * (v >> 2) + 4 * h + (v & 3)) * OW + 32 * nb + l32] =
+                        acc[ROWS / 32 * half + mb][nb][v];
+        lds_barrier();
+#pragma unroll 2
+        for (int it = 0; it < ROWS / 2 * CH / 64; ++it) {
+            const int row = ROWS / 2 * side + (64 / CH) * it + lane / CH, ch = lane % CH;
+            const int64_t gm = m0 + ROWS * half + row;
+            const int gn = n0 + OW * wside + 8 * ch;
+            float g[8], u[8];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                *(f32x4*)(g + 4 * q) = *(const f32x4*)(og + row * OW + 8 * ch + 4 * q);
+                *(f32x4*)(u + 4 * q) = *(const f32x4*)(ou + row * OW + 8 * ch + 4 * q);
+            }
+            if (gm < L && gn < R) {
+                const int64_t at = gm * R + gn;
+                u32x4 out;
+                if (pair.G != nullptr) {
+                    u32x4 g8, u8;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        g8[q] = pack_bf16x2(g[2 * q], g[2 * q + 1]);
+                        u8[q] = pack_bf16x2(u[2 * q], u[2 * q + 1]);
+                    }
+                    *(u32x4*)(pair.G + at) = g8;
+                    *(u32x4*)(pair.U + at) = u8;
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    out[q] = pack_bf16x2(activate(g[2 * q], pair.gelu) * u[2 * q], activate(g[2 * q + 1], pair.gelu) * u[2 * q + 1]);
+                *(u32x4*)(Y + at) = out;
+            }
+        }
+    }
+#elif LORS_GATED == 1
     // Staged in fp32, in two halves where the tile has 256 tokens, so that
     // the eight outputs of a lane's 16-byte stores are unrounded: the
     // gate's tile gives G (where it is kept) and act(g), the latter in H's
@@ -645,7 +728,7 @@ __global__ __launch_bounds__(NT, 1) void fwd_kernel(
         if (gm < L && gn < R) *(u32x4*)(Y + gm * R + gn) = v;
     }
 #endif
-#ifdef LORS_GATED
+#if LORS_GATED == 1
     }
 #endif
 }
@@ -681,7 +764,7 @@ template <int RK>
 hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
     if (a.two_four && a.sparse_mfma) return launch_fwd24_bf16(a, st);  // structured-sparse MFMA
     const int tiles_m = (int)((a.L + BM - 1) / BM);
-    const int tiles_n = (int)((a.R + BN - 1) / BN);
+    const int tiles_n = (int)((a.R + HN - 1) / HN);
     const int tiles = tiles_m * tiles_n;
     const bool krag = !fwd_fixed_copies(a.C);
     const bool fold = folds(a);
@@ -694,7 +777,7 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
     TailSplit sp{tiles, 1, tiles};
     if (a.split_ws != nullptr && !fwd_whole_tiles(a.L, a.R, a.C))
         sp = tail_split(tiles, (a.C + BK - 1) / BK, a.split_budget);
-    const ThinPlan tp = sp.split == 1 ? thin_plan(a.L, a.R) : ThinPlan{tiles, 0, 0};
+    const ThinPlan tp = sp.split == 1 ? thin_plan(a.L, (int64_t)kSides * a.R) : ThinPlan{tiles, 0, 0};
     float* part = sp.split > 1 ? (float*)a.split_ws : nullptr;
     // with thin tiles the whole-tile grid is exactly the first n_full tiles
     // (work_coords regroups ids over the tiles it is told the grid holds)
@@ -725,7 +808,7 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
 template <int RK, bool KRAG, bool FOLD, int TM>
 hipError_t launch_thin_tm(const LayerArgs& a, hipStream_t st, int first, int tail) {
     const int tiles_m = (int)((a.L + thin_span(TM) - 1) / thin_span(TM));
-    const int tiles_n = (int)((a.R + BN - 1) / BN);
+    const int tiles_n = (int)((a.R + HN - 1) / HN);
     hipLaunchKernelGGL((fwd_kernel<RK, KRAG, FOLD, TM, 1>), dim3(tail * (2 * thin_span(TM) / TM)), dim3(NT), 0, st,
                        (const uint16_t*)a.X, (const uint16_t*)a.W, a.M, (const uint16_t*)a.B,
                        (const uint16_t*)a.A, (const uint16_t*)a.bias, (uint16_t*)a.Y, a.L, (int)a.R, (int)a.C,
@@ -763,13 +846,23 @@ hipError_t launch_thin_rk(const LayerArgs& a, hipStream_t st, int first, int tai
 hipError_t LORS_FWD(const LayerArgs& a, hipStream_t st) {
     if (a.L == 0) return hipSuccess;
     if (!a.sparse_mfma && fwd_few_tokens(a.L, a.R, a.C)) return LORS_FWD_FEW(a, st);
+#if LORS_GATED == 1
+    if (a.r <= 48) return launch_gated_pair_fwd_bf16(a, st);
+    if (a.r <= 64) return launch_rk<4>(a, st);
+#else
     switch ((a.r + 15) / 16) {
         case 1: return launch_rk<1>(a, st);
         case 2: return launch_rk<2>(a, st);
         case 3: return launch_rk<3>(a, st);
+#if LORS_GATED != 2
         case 4: return launch_rk<4>(a, st);
+#endif
         default: break;
     }
+#endif
+#if LORS_GATED == 2
+    return hipErrorInvalidValue;
+#else
     if (a.r > 128) return hipErrorInvalidValue;  // the problem check caps r at 128
     // Ranks above 64: a wave has registers for the rank-r operands of one
     // 32-feature block only, so every tile runs as half-feature thin tiles.
@@ -782,6 +875,7 @@ hipError_t LORS_FWD(const LayerArgs& a, hipStream_t st) {
     for (int i = 0; i < n && e == hipSuccess; ++i)
         e = LORS_FWD_THIN(a, st, run[i].n_full, run[i].tail, run[i].tm);
     return e;
+#endif
 }
 
 #else
@@ -789,14 +883,18 @@ hipError_t LORS_FWD(const LayerArgs& a, hipStream_t st) {
 hipError_t LORS_FWD_THIN(const LayerArgs& a, hipStream_t st, int first, int tail, int tm) {
     if (tail <= 0) return hipSuccess;
     switch ((a.r + 15) / 16) {
+#if LORS_GATED != 1
         case 1: return launch_thin_rk<1>(a, st, first, tail, tm);
         case 2: return launch_thin_rk<2>(a, st, first, tail, tm);
         case 3: return launch_thin_rk<3>(a, st, first, tail, tm);
+#endif
+#if LORS_GATED != 2
         case 4: return launch_thin_rk<4>(a, st, first, tail, tm);
         case 5: return launch_thin_rk<5>(a, st, first, tail, tm);
         case 6: return launch_thin_rk<6>(a, st, first, tail, tm);
         case 7: return launch_thin_rk<7>(a, st, first, tail, tm);
         case 8: return launch_thin_rk<8>(a, st, first, tail, tm);
+#endif
         default: return hipErrorInvalidValue;
     }
 }

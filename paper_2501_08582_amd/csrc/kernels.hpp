@@ -162,6 +162,8 @@ hipError_t launch_dbias_bf16(const LayerArgs& a, hipStream_t s);
 // projections; dB and dA are cleared by the dX launch (a.clear_grads) or the caller.
 hipError_t launch_gated_fwd_bf16(const LayerArgs& a, hipStream_t s);
 hipError_t launch_gated_fwd_thin_bf16(const LayerArgs& a, hipStream_t s, int first, int tail, int tm);
+hipError_t launch_gated_pair_fwd_bf16(const LayerArgs& a, hipStream_t s);  // ranks up to 48
+hipError_t launch_gated_pair_fwd_thin_bf16(const LayerArgs& a, hipStream_t s, int first, int tail, int tm);
 hipError_t launch_gated_fwd_few_bf16(const LayerArgs& a, hipStream_t s);
 hipError_t launch_gated_dx_bf16(const LayerArgs& a, hipStream_t s);
 hipError_t launch_gated_dx_thin_bf16(const LayerArgs& a, hipStream_t s, int ra, int first, int tail, int tm, bool clear);

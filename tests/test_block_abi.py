@@ -103,6 +103,7 @@ def test_gated_refusals_in_order(call):
     assert run() == _lib.ERR_ALIGN
     # 2^30 tiles of a projection are 2^31 of both together
     assert run(R=(1 << 31) - 256, C=129 * 256, L=1) == _lib.ERR_UNSUPPORTED
+    assert run(R=(1 << 31) - 256, C=64, L=129 * 256) == _lib.ERR_UNSUPPORTED
 
 
 def test_gated_alignment_of_every_pointer():
