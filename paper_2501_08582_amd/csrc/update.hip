@@ -185,7 +185,7 @@ template <int DT>
 constexpr int kTiles = DT * (DT + 1) / 2;
 // Columns of a lane in a turn of the first pass (the widest short side has registers for four).
 template <int DT>
-constexpr int kEach = DT == 8 ? 4 : 8;
+constexpr int kEach = DT >= 6 ? 4 : 8;
 
 // FULL: the turn's columns exist and rows are read in whole vectors (read_whole): every
 // lane loads, from the last row that exists where its own does not, and takes 0 instead.
@@ -301,7 +301,7 @@ __device__ __forceinline__ void gram_piece(const Matrix& x, const Rule& rule, in
 }
 
 template <int DT>
-__global__ __launch_bounds__(NT, DT == 8 ? 1 : 2) void gram_kernel(Source src, Rule rule, uint8_t* __restrict__ ws) {
+__global__ __launch_bounds__(NT, DT >= 6 ? 1 : 2) void gram_kernel(Source src, Rule rule, uint8_t* __restrict__ ws) {
     constexpr int G = kTiles<DT> < 8 ? kTiles<DT> : 8;  // tiles joined at a time
     __shared__ double red[NT / 64][G][256];
     int piece;
@@ -354,7 +354,12 @@ __global__ __launch_bounds__(NT) void sum_kernel(Source src, int entries, uint8_
 template <int DT>
 struct Square {
     static constexpr int D = 16 * DT;
-    static constexpr int PITCH = D + (DT > 1 ? 16 : 0);  // rows k, k + 1 on other banks
+    static constexpr int PITCH = D + (DT % 2 == 0 ? 16 : 0);  // rows k, k + 1 on other banks
+    // Element (row, col) of a left operand in LDS: the 16 columns of a tile in the order that
+    // the row's number gives, so that the writes of 16 rows' column (put) fall on 16 places as the
+    // reads of a row do.  (In one order for all rows the writes met on one bank: 4200 cycles of a
+    // product's 4300 at 64 x 64, 31000 of 30000 at 128 x 128.)
+    static __device__ __forceinline__ int at(int row, int col) { return row * PITCH + (col ^ (row & 15)); }
 };
 
 // L . B with L in LDS, transposed (put).  The matrices are symmetric but for rounding, and that
@@ -362,21 +367,33 @@ struct Square {
 // steps, against 2^-39).
 template <int DT>
 __device__ __forceinline__ void read_left(const double* L, int group, double (&l)[DT]) {
+    int lane = threadIdx.x & 63;
+    if constexpr (DT >= 6) asm volatile("" : "+v"(lane));  // the addresses anew each time: there are no registers for all of them
+    const double* row = L + Square<DT>::at(4 * group + (lane >> 4), lane & 15);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) l[t] = row[16 * t];
+}
+// The same of a matrix that stands in LDS row by row (apply_kernel, whose copy is written so).
+template <int DT>
+__device__ __forceinline__ void read_plain(const double* L, int group, double (&l)[DT]) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int t = 0; t < DT; ++t) l[t] = L[(4 * group + (lane >> 4)) * Square<DT>::PITCH + 16 * t + (lane & 15)];
 }
-// (The left operands of four columns of L are read while the products of the four before run; the
-// barriers keep the compiler from reading all of L ahead, for which there are no registers.)
+// (The left operands of four columns of L are read while the products of the four before run --
+// with six tiles and more a SIMD has a second wave for that, and no registers; the
+// barriers keep the compiler from reading all of L ahead, for which there are none either.)
 template <int DT>
 __device__ __forceinline__ void times(const double* L, const f64x4 (&B)[DT], f64x4 (&out)[DT]) {
+    constexpr bool AHEAD = DT < 6;
     double l[2][DT];
-    read_left<DT>(L, 0, l[0]);
+    if (AHEAD) read_left<DT>(L, 0, l[0]);
 #pragma unroll
     for (int t = 0; t < DT; ++t) out[t] = f64x4{0., 0., 0., 0.};
 #pragma unroll
     for (int g = 0; g < 4 * DT; ++g) {
-        if (g + 1 < 4 * DT) read_left<DT>(L, g + 1, l[(g + 1) & 1]);
+        if (!AHEAD) read_left<DT>(L, g, l[g & 1]);
+        else if (g + 1 < 4 * DT) read_left<DT>(L, g + 1, l[(g + 1) & 1]);
 #pragma unroll
         for (int t = 0; t < DT; ++t) out[t] = mfma64(l[g & 1][t], B[g >> 2][g & 3], out[t]);
         __builtin_amdgcn_sched_barrier(0);
@@ -389,7 +406,7 @@ __device__ __forceinline__ void put(double* L, const f64x4 (&B)[DT], int wave) {
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) L[(16 * wave + p) * Square<DT>::PITCH + 16 * t + 4 * v + h] = B[t][v];
+        for (int v = 0; v < 4; ++v) L[Square<DT>::at(16 * wave + p, 16 * t + 4 * v + h)] = B[t][v];
 }
 
 template <int DT>
@@ -398,8 +415,9 @@ constexpr int kStepThreads = 64 * DT < NT ? NT : 64 * DT;
 template <int DT>
 __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, double eps, double a, double b, double c, int steps,
                                                                   uint8_t* __restrict__ ws) {
-    constexpr int D = Square<DT>::D, PITCH = Square<DT>::PITCH, N = kStepThreads<DT>;
-    __shared__ double L[D * PITCH];
+    using Left = Square<DT>;
+    constexpr int D = Left::D, N = kStepThreads<DT>;
+    __shared__ double L[D * Left::PITCH];
     __shared__ double trace[2];
     const Matrix x = matrix_at(src, (int)blockIdx.x);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, p = lane & 15, h = lane >> 4;
@@ -410,13 +428,13 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, dou
         int t = 0, k = e >> 8;  // tile k is (t, u)
         while (k >= DT - t) k -= DT - t++;
         const int u = t + k, row = 16 * t + 4 * ((e >> 6) & 3) + ((e >> 4) & 3), col = 16 * u + (e & 15);
-        L[row * PITCH + col] = s;
-        if (t != u) L[col * PITCH + row] = s;
+        L[Left::at(row, col)] = s;
+        if (t != u) L[Left::at(col, row)] = s;
     }
     __syncthreads();
     if (wave == 0) {
-        double s = lane < D ? L[lane * PITCH + lane] : 0.;
-        if (D > 64) s += L[(D > 64 ? lane + 64 : 0) * PITCH + (D > 64 ? lane + 64 : 0)];
+        double s = lane < D ? L[Left::at(lane, lane)] : 0.;
+        if (D > 64 && lane + 64 < D) s += L[Left::at(lane + 64, lane + 64)];
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
         if (lane == 0) trace[0] = s;
@@ -424,12 +442,17 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, dou
     __syncthreads();
     const double inv = 1. / (sqrt(trace[0]) + eps);
     const bool works = wave < DT;
+    double* out = (double*)(ws + x.scratch) + pieces * (kTiles<DT> * 256);
+    auto at = [&](int t, int v) -> double& { return out[(16 * wave + p) * D + 16 * t + 4 * v + h]; };
+    // With six tiles and more the registers hold two matrices at a time: the product of the steps
+    // waits in its place of the scratch, where each lane reads what it wrote itself.
+    constexpr bool PARK = DT >= 6;
     f64x4 S[DT], Q[DT], W[DT];
     if (works) {
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) S[t][v] = L[(16 * t + 4 * v + h) * PITCH + 16 * wave + p] * inv * inv;
+            for (int v = 0; v < 4; ++v) S[t][v] = L[Left::at(16 * t + 4 * v + h, 16 * wave + p)] * inv * inv;
     }
     for (int k = 0; k < steps; ++k) {
         __syncthreads();  // every wave is done with the left operand
@@ -446,16 +469,32 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, dou
         __syncthreads();
         if (works) {
             put<DT>(L, W, wave);
-            if (k == 0)
+            if (k == 0) {
 #pragma unroll
-                for (int t = 0; t < DT; ++t) Q[t] = W[t];
+                for (int t = 0; t < DT; ++t) {
+                    Q[t] = W[t];
+                    if constexpr (PARK)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) at(t, v) = Q[t][v];
+                }
+            }
         }
         __syncthreads();
         if (works) {
             if (k > 0) {
+                if constexpr (PARK)
+#pragma unroll
+                    for (int t = 0; t < DT; ++t)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) Q[t][v] = at(t, v);
                 times<DT>(L, Q, W);
 #pragma unroll
-                for (int t = 0; t < DT; ++t) Q[t] = W[t];
+                for (int t = 0; t < DT; ++t) {
+                    Q[t] = W[t];
+                    if constexpr (PARK)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) at(t, v) = Q[t][v];
+                }
             }
             if (k + 1 < steps) {
                 times<DT>(L, S, W);
@@ -463,12 +502,11 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, dou
             }
         }
     }
-    double* out = (double*)(ws + x.scratch) + pieces * (kTiles<DT> * 256);
     if (works) {
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) out[(16 * wave + p) * D + 16 * t + 4 * v + h] = Q[t][v] * inv;
+            for (int v = 0; v < 4; ++v) at(t, v) = (PARK ? at(t, v) : Q[t][v]) * inv;
     }
 }
 
@@ -539,7 +577,7 @@ __device__ __forceinline__ void apply_turn(const Matrix& x, const Rule& rule, in
                 const Place at = run(k, n);
                 read_whole<float, E>(at_place(x.master, at), true, old[k]);
             }
-    constexpr int EG = DT == 8 ? 1 : DT == 4 ? 2 : 4;  // sets of columns at a time, for the registers
+    constexpr int EG = DT >= 6 ? 1 : DT >= 3 ? 2 : 4;  // sets of columns at a time, for the registers
 #pragma unroll
     for (int e0 = 0; e0 < 4; e0 += EG) {
         f64x4 o[EG][DT];
@@ -548,10 +586,10 @@ __device__ __forceinline__ void apply_turn(const Matrix& x, const Rule& rule, in
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[e][t] = f64x4{0., 0., 0., 0.};
         double l[2][DT];
-        read_left<DT>(L, 0, l[0]);
+        read_plain<DT>(L, 0, l[0]);
 #pragma unroll
         for (int g = 0; g < 4 * DT; ++g) {
-            if (g + 1 < 4 * DT) read_left<DT>(L, g + 1, l[(g + 1) & 1]);
+            if (g + 1 < 4 * DT) read_plain<DT>(L, g + 1, l[(g + 1) & 1]);
             double r[EG];
 #pragma unroll
             for (int e = 0; e < EG; ++e) r[e] = (double)v[g >> 2][g & 3][e0 + e];
@@ -574,7 +612,7 @@ __device__ __forceinline__ void apply_turn(const Matrix& x, const Rule& rule, in
 #pragma unroll
         for (int e = 0; e < E; ++e) value(k, e) *= x.rate;
     if (x.master != nullptr) {
-        constexpr int RUNS = WIDE ? 4 : DT == 8 ? 1 : 2;  // runs of the master in flight
+        constexpr int RUNS = WIDE ? 4 : DT >= 6 ? 1 : 2;  // runs of the master in flight
 #pragma unroll
         for (int k0 = 0; k0 < K; k0 += RUNS) {
             float before[RUNS][E];
@@ -630,7 +668,7 @@ __host__ __device__ inline bool whole_rows(bool wide, int64_t d, int64_t n, int 
 }
 
 template <int DT, bool WIDE, bool FULL>
-__global__ __launch_bounds__(NT, DT == 8 ? 1 : 2) void apply_kernel(Source src, Rule rule, int64_t cols, const uint8_t* __restrict__ ws) {
+__global__ __launch_bounds__(NT, DT >= 6 ? 1 : 2) void apply_kernel(Source src, Rule rule, int64_t cols, const uint8_t* __restrict__ ws) {
     constexpr int D = Square<DT>::D, PITCH = Square<DT>::PITCH;
     __shared__ __attribute__((aligned(16))) double L[D * PITCH];
     int piece;
@@ -649,7 +687,7 @@ __global__ __launch_bounds__(NT, DT == 8 ? 1 : 2) void apply_kernel(Source src, 
         apply_turn<DT, WIDE, FULL>(x, rule, jb, j1, L);
 }
 
-int blocks_of(int64_t d) { return d <= 16 ? 1 : d <= 32 ? 2 : d <= 64 ? 4 : 8; }
+int blocks_of(int64_t d) { return d <= 16 ? 1 : d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 96 ? 6 : 8; }
 
 // The chosen ones of the matrices, whose workgroups f counts, as a launch's source; `table` has
 // room for all of them.
@@ -732,7 +770,9 @@ hipError_t launch_update(const UpdateArgs& a, const Matrix* matrices, int64_t co
     t.first = (int*)(t.m + (table != nullptr ? count : 0));
     hipError_t e = launch_size<1>(a, matrices, count, t, s);
     if (e == hipSuccess) e = launch_size<2>(a, matrices, count, t, s);
+    if (e == hipSuccess) e = launch_size<3>(a, matrices, count, t, s);
     if (e == hipSuccess) e = launch_size<4>(a, matrices, count, t, s);
+    if (e == hipSuccess) e = launch_size<6>(a, matrices, count, t, s);
     if (e == hipSuccess) e = launch_size<8>(a, matrices, count, t, s);
     return e;
 }

@@ -45,7 +45,8 @@ def close(what, got, ref, slack=2.0**-25):
 # one, below a run of lanes, over a piece's end, and both orientations
 SHAPES = [(1, 1), (1, 700), (5, 1), (3, 3), (16, 64), (13, 517), (517, 13), (16, 4096), (17, 33), (32, 1000), (1000, 31), (33, 513),
           (64, 1024), (1500, 64), (63, 2051), (37, 5003), (5003, 37), (65, 200), (128, 1025), (1025, 128), (100, 777), (777, 101),
-          (128, 128), (2, 140001), (140001, 3)]
+          (128, 128), (2, 140001), (140001, 3),
+          (48, 1000), (1000, 48), (2051, 41), (41, 700), (96, 1031), (1031, 96), (90, 300), (300, 70), (49, 500), (97, 300)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
