@@ -142,7 +142,7 @@ typedef struct lors_update_item {
 size_t lors_orthogonal_workspace_bytes(const lors_update_t* p, const lors_update_item_t* items, int64_t count);
 
 /*
- * One step of `count` matrices (0 .. 2^20, otherwise LORS_ERR_SHAPE).  `items` is a
+ * One step of `count` matrices (0 .. 65535, otherwise LORS_ERR_SHAPE).  `items` is a
  * host array, read during the call.  m, master and param may not overlap anything
  * else of the call (the same array in two items: LORS_ERR_ALIAS).  Every result is a
  * function of the inputs alone, bit for bit; where a matrix's gradient holds an Inf

@@ -106,7 +106,7 @@ lors::LayerArgs second_alone(const lors::LayerArgs& a) {
 // ---------------------------------------------------------------------------
 // update
 // ---------------------------------------------------------------------------
-constexpr int64_t kMostMatrices = int64_t(1) << 20;
+constexpr int64_t kMostMatrices = 65535;  // of up to 256 workgroups each, 256 threads: below 2^32
 
 // Checks in the documented order, up to the range of the extents.
 lors_status_t check_update(const lors_update_t* p, const lors_update_item_t* items, int64_t count) {

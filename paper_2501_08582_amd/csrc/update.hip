@@ -161,13 +161,6 @@ __device__ __forceinline__ Matrix matrix_of(const Source& s, int block, int& pie
 }
 __device__ __forceinline__ Matrix matrix_at(const Source& s, int i) { return uniform(s.many ? s.table.m[i] : s.batch.m[i]); }
 
-__global__ __launch_bounds__(64) void table_kernel(Batch b, int at, Table t) {
-    const int i = threadIdx.x;
-    if (i >= b.count) return;
-    t.first[at + i] = b.first[i];
-    t.m[at + i] = b.m[i];
-}
-
 struct Rule {
     float beta, fresh;
     int nesterov, grad_bf16, param_bf16;
@@ -186,6 +179,14 @@ constexpr int kTiles = DT * (DT + 1) / 2;
 // Columns of a lane in a turn of the first pass (the widest short side has registers for four).
 template <int DT>
 constexpr int kEach = DT >= 6 ? 4 : 8;
+// The widest short side's 36 tiles are more than a wave's accumulators: there two waves read the
+// same columns, wave w takes the tiles of w's parity, and the even one stores m, once
+// both have read it.  (All 36 in one wave: 377 registers spilled; 128 x 4096 in
+// 96 us, against 29.)
+template <int DT>
+constexpr int kShare = DT == 8 ? 2 : 1;
+template <int DT>
+constexpr int kOwn = kTiles<DT> / kShare<DT>;
 
 // FULL: the turn's columns exist and rows are read in whole vectors (read_whole): every
 // lane loads, from the last row that exists where its own does not, and takes 0 instead.
@@ -219,7 +220,8 @@ __device__ __forceinline__ void read_grad(const void* p, bool bf16, const Place&
 }
 
 template <int DT, bool WIDE, bool FULL>
-__device__ __forceinline__ void gram_turn(const Matrix& x, const Rule& rule, int64_t jb, int64_t j1, f64x4 (&acc)[kTiles<DT>]) {
+__device__ __forceinline__ void gram_turn(const Matrix& x, const Rule& rule, int64_t jb, int64_t j1, f64x4 (&acc)[kOwn<DT>]) {
+    const int part = kShare<DT> == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kShare<DT>;
     const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 4;
     // run k of a lane: where it starts and how many of its elements exist
     constexpr int N = kEach<DT>, K = WIDE ? DT : N, E = WIDE ? N : DT;
@@ -266,35 +268,49 @@ __device__ __forceinline__ void gram_turn(const Matrix& x, const Rule& rule, int
                 m[k][e] = rule.moment(m[k][e], g[k][e]);
                 g[k][e] = rule.direction(m[k][e], g[k][e]);
             }
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            int n;
-            const Place at = run(k, n);
-            if (n > 0) write_some<float, E>(at_place(x.m, at), FULL ? E : n, m[k]);
+        if constexpr (kShare<DT> > 1) {  // the other wave has its m
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
         }
+        if (part == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                int n;
+                const Place at = run(k, n);
+                if (n > 0) write_some<float, E>(at_place(x.m, at), FULL ? E : n, m[k]);
+            }
     }
+    auto products = [&](auto part_tag) {
+        constexpr int PART = decltype(part_tag)::value;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        double v[DT];
+        for (int e = 0; e < N; ++e) {
+            double v[DT];
 #pragma unroll
-        for (int t = 0; t < DT; ++t) v[t] = (double)g[WIDE ? t : e][WIDE ? e : t];
-        int k = 0;
+            for (int t = 0; t < DT; ++t) v[t] = (double)g[WIDE ? t : e][WIDE ? e : t];
+            int k = 0;
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+            for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int u = t; u < DT; ++u, ++k) acc[k] = mfma64(v[t], v[u], acc[k]);
-    }
+                for (int u = t; u < DT; ++u, ++k)
+                    if (k % kShare<DT> == PART) acc[k / kShare<DT>] = mfma64(v[t], v[u], acc[k / kShare<DT>]);
+        }
+    };
+    if (part == 0) products(std::integral_constant<int, 0>{});
+    else products(std::integral_constant<int, kShare<DT> - 1>{});
 }
 
 // v of 4 N columns a turn: lane l holds, of row l % 16 of every block, the columns N (l / 16) + e
 // (wide) or 4 e + l / 16 (tall); any assignment does that is the same for every row.
 template <int DT, bool WIDE>
-__device__ __forceinline__ void gram_piece(const Matrix& x, const Rule& rule, int64_t j0, int64_t j1, f64x4 (&acc)[kTiles<DT>]) {
+__device__ __forceinline__ void gram_piece(const Matrix& x, const Rule& rule, int64_t j0, int64_t j1, f64x4 (&acc)[kOwn<DT>]) {
     const bool whole = WIDE ? x.n < (int64_t)1 << 26 : x.d % DT == 0;  // (a lane's own offset fits 32 bits)
     constexpr int C = 4 * kEach<DT>;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int SETS = NT / 64 / kShare<DT>;  // turns at a time; where they hold a barrier, all waves take as many
+    const int set = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kShare<DT>;
 #pragma unroll 1
-    for (int64_t jb = j0 + C * wave; jb < j1; jb += C * (NT / 64)) {
+    for (int64_t ja = j0; ja < j1; ja += C * SETS) {
+        const int64_t jb = ja + C * set;
+        if (kShare<DT> == 1 && jb >= j1) break;
         if (whole && jb + C <= j1) gram_turn<DT, WIDE, true>(x, rule, jb, j1, acc);
         else gram_turn<DT, WIDE, false>(x, rule, jb, j1, acc);
     }
@@ -302,43 +318,46 @@ __device__ __forceinline__ void gram_piece(const Matrix& x, const Rule& rule, in
 
 template <int DT>
 __global__ __launch_bounds__(NT, DT >= 6 ? 1 : 2) void gram_kernel(Source src, Rule rule, uint8_t* __restrict__ ws) {
-    constexpr int G = kTiles<DT> < 8 ? kTiles<DT> : 8;  // tiles joined at a time
+    constexpr int G = kOwn<DT> < 8 ? kOwn<DT> : 8;  // tiles joined at a time
+    constexpr int SHARE = kShare<DT>;
     __shared__ double red[NT / 64][G][256];
     int piece;
     const Matrix x = matrix_of(src, (int)blockIdx.x, piece);
     const int64_t cols = piece_cols(x.n), j0 = piece * cols, j1 = j0 + cols < x.n ? j0 + cols : x.n;
-    f64x4 acc[kTiles<DT>];
+    f64x4 acc[kOwn<DT>];
 #pragma unroll
-    for (int k = 0; k < kTiles<DT>; ++k) acc[k] = f64x4{0., 0., 0., 0.};
+    for (int k = 0; k < kOwn<DT>; ++k) acc[k] = f64x4{0., 0., 0., 0.};
     if (x.wide) gram_piece<DT, true>(x, rule, j0, j1, acc);
     else gram_piece<DT, false>(x, rule, j0, j1, acc);
     // the waves' sums, in wave order
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     double* out = (double*)(ws + x.scratch) + (int64_t)piece * (kTiles<DT> * 256);
 #pragma unroll
-    for (int k0 = 0; k0 < kTiles<DT>; k0 += G) {
+    for (int k0 = 0; k0 < kOwn<DT>; k0 += G) {
         if (k0 > 0) __syncthreads();
 #pragma unroll
         for (int k = 0; k < G; ++k)
-            if (k0 + k < kTiles<DT>)
+            if (k0 + k < kOwn<DT>)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) red[wave][k][64 * v + lane] = acc[k0 + k < kTiles<DT> ? k0 + k : 0][v];
+                for (int v = 0; v < 4; ++v) red[wave][k][64 * v + lane] = acc[k0 + k < kOwn<DT> ? k0 + k : 0][v];
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < G; ++k)
-            if (k0 + k < kTiles<DT>) {
-                double s = red[0][k][tid];
+            if (k0 + k < kOwn<DT>)
 #pragma unroll
-                for (int w = 1; w < NT / 64; ++w) s += red[w][k][tid];
-                out[(k0 + k) * 256 + tid] = s;
-            }
+                for (int q = 0; q < SHARE; ++q) {
+                    double s = red[q][k][tid];
+#pragma unroll
+                    for (int w = q + SHARE; w < NT / 64; w += SHARE) s += red[w][k][tid];
+                    out[(SHARE * (k0 + k) + q) * 256 + tid] = s;
+                }
     }
 }
 
 // The pieces' sum, in their order, into the first piece's place: one entry a thread.
 __global__ __launch_bounds__(NT) void sum_kernel(Source src, int entries, uint8_t* __restrict__ ws) {
-    const Matrix x = matrix_at(src, (int)blockIdx.y);
-    const int e = blockIdx.x * NT + threadIdx.x;
+    const Matrix x = matrix_at(src, (int)blockIdx.x);
+    const int e = blockIdx.y * NT + threadIdx.x;
     double* part = (double*)(ws + x.scratch) + e;
     const int64_t pieces = pieces_of(x.n);
     if (pieces == 1) return;
@@ -689,29 +708,52 @@ __global__ __launch_bounds__(NT, DT >= 6 ? 1 : 2) void apply_kernel(Source src, 
 
 int blocks_of(int64_t d) { return d <= 16 ? 1 : d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 96 ? 6 : 8; }
 
-// The chosen ones of the matrices, whose workgroups f counts, as a launch's source; `table` has
-// room for all of them.
-template <class Choose, class Count>
-Source collect(const Matrix* matrices, int64_t count, Table table, hipStream_t s, int& blocks, Choose choose, Count f) {
-    Source src{};
-    src.table = table;
-    for (int64_t i = 0; i < count; ++i) src.count += choose(matrices[i]) ? 1 : 0;
-    src.many = src.count > kBatch;
-    Batch& b = src.batch;
-    int at = 0;
-    blocks = 0;
-    for (int64_t i = 0; i < count; ++i) {
-        if (!choose(matrices[i])) continue;
-        b.m[b.count] = matrices[i];
-        b.first[b.count++] = blocks;
-        blocks += f(matrices[i]);
-        if (src.many && (b.count == kBatch || at + b.count == src.count)) {
-            hipLaunchKernelGGL(table_kernel, dim3(1), dim3(64), 0, s, b, at, table);
-            at += b.count;
-            b.count = 0;
+// The launches over one size's matrices: 0 the first pass, 1 + 2 (tall) + (edges) the second's.
+constexpr int kLaunches = 5;
+struct Plan {
+    int64_t cols[kLaunches];  // columns of a workgroup
+};
+// Columns that a launch takes of a matrix, and its workgroups there.
+template <int DT>
+__host__ __device__ inline int64_t cols_in(const Matrix& x, int launch) {
+    if (launch == 0) return x.n;
+    const bool wide = launch <= 2, full = launch % 2 == 1;
+    if ((x.wide != 0) != wide) return 0;
+    const bool whole = whole_rows(wide, x.d, x.n, DT);
+    return full ? (whole ? x.n / 64 * 64 : 0) : whole ? x.n % 64 : x.n;
+}
+template <int DT>
+__host__ __device__ inline int blocks_in(const Matrix& x, int launch, const Plan& plan) {
+    if (launch == 0) return (int)pieces_of(x.n);
+    return (int)((cols_in<DT>(x, launch) + plan.cols[launch] - 1) / plan.cols[launch]);
+}
+
+// The descriptors of more matrices than a batch holds go to the workspace, one wave for 60
+// of them, with every launch's first workgroups.
+constexpr int kUpload = 60;
+struct Upload {
+    int count, at, total;
+    int base[kLaunches];
+    Matrix m[kUpload];
+};
+static_assert(sizeof(Upload) + sizeof(Plan) + sizeof(Table) <= 4096, "kernel arguments");
+template <int DT>
+__global__ __launch_bounds__(64) void table_kernel(Upload u, Plan plan, Table t) {
+    const int i = threadIdx.x;
+    const bool have = i < u.count;
+    const Matrix x = u.m[have ? i : 0];
+    if (have) t.m[u.at + i] = x;
+#pragma unroll
+    for (int l = 0; l < kLaunches; ++l) {
+        const int own = have ? blocks_in<DT>(x, l, plan) : 0;
+        int upto = own;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(upto, o);
+            if (i >= o) upto += y;
         }
+        if (have) t.first[(int64_t)l * u.total + u.at + i] = u.base[l] + upto - own;
     }
-    return src;
 }
 
 // The matrices of one size of the short side.
@@ -719,39 +761,65 @@ template <int DT>
 hipError_t launch_size(const UpdateArgs& a, const Matrix* matrices, int64_t count, Table table, hipStream_t s) {
     const Rule rule{a.momentum, a.fresh, (int)a.nesterov, (int)a.grad_bf16, (int)a.param_bf16};
     auto mine = [](const Matrix& x) { return blocks_of(x.d) == DT; };
-    int blocks = 0;
-    const Source all = collect(matrices, count, table, s, blocks, mine, [](const Matrix& x) { return (int)pieces_of(x.n); });
-    if (all.count == 0) return hipSuccess;
-    hipLaunchKernelGGL((gram_kernel<DT>), dim3(blocks), dim3(NT), 0, s, all, rule, a.workspace);
-    hipLaunchKernelGGL(sum_kernel, dim3(kTiles<DT>, all.count), dim3(NT), 0, s, all, kTiles<DT> * 256, a.workspace);
-    hipLaunchKernelGGL((steps_kernel<DT>), dim3(all.count), dim3(kStepThreads<DT>), 0, s, all, a.eps, a.a, a.b, a.c, a.steps,
-                       a.workspace);
-    auto apply = [&](auto wide_tag, auto full_tag) {
-        constexpr bool WIDE = decltype(wide_tag)::value, FULL = decltype(full_tag)::value;
-        auto cols_of = [](const Matrix& x) {
-            const bool whole = whole_rows(WIDE, x.d, x.n, DT);
-            return FULL ? (whole ? x.n / 64 * 64 : 0) : whole ? x.n % 64 : x.n;
-        };
-        auto some = [&](const Matrix& x) { return mine(x) && (x.wide != 0) == WIDE && cols_of(x) > 0; };
-        // Columns of a workgroup: its copy of Q is worth several turns of them where there are
-        // workgroups enough.
-        int64_t turns = 0;
-        for (int64_t i = 0; i < count; ++i)
-            if (some(matrices[i])) turns += (cols_of(matrices[i]) + kPiece - 1) / kPiece;
-        if (turns == 0) return;
-        int64_t each = turns / 512;
+    int total = 0;
+    int64_t turns[kLaunches] = {};
+    for (int64_t i = 0; i < count; ++i) {
+        if (!mine(matrices[i])) continue;
+        ++total;
+        for (int l = 1; l < kLaunches; ++l) turns[l] += (cols_in<DT>(matrices[i], l) + kPiece - 1) / kPiece;
+    }
+    if (total == 0) return hipSuccess;
+    // Columns of a workgroup of the second pass: its copy of Q is worth several turns of them where
+    // there are workgroups enough.
+    Plan plan{};
+    for (int l = 1; l < kLaunches; ++l) {
+        int64_t each = turns[l] / 512;
         each = each < 1 ? 1 : each > 8 ? 8 : each;
-        while (turns / each + count > (int64_t)1 << 30) each *= 2;  // (they are counted in 32 bits)
-        const int64_t cols = each * kPiece;
-        int grid = 0;
-        const Source src = collect(matrices, count, table, s, grid, some,
-                                   [&](const Matrix& x) { return (int)((cols_of(x) + cols - 1) / cols); });
-        hipLaunchKernelGGL((apply_kernel<DT, WIDE, FULL>), dim3(grid), dim3(NT), 0, s, src, rule, cols, (const uint8_t*)a.workspace);
+        while (turns[l] / each + count > (int64_t)1 << 23) each *= 2;  // (a grid's threads are counted in 32 bits)
+        plan.cols[l] = each * kPiece;
+    }
+    Source src[kLaunches] = {};
+    int blocks[kLaunches] = {};
+    const bool many = total > kBatch;
+    Upload u{};
+    u.total = total;
+    for (int64_t i = 0, at = 0; i < count; ++i) {
+        if (!mine(matrices[i])) continue;
+        if (many) u.m[u.count++] = matrices[i];
+        for (int l = 0; l < kLaunches; ++l) {
+            if (!many) {
+                src[l].batch.m[at] = matrices[i];
+                src[l].batch.first[at] = blocks[l];
+            }
+            blocks[l] += blocks_in<DT>(matrices[i], l, plan);
+        }
+        ++at;
+        if (many && (u.count == kUpload || at == total)) {
+            u.at = (int)at - u.count;
+            hipLaunchKernelGGL((table_kernel<DT>), dim3(1), dim3(64), 0, s, u, plan, table);
+            for (int l = 0; l < kLaunches; ++l) u.base[l] = blocks[l];
+            u.count = 0;
+        }
+    }
+    for (int l = 0; l < kLaunches; ++l) {
+        src[l].table = Table{table.first + (many ? (int64_t)l * total : 0), table.m};
+        src[l].count = total;
+        src[l].many = many;
+    }
+    hipLaunchKernelGGL((gram_kernel<DT>), dim3(blocks[0]), dim3(NT), 0, s, src[0], rule, a.workspace);
+    hipLaunchKernelGGL(sum_kernel, dim3(total, kTiles<DT>), dim3(NT), 0, s, src[0], kTiles<DT> * 256, a.workspace);
+    hipLaunchKernelGGL((steps_kernel<DT>), dim3(total), dim3(kStepThreads<DT>), 0, s, src[0], a.eps, a.a, a.b, a.c, a.steps,
+                       a.workspace);
+    auto apply = [&](int l, auto wide_tag, auto full_tag) {
+        constexpr bool WIDE = decltype(wide_tag)::value, FULL = decltype(full_tag)::value;
+        if (blocks[l] > 0)
+            hipLaunchKernelGGL((apply_kernel<DT, WIDE, FULL>), dim3(blocks[l]), dim3(NT), 0, s, src[l], rule, plan.cols[l],
+                               (const uint8_t*)a.workspace);
     };
-    apply(std::true_type{}, std::true_type{});
-    apply(std::false_type{}, std::true_type{});
-    apply(std::true_type{}, std::false_type{});
-    apply(std::false_type{}, std::false_type{});
+    apply(1, std::true_type{}, std::true_type{});
+    apply(3, std::false_type{}, std::true_type{});
+    apply(2, std::true_type{}, std::false_type{});
+    apply(4, std::false_type{}, std::false_type{});
     return hipGetLastError();
 }
 
@@ -762,7 +830,7 @@ int64_t update_scratch(int64_t d, int64_t n) {
     return 8 * (pieces_of(n) * (dt * (dt + 1) / 2 * 256) + 256 * dt * dt);
 }
 
-int64_t update_table(int64_t count) { return count > kBatch ? count * (int64_t)(sizeof(Matrix) + sizeof(int)) : 0; }
+int64_t update_table(int64_t count) { return count > kBatch ? count * (int64_t)(sizeof(Matrix) + kLaunches * sizeof(int)) : 0; }
 
 hipError_t launch_update(const UpdateArgs& a, const Matrix* matrices, int64_t count, void* table, hipStream_t s) {
     Table t{};
