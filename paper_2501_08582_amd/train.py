@@ -539,7 +539,7 @@ class OrthogonalUpdate:
 
     with the direction of ``orthogonalize``.  ``masters`` and ``momenta`` are fp32 (momenta: zeros if
     not given) and changed in place; ``params``, of one type, receive the masters' values and may be
-    left out.  A step is one call, whatever the count: its launches are a few for each size of the
+    left out, or be the masters themselves where they are fp32.  A step is one call, whatever the count: its launches are a few for each size of the
     short side (up to 16, 32, 64, 128).  ``step`` may be captured into a graph; its scratch memory belongs to
     the object, so steps of one object must not overlap."""
 
@@ -559,7 +559,10 @@ class OrthogonalUpdate:
         self.weight_decay = float(weight_decay)
         self._device = _dev(self.masters[0])
         self._rule = (momentum, nesterov, coefficients, steps, eps)
-        kept = [0] * len(self.masters) if self.params is None else [t.data_ptr() for t in self.params]
+        kept = [0] * len(self.masters)
+        if self.params is not None:  # an fp32 parameter may be its own master
+            own = self.params[0].dtype == torch.float32
+            kept = [0 if own and q.data_ptr() == w.data_ptr() else q.data_ptr() for q, w in zip(self.params, self.masters)]
         self._items = (_lib.UpdateItem * len(self.masters))(*(
             (*w.shape, w.data_ptr(), m.data_ptr(), w.data_ptr(), q or None, 0.0, 0.0)
             for w, m, q in zip(self.masters, self.momenta, kept)))

@@ -147,6 +147,18 @@ def test_optimiser_steps(gdt, pdt, nesterov):
         assert opt.params is None
 
 
+def test_parameters_that_are_their_own_masters():
+    shapes = [(16, 300), (77, 9)]
+    grads, momenta, masters, _ = group(shapes, "f32", None)
+    twins = [w.clone() for w in masters], [m.clone() for m in momenta]
+    train.OrthogonalUpdate(masters, masters, momenta).step(grads, 0.1)
+    train.OrthogonalUpdate(twins[0], None, twins[1]).step(grads, 0.1)
+    assert all(torch.equal(a, b) for a, b in zip(masters + momenta, twins[0] + twins[1]))
+    with pytest.raises(_lib.LorsError):  # another's master is not its own
+        train.OrthogonalUpdate(masters[:1] + [twins[0][1]], [masters[0], masters[1][:, :].reshape(77, 9)],
+                               momenta[:1] + [masters[1]]).step(grads, 0.1)
+
+
 def test_momenta_start_at_zero_and_lr_changes():
     grads, _, masters, _ = group([(8, 40)], "f32", None)
     w0 = masters[0].clone()
