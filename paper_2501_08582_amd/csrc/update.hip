@@ -9,7 +9,9 @@
 // (all of them symmetric, and they commute, but for rounding):
 //   gram_kernel    m and v out of the gradient and the momentum; v v^T by pieces of the
 //                  long side
-//   steps_kernel   one workgroup a matrix: the pieces' sum, |v| out of its trace, the steps
+//   sum_kernel     the pieces' sum
+//   steps_kernel   one workgroup a matrix: |v| out of the trace, the steps (sides above 64:
+//                  start_kernel and product_kernel, a launch for each product)
 //   apply_kernel   v again, Q v, and the update of master and param
 //
 // Why 64 bits: S squares the singular values.  A direction of sigma = 2e-3 of |v|
@@ -20,8 +22,12 @@
 // operand of the k = 4v .. 4v + 3.  The matrices of the steps therefore never leave the
 // registers; only the left operands pass through LDS.
 //
-// Bound by HBM for many matrices: 10 bytes an element in the first pass (bf16 gradient), 16
-// in the second.  One matrix alone is bound by the steps' chain of products.
+// Bound by memory for many matrices: 10 bytes an element in the first pass (bf16 gradient: it,
+// m twice), 16 in the second (it, m, master twice, param).  112 adapters of rank 16 (7.7
+// million elements) take 87 us: 24.5 in the first pass, 5.6 + 7 in the sum and the
+// steps, 34 in the second pass, 7 for the descriptors.  Of rank 64 (50 million, 452 us): 147 (3.4 TB/s),
+// 15, 45, 254 (3.2 TB/s).  One matrix alone is bound by the steps' chain of products: 64 x 14336 takes 75 us, of which
+// 42 are the steps' 17 products of 64 x 64 (4096 cycles of one compute unit's matrix cores each: 29 us).
 #include <type_traits>
 
 #include "block_kernels.hpp"
@@ -376,8 +382,8 @@ struct Square {
     static constexpr int PITCH = D + (DT % 2 == 0 ? 16 : 0);  // rows k, k + 1 on other banks
     // Element (row, col) of a left operand in LDS: the 16 columns of a tile in the order that
     // the row's number gives, so that the writes of 16 rows' column (put) fall on 16 places as the
-    // reads of a row do.  (In one order for all rows the writes met on one bank: 4200 cycles of a
-    // product's 4300 at 64 x 64, 31000 of 30000 at 128 x 128.)
+    // reads of a row do.  (In one order for all rows the writes met on one bank: 4200 cycles at 64 x
+    // 64, as long as a product.)
     static __device__ __forceinline__ int at(int row, int col) { return row * PITCH + (col ^ (row & 15)); }
 };
 
@@ -386,8 +392,7 @@ struct Square {
 // steps, against 2^-39).
 template <int DT>
 __device__ __forceinline__ void read_left(const double* L, int group, double (&l)[DT]) {
-    int lane = threadIdx.x & 63;
-    if constexpr (DT >= 6) asm volatile("" : "+v"(lane));  // the addresses anew each time: there are no registers for all of them
+    const int lane = threadIdx.x & 63;
     const double* row = L + Square<DT>::at(4 * group + (lane >> 4), lane & 15);
 #pragma unroll
     for (int t = 0; t < DT; ++t) l[t] = row[16 * t];
@@ -399,20 +404,17 @@ __device__ __forceinline__ void read_plain(const double* L, int group, double (&
 #pragma unroll
     for (int t = 0; t < DT; ++t) l[t] = L[(4 * group + (lane >> 4)) * Square<DT>::PITCH + 16 * t + (lane & 15)];
 }
-// (The left operands of four columns of L are read while the products of the four before run --
-// with six tiles and more a SIMD has a second wave for that, and no registers; the
-// barriers keep the compiler from reading all of L ahead, for which there are none either.)
+// (The left operands of four columns of L are read while the products of the four before run; the
+// barriers keep the compiler from reading all of L ahead, for which there are no registers.)
 template <int DT>
 __device__ __forceinline__ void times(const double* L, const f64x4 (&B)[DT], f64x4 (&out)[DT]) {
-    constexpr bool AHEAD = DT < 6;
     double l[2][DT];
-    if (AHEAD) read_left<DT>(L, 0, l[0]);
+    read_left<DT>(L, 0, l[0]);
 #pragma unroll
     for (int t = 0; t < DT; ++t) out[t] = f64x4{0., 0., 0., 0.};
 #pragma unroll
     for (int g = 0; g < 4 * DT; ++g) {
-        if (!AHEAD) read_left<DT>(L, g, l[g & 1]);
-        else if (g + 1 < 4 * DT) read_left<DT>(L, g + 1, l[(g + 1) & 1]);
+        if (g + 1 < 4 * DT) read_left<DT>(L, g + 1, l[(g + 1) & 1]);
 #pragma unroll
         for (int t = 0; t < DT; ++t) out[t] = mfma64(l[g & 1][t], B[g >> 2][g & 3], out[t]);
         __builtin_amdgcn_sched_barrier(0);
@@ -428,14 +430,12 @@ __device__ __forceinline__ void put(double* L, const f64x4 (&B)[DT], int wave) {
         for (int v = 0; v < 4; ++v) L[Square<DT>::at(16 * wave + p, 16 * t + 4 * v + h)] = B[t][v];
 }
 
-template <int DT>
-constexpr int kStepThreads = 64 * DT < NT ? NT : 64 * DT;
 
 template <int DT>
-__global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, double eps, double a, double b, double c, int steps,
+__global__ __launch_bounds__(NT) void steps_kernel(Source src, double eps, double a, double b, double c, int steps,
                                                                   uint8_t* __restrict__ ws) {
     using Left = Square<DT>;
-    constexpr int D = Left::D, N = kStepThreads<DT>;
+    constexpr int D = Left::D, N = NT;
     __shared__ double L[D * Left::PITCH];
     __shared__ double trace[2];
     const Matrix x = matrix_at(src, (int)blockIdx.x);
@@ -453,7 +453,6 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, dou
     __syncthreads();
     if (wave == 0) {
         double s = lane < D ? L[Left::at(lane, lane)] : 0.;
-        if (D > 64 && lane + 64 < D) s += L[Left::at(lane + 64, lane + 64)];
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
         if (lane == 0) trace[0] = s;
@@ -462,10 +461,6 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, dou
     const double inv = 1. / (sqrt(trace[0]) + eps);
     const bool works = wave < DT;
     double* out = (double*)(ws + x.scratch) + pieces * (kTiles<DT> * 256);
-    auto at = [&](int t, int v) -> double& { return out[(16 * wave + p) * D + 16 * t + 4 * v + h]; };
-    // With six tiles and more the registers hold two matrices at a time: the product of the steps
-    // waits in its place of the scratch, where each lane reads what it wrote itself.
-    constexpr bool PARK = DT >= 6;
     f64x4 S[DT], Q[DT], W[DT];
     if (works) {
 #pragma unroll
@@ -488,32 +483,16 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, dou
         __syncthreads();
         if (works) {
             put<DT>(L, W, wave);
-            if (k == 0) {
+            if (k == 0)
 #pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    Q[t] = W[t];
-                    if constexpr (PARK)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) at(t, v) = Q[t][v];
-                }
-            }
+                for (int t = 0; t < DT; ++t) Q[t] = W[t];
         }
         __syncthreads();
         if (works) {
             if (k > 0) {
-                if constexpr (PARK)
-#pragma unroll
-                    for (int t = 0; t < DT; ++t)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) Q[t][v] = at(t, v);
                 times<DT>(L, Q, W);
 #pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    Q[t] = W[t];
-                    if constexpr (PARK)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) at(t, v) = Q[t][v];
-                }
+                for (int t = 0; t < DT; ++t) Q[t] = W[t];
             }
             if (k + 1 < steps) {
                 times<DT>(L, S, W);
@@ -525,7 +504,7 @@ __global__ __launch_bounds__(kStepThreads<DT>) void steps_kernel(Source src, dou
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) at(t, v) = (PARK ? at(t, v) : Q[t][v]) * inv;
+            for (int v = 0; v < 4; ++v) out[(16 * wave + p) * D + 16 * t + 4 * v + h] = Q[t][v] * inv;
     }
 }
 
@@ -708,6 +687,133 @@ __global__ __launch_bounds__(NT, DT >= 6 ? 1 : 2) void apply_kernel(Source src, 
 
 int blocks_of(int64_t d) { return d <= 16 ? 1 : d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 96 ? 6 : 8; }
 
+// The steps of sides above 64, whose products are 8 to 14 us of one compute unit's: each of
+// them a launch in which a wave takes a tile of the result, and the matrices in the
+// workspace.  P is a left operand alone and kept transposed, S in both forms, so that every
+// operand is read in rows of 16 doubles.  14 launches of 6 us in place of one of 333 for the five
+// steps; 128 x 4096 takes 160 us in place of 414.
+template <int DT>
+struct Wide {
+    static constexpr int D = 16 * DT;
+    double *q, *spare, *s, *st, *pt, *w, *inv;  // q: what apply_kernel reads
+    __device__ __forceinline__ Wide(uint8_t* ws, const Matrix& x) {
+        q = (double*)(ws + x.scratch) + pieces_of(x.n) * (kTiles<DT> * 256);
+        spare = q + D * D;
+        s = spare + D * D;
+        st = s + D * D;
+        pt = st + D * D;
+        w = pt + D * D;
+        inv = w + D * D;
+    }
+    static constexpr int64_t kDoubles = 6 * D * D + 2;
+};
+
+// S_0 out of the pieces' sum (tiles (t, u), t <= u, of 16 x 16 each).
+template <int DT>
+__global__ __launch_bounds__(NT) void start_kernel(Source src, double eps, uint8_t* __restrict__ ws) {
+    constexpr int D = 16 * DT;
+    const Matrix x = matrix_at(src, (int)blockIdx.x / DT);
+    const int panel = blockIdx.x % DT, tid = threadIdx.x, lane = tid & 63;
+    const Wide<DT> m(ws, x);
+    const double* part = (const double*)(ws + x.scratch);
+    auto entry = [&](int row, int col) {
+        const int i = row < col ? row : col, j = row < col ? col : row, t = i >> 4, u = j >> 4;
+        const int k = t * DT - t * (t - 1) / 2 + u - t;
+        // (within a diagonal tile the two halves differ by rounding alone: the upper one)
+        return part[256 * k + 16 * (i & 15) + (j & 15)];
+    };
+    double trace = entry(lane, lane);
+    if (lane + 64 < D) trace += entry(lane + 64, lane + 64);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) trace += __shfl_xor(trace, o);
+    const double inv = 1. / (sqrt(trace) + eps);
+    for (int e = tid; e < D * 16; e += NT) {
+        const int row = e >> 4, col = 16 * panel + (e & 15);
+        const double v = entry(row, col) * inv * inv;
+        m.s[row * D + col] = v;
+        m.st[row * D + col] = v;
+    }
+    if (panel == 0 && tid == 0) *m.inv = inv;
+}
+
+// Part of a step: 0  P = a I + b S + c S^2 (of the first step also Q), 1  Q <- P Q, or W = P S in
+// workgroups from `split` on, 2  S <- P W.  The last step's Q is divided by |v| and stands
+// transposed, a left operand's way.
+struct Step {
+    int part, first, last, split, odd;  // odd: Q comes from q and goes to spare
+    double a, b, c;
+};
+template <int DT>
+constexpr int kParts = DT * ((DT + 3) / 4);  // workgroups of a product: 16 columns and up to four tiles of rows each
+template <int DT>
+__global__ __launch_bounds__(NT) void product_kernel(Source src, Step step, uint8_t* __restrict__ ws) {
+    constexpr int D = 16 * DT;
+    int id = blockIdx.x;
+    const bool second = step.part == 1 && id >= step.split;
+    if (second) id -= step.split;
+    const Matrix x = matrix_at(src, id / kParts<DT>);
+    id %= kParts<DT>;
+    const Wide<DT> m(ws, x);
+    const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = 16 * (id % DT) + p, t = 4 * (id / DT) + wave;
+    if (t >= DT) return;
+    double* const from = step.odd ? m.q : m.spare;
+    double* const to = step.odd ? m.spare : m.q;
+    const double* left = (step.part == 0 ? m.st : m.pt) + 16 * t + p;
+    const double* right = (step.part == 0 || second ? m.s : step.part == 1 ? from : m.w) + col;
+    double l[4 * DT], r[4 * DT];
+#pragma unroll
+    for (int g = 0; g < 4 * DT; ++g) {
+        l[g] = left[(4 * g + h) * D];
+        r[g] = right[(4 * g + h) * D];
+    }
+    const double inv = step.last ? *m.inv : 1.;
+    __builtin_amdgcn_sched_barrier(0);  // all loads in flight together
+    f64x4 acc = {0., 0., 0., 0.}, other = {0., 0., 0., 0.};  // two chains, each product waits for its own
+#pragma unroll
+    for (int g = 0; g < 4 * DT; g += 2) {
+        acc = mfma64(l[g], r[g], acc);
+        other = mfma64(l[g + 1], r[g + 1], other);
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const int row = 16 * t + 4 * v + h;
+        double y = acc[v] + other[v];
+        if (step.part == 0) {
+            y = fma(step.c, y, fma(step.b, right[row * D], row == col ? step.a : 0.));
+            m.pt[col * D + row] = y;
+            if (step.first) to[step.last ? col * D + row : row * D + col] = y * inv;
+        } else if (step.part == 1) {
+            if (second) m.w[row * D + col] = y;
+            else to[step.last ? col * D + row : row * D + col] = y * inv;
+        } else {
+            m.s[row * D + col] = y;
+            m.st[col * D + row] = y;
+        }
+    }
+}
+
+template <int DT>
+void launch_steps(const UpdateArgs& a, const Source& src, hipStream_t s) {
+    if constexpr (DT <= 4) {
+        hipLaunchKernelGGL((steps_kernel<DT>), dim3(src.count), dim3(NT), 0, s, src, a.eps, a.a, a.b, a.c, a.steps, a.workspace);
+    } else {
+        const int panels = src.count * kParts<DT>;
+        hipLaunchKernelGGL((start_kernel<DT>), dim3(src.count * DT), dim3(NT), 0, s, src, a.eps, a.workspace);
+        for (int k = 0; k < a.steps; ++k) {
+            const bool first = k == 0, last = k + 1 == a.steps;
+            // Q after the last step stands in q, after the one before it in spare
+            Step step{0, first, last, first ? 0 : panels, (a.steps - 1 - k) % 2, a.a, a.b, a.c};
+            hipLaunchKernelGGL((product_kernel<DT>), dim3(panels), dim3(NT), 0, s, src, step, a.workspace);
+            step.part = 1;
+            const int products = (first ? 0 : 1) + (last ? 0 : 1);
+            if (products > 0) hipLaunchKernelGGL((product_kernel<DT>), dim3(products * panels), dim3(NT), 0, s, src, step, a.workspace);
+            step.part = 2;
+            if (!last) hipLaunchKernelGGL((product_kernel<DT>), dim3(panels), dim3(NT), 0, s, src, step, a.workspace);
+        }
+    }
+}
+
 // The launches over one size's matrices: 0 the first pass, 1 + 2 (tall) + (edges) the second's.
 constexpr int kLaunches = 5;
 struct Plan {
@@ -808,8 +914,7 @@ hipError_t launch_size(const UpdateArgs& a, const Matrix* matrices, int64_t coun
     }
     hipLaunchKernelGGL((gram_kernel<DT>), dim3(blocks[0]), dim3(NT), 0, s, src[0], rule, a.workspace);
     hipLaunchKernelGGL(sum_kernel, dim3(total, kTiles<DT>), dim3(NT), 0, s, src[0], kTiles<DT> * 256, a.workspace);
-    hipLaunchKernelGGL((steps_kernel<DT>), dim3(total), dim3(kStepThreads<DT>), 0, s, src[0], a.eps, a.a, a.b, a.c, a.steps,
-                       a.workspace);
+    launch_steps<DT>(a, src[0], s);
     auto apply = [&](int l, auto wide_tag, auto full_tag) {
         constexpr bool WIDE = decltype(wide_tag)::value, FULL = decltype(full_tag)::value;
         if (blocks[l] > 0)
@@ -827,7 +932,8 @@ hipError_t launch_size(const UpdateArgs& a, const Matrix* matrices, int64_t coun
 
 int64_t update_scratch(int64_t d, int64_t n) {
     const int64_t dt = blocks_of(d);
-    return 8 * (pieces_of(n) * (dt * (dt + 1) / 2 * 256) + 256 * dt * dt);
+    // (the steps of the wide sides keep six matrices and |v| there)
+    return 8 * (pieces_of(n) * (dt * (dt + 1) / 2 * 256) + (dt > 4 ? 6 * 256 * dt * dt + 2 : 256 * dt * dt));
 }
 
 int64_t update_table(int64_t count) { return count > kBatch ? count * (int64_t)(sizeof(Matrix) + kLaunches * sizeof(int)) : 0; }
