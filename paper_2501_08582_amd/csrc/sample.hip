@@ -12,6 +12,18 @@
 // Bins hold fixed-point sums, whose order of addition does not matter; the sums of pass 4
 // are fp64 in a fixed order.  A bin of more entries than are sorted at a time is cut again,
 // by those numbers.
+// Rows of bf16 (sample_values) need no sort: 11777 values hold every logit but those below
+// 2^-30 and from 2^16 on (rows with such take the passes above), so that
+//   A  counts each value's entries in LDS; from the counts, a weight per value (one exp each,
+//      not one an entry), the filters' border and how many entries of its value are kept
+//   B  sums the kept weights by runs, as pass 4, out of the table of weights
+// The row is read twice and sorted never.
+//
+// One workgroup a row, because the passes wait for each other: a second launch or a grid's
+// barrier costs what splitting a row would save.  Bound by that workgroup's own work: 131072
+// entries alone 37 us (about a third each of A, the border, B and the end), 256 such rows, one to a
+// compute unit, 49 (67 MB: 14 at a copy's rate); 37 rows of 50021 fp32 with top-p 59, whose fixed-point
+// sums take a 64-bit exp an entry, 46 with top-k alone.
 #include "block_kernels.hpp"
 #include "train_common.hpp"
 
@@ -120,26 +132,35 @@ struct Row {
     static constexpr int AHEAD = 4;  // units in flight in a lane
     const T* at;
     uint32_t V;
+    // Unit i of U entries, and how many of them exist.  One past the row reads the last whole
+    // unit: no load stands behind a branch, and all of a turn are in flight together.
+    __device__ __forceinline__ train::Raw<T, U> unit(uint32_t i, int& n) const {
+        const uint32_t units = V / U;
+        n = i < units ? U : i == units ? (int)(V % U) : 0;
+        if (units == 0) return train::Raw<T, U>{};
+        return train::load_whole<T, U>(at + (uint64_t)(i < units ? i : units - 1) * U);
+    }
+    // (the row's last, where it is not whole)
+    __device__ __forceinline__ void edge(int n, train::Raw<T, U>& raw) const {
+        if (n > 0 && n < U) raw = train::load_unit<T, U>(at + (uint64_t)(V / U) * U, n);
+    }
     // f(logit, index, whether it exists) over the elements of this thread, every lane of a
     // wave at the same time
     template <class F>
     __device__ __forceinline__ void each(F f) const {
-        const uint32_t wave0 = (threadIdx.x & ~63u) * U;
-        for (uint64_t i0 = 0; i0 + wave0 < V; i0 += (uint64_t)AHEAD * NT * U) {
+        const uint32_t wave0 = threadIdx.x & ~63u, all = (V + U - 1) / U;
+        for (uint32_t i0 = 0; i0 + wave0 < all; i0 += AHEAD * NT) {
             train::Raw<T, U> raw[AHEAD];
             int n[AHEAD];
 #pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
-                const uint64_t i = i0 + (uint64_t)(q * NT + threadIdx.x) * U;
-                n[q] = i < V ? (V - i < U ? (int)(V - i) : U) : 0;
-                raw[q] = train::load_unit<T, U>(n[q] ? at + i : at, n[q]);
-            }
+            for (int q = 0; q < AHEAD; ++q) raw[q] = unit(i0 + q * NT + threadIdx.x, n[q]);
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q) {
-                const uint64_t i = i0 + (uint64_t)(q * NT + threadIdx.x) * U;
+                const uint32_t i = (i0 + q * NT + threadIdx.x) * U;  // (of one that exists: below 2^31)
+                edge(n[q], raw[q]);
                 const train::F<U> z = train::widen<T, U>(raw[q]);
 #pragma unroll
-                for (int e = 0; e < U; ++e) f(z.v[e], (uint32_t)i + e, e < n[q]);
+                for (int e = 0; e < U; ++e) f(z.v[e], i + e, e < n[q]);
             }
         }
     }
@@ -398,9 +419,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
     };
     // this lane's U elements of a block, and their weights
     auto load = [&](uint64_t block, int& m) {
-        const uint64_t i = (block * 64 + lane) * U;
-        m = i < row.V ? (row.V - i < U ? (int)(row.V - i) : U) : 0;
-        return train::load_unit<T, U>(m ? row.at + i : row.at, m);
+        train::Raw<T, U> raw = row.unit((uint32_t)(block * 64 + lane), m);
+        row.edge(m, raw);
+        return raw;
     };
     auto weigh = [&](const train::Raw<T, U>& raw, int m, uint64_t block, double (&w)[U]) {
         const train::F<U> z = train::widen<T, U>(raw);
@@ -414,12 +435,13 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
             int m[AHEAD];
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q) {
-                const int r = r0 + q * kWaves;
-                raw[q] = load(r < runs ? (uint64_t)r * reps + b : blocks, m[q]);
+                const uint32_t block = (r0 + q * kWaves) * reps + b;  // (of a run past the last: past the row)
+                raw[q] = row.unit(block * 64 + lane, m[q]);
             }
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q) {
                 double w[U];
+                row.edge(m[q], raw[q]);
                 weigh(raw[q], m[q], (uint64_t)(r0 + q * kWaves) * reps + b, w);
 #pragma unroll
                 for (int e = 0; e < U; ++e) sum[q] += w[e];
@@ -435,10 +457,11 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
     }
     __syncthreads();
     if (wave != 0) return;
-    // sums before each run: 16 consecutive ones a lane
+    // sums before each run: up to 16 consecutive ones a lane
+    const int per_lane = (runs + 63) / 64;
     double part = 0.;
-    for (int e = 0; e < kRuns / 64; ++e) {
-        const int r = lane * (kRuns / 64) + e;
+    for (int e = 0; e < per_lane; ++e) {
+        const int r = lane * per_lane + e;
         if (r < runs) part += s.runs[r];
     }
     double upto_lane = part;
@@ -454,8 +477,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
     double base = 0., run = __shfl_up(upto_lane, 1);
     if (lane == 0) run = 0.;
     double at_first = 0.;
-    for (int e = 0; e < kRuns / 64; ++e) {
-        const int r = lane * (kRuns / 64) + e;
+    for (int e = 0; e < per_lane; ++e) {
+        const int r = lane * per_lane + e;
         if (r >= runs) break;
         const double w = s.runs[r];
         if (w > 0.) positive = r;
@@ -629,7 +652,7 @@ __device__ __forceinline__ A sum_of_four(const A (&v)[4]) {
 // false (every thread): the row holds other values
 __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Values& s) {
     using R = Row<uint16_t>;
-    constexpr int U = R::U, AHEAD = 8, E = Values::kEach;
+    constexpr int U = R::U, AHEAD = 4, E = Values::kEach;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t V = (uint32_t)a.vocab;
     const uint16_t* at = (const uint16_t*)a.logits + n * a.row_stride;
@@ -643,6 +666,14 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
         const uint32_t lo = e & 2 ? raw.w[1] : raw.w[0], hi = e & 2 ? raw.w[3] : raw.w[2];
         return (e & 4 ? hi : lo) >> (16 * (e & 1)) & 0xFFFFu;
     };
+    // Units of U entries of the row that exist whole; loads past them read the last one, so that no load
+    // stands behind a branch and all of a turn are in flight together.
+    const uint32_t units = V / U, left = V % U;
+    if (units == 0) return false;
+    auto unit = [&](uint32_t i) {
+        const uint32_t from = i < units ? i : units - 1;
+        return train::load_whole<uint16_t, U>((const uint16_t*)((const uint8_t*)at + from * (uint32_t)(2 * U)));
+    };
     // ---- A
     for (int e = tid; e < Values::kCount; e += NT) s.count[e] = 0;
     if (tid == 0) {
@@ -652,19 +683,15 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
     }
     __syncthreads();
     bool odd = false;
-    for (uint64_t i0 = 0; i0 + (uint64_t)tid * U < V; i0 += (uint64_t)AHEAD * NT * U) {
+    for (uint32_t i0 = 0; i0 < units; i0 += AHEAD * NT) {
         train::Raw<uint16_t, U> raw[AHEAD];
-        int m[AHEAD];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) raw[q] = unit(i0 + q * NT + tid);
 #pragma unroll
         for (int q = 0; q < AHEAD; ++q) {
-            const uint64_t i = i0 + (uint64_t)(q * NT + tid) * U;
-            m[q] = i < V ? (V - i < U ? (int)(V - i) : U) : 0;
-            raw[q] = train::load_unit<uint16_t, U>(m[q] ? at + i : at, m[q]);
-        }
-#pragma unroll
-        for (int q = 0; q < AHEAD; ++q) {
+            if (i0 + q * NT + tid >= units) break;
             uint32_t bins[U / 2];
-            bool plain = m[q] == U;
+            bool plain = true;
 #pragma unroll
             for (int e = 0; e < U / 2; ++e) plain &= Values::bins_of(raw[q].w[e], bins[e]);
             if (plain) {
@@ -674,13 +701,18 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
                     atomicAdd(&s.count[bins[e] >> 16], 1u);
                 }
             } else {
-                for (int e = 0; e < m[q]; ++e) {
+                for (int e = 0; e < U; ++e) {
                     const int bin = Values::bin_of(bits_at(raw[q], e));
                     if (bin >= 0) atomicAdd(&s.count[bin], 1u);
                     odd |= bin == -2;
                 }
             }
         }
+    }
+    if (tid < left) {
+        const int bin = Values::bin_of(at[V - left + tid]);
+        if (bin >= 0) atomicAdd(&s.count[bin], 1u);
+        odd |= bin == -2;
     }
     if (odd) s.odd = 1;
     __syncthreads();
@@ -709,7 +741,9 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
     uint64_t count = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        w[e] = c[e] != 0 ? power_of_two(((double)Values::value_of(E * tid + e) - top) * rate) : 0.;
+        w[e] = 0.;
+        if (__ballot(c[e] != 0) != 0)  // (most waves' values are not in the row)
+            w[e] = c[e] != 0 ? power_of_two(((double)Values::value_of(E * tid + e) - top) * rate) : 0.;
         s.weight[E * tid + e] = w[e];
         mass += (double)c[e] * w[e];
         count += c[e];
@@ -810,17 +844,24 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
         double sum[BEHIND] = {};
         uint32_t ties[BEHIND] = {};
         for (uint32_t b = 0; b < reps; ++b) {
+            // (blocks past the row's, and those of runs past the last, have no unit)
+            auto index = [&](int q) { return ((r0 + q * kWaves) * reps + b) * 64u + lane; };
             train::Raw<uint16_t, U> raw[BEHIND];
-            int m[BEHIND];
+#pragma unroll
+            for (int q = 0; q < BEHIND; ++q) raw[q] = unit(index(q));
 #pragma unroll
             for (int q = 0; q < BEHIND; ++q) {
-                const int r = r0 + q * kWaves;
-                raw[q] = load(r < runs ? (uint64_t)r * reps + b : blocks, m[q]);
-            }
-#pragma unroll
-            for (int q = 0; q < BEHIND; ++q) {
+                const uint32_t i = index(q);
+                if (i >= units) {
+                    for (uint32_t e = 0; i == units && e < left; ++e) {
+                        const int bin = Values::bin_of(at[V - left + e]);
+                        if (bin >= 0) sum[q] += s.weight[bin];
+                        ties[q] += bin == border ? 1 : 0;
+                    }
+                    continue;
+                }
                 uint32_t bins[U / 2];
-                bool plain = m[q] == U;
+                bool plain = true;
 #pragma unroll
                 for (int e = 0; e < U / 2; ++e) plain &= Values::bins_of(raw[q].w[e], bins[e]);
                 if (plain) {
@@ -837,7 +878,7 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
 #pragma unroll
                         for (int e = 0; e < U; ++e) ties[q] += (int)(bins[e >> 1] >> (16 * (e & 1)) & 0xFFFFu) == border ? 1 : 0;
                 } else {
-                    for (int e = 0; e < m[q]; ++e) {
+                    for (int e = 0; e < U; ++e) {
                         const int bin = Values::bin_of(bits_at(raw[q], e));
                         if (bin >= 0) sum[q] += s.weight[bin];
                         ties[q] += bin == border ? 1 : 0;
@@ -855,10 +896,10 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
     }
     __syncthreads();
     if (wave != 0) return true;
-    // sums before each run: 16 consecutive ones a lane; a run's ties count while the quota lasts
-    constexpr int EACH = kRuns / 64;
+    // sums before each run: up to 16 consecutive ones a lane; a run's ties count while the quota lasts
+    const int each = (runs + 63) / 64;
     uint32_t tied = 0;
-    for (int e = 0; e < EACH; ++e) tied += lane * EACH + e < runs ? s.ties[Values::place(lane * EACH + e)] : 0;
+    for (int e = 0; e < each; ++e) tied += lane * each + e < runs ? s.ties[Values::place(lane * each + e)] : 0;
     uint64_t ties0 = tied;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -873,8 +914,8 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
     };
     double part = 0.;
     uint64_t t = ties0;
-    for (int e = 0; e < EACH; ++e)
-        if (lane * EACH + e < runs) part += of_run(lane * EACH + e, t);
+    for (int e = 0; e < each; ++e)
+        if (lane * each + e < runs) part += of_run(lane * each + e, t);
     double upto_lane = part;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -888,8 +929,8 @@ __device__ __forceinline__ bool sample_values(const SampleArgs& a, int64_t n, Va
     double at_first = 0.;
     uint64_t ties_first = 0, ties_last = 0;
     t = ties0;
-    for (int e = 0; e < EACH; ++e) {
-        const int r = lane * EACH + e;
+    for (int e = 0; e < each; ++e) {
+        const int r = lane * each + e;
         if (r >= runs) break;
         const uint64_t before = t;
         const double x = of_run(r, t);
