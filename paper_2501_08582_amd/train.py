@@ -540,8 +540,9 @@ class OrthogonalUpdate:
     with the direction of ``orthogonalize``.  ``masters`` and ``momenta`` are fp32 (momenta: zeros if
     not given) and changed in place; ``params``, of one type, receive the masters' values and may be
     left out, or be the masters themselves where they are fp32.  A step is one call, whatever the count: its launches are a few for each size of the
-    short side (up to 16, 32, 64, 128).  ``step`` may be captured into a graph; its scratch memory belongs to
-    the object, so steps of one object must not overlap."""
+    short side (up to 16, 32, 48, 64, 96, 128).  ``step`` may be captured into a graph, with the lr of
+    that call; its scratch memory belongs to the object, which the graph must not outlive, and steps of one
+    object must not overlap."""
 
     def __init__(self, masters: Sequence[torch.Tensor], params: Optional[Sequence[torch.Tensor]] = None,
                  momenta: Optional[Sequence[torch.Tensor]] = None, momentum: float = 0.95, nesterov: bool = True,
@@ -570,6 +571,7 @@ class OrthogonalUpdate:
         self._lr: Optional[float] = None
         p = self._descriptor(self.masters[0])
         self._ws = _workspace(_lib.orthogonal_workspace_bytes(p, self._items, len(self.masters)), self._device)
+        self._stream = _raw_stream(self._device.index)  # whose memory the workspace is
 
     def _descriptor(self, grad: torch.Tensor) -> _lib.Update:
         return _update(*self._rule, grad, self.masters[0] if self.params is None else self.params[0])
@@ -586,6 +588,8 @@ class OrthogonalUpdate:
             self._lr = lr
         for item, g in zip(items, grads):
             item.grad = g.data_ptr()
+        if _raw_stream(self._device.index) != self._stream and not torch.cuda.is_current_stream_capturing():
+            self._ws.record_stream(torch.cuda.current_stream(self._device))
         _run_update(self._descriptor(grads[0]), items, len(grads), self._ws, self._device)
 
 

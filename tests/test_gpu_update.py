@@ -200,7 +200,7 @@ def test_nothing_is_written_past_the_end(shape):
 
 
 def test_other_stream_and_graph_replays():
-    shapes = [(16, 700), (300, 64), (9, 9)]
+    shapes = [(16, 700), (300, 64), (9, 9), (100, 300)] + [(8, 40)] * 50  # every kind of launch
     grads, momenta, masters, params = group(shapes, "bf16", "bf16")
     twin = [[t.clone() for t in ts] for ts in (momenta, masters, params)]
     opt = train.OrthogonalUpdate(masters, params, momenta)
