@@ -1,8 +1,12 @@
 // The elementwise steps of a gated block: H = act(G) U where the projections ran one by
 // one (fp32), and the gradients of the projections' results,
 //   dG = dH U act'(G),  dU = dH act(G).
-// Bound by HBM: one pass, five arrays of 2 bytes an element in bf16.  A lane takes units
-// of 16 bytes, a grid's stride apart.
+// dG and dU are rounded to bf16 there, half a step each, because they are operands of
+// the matrix instructions that follow; everything before that rounding is fp32.
+// Bound by HBM: one pass, five arrays of 2 bytes an element in bf16 (4096 x 13824: 566 MB
+// in 91 us, 6.2 TB/s).  A lane takes units of 16 bytes, a grid's stride apart.  As
+// a pass of its own it is 4 % of the backward: dX's and the gradients' kernels both read the
+// results, in copies straight to LDS that compute nothing on the way.
 #include "gated.hpp"
 #include "train_common.hpp"
 

@@ -23,11 +23,12 @@
 // registers; only the left operands pass through LDS.
 //
 // Bound by memory for many matrices: 10 bytes an element in the first pass (bf16 gradient: it,
-// m twice), 16 in the second (it, m, master twice, param).  112 adapters of rank 16 (7.7
-// million elements) take 87 us: 24.5 in the first pass, 5.6 + 7 in the sum and the
-// steps, 34 in the second pass, 7 for the descriptors.  Of rank 64 (50 million, 452 us): 147 (3.4 TB/s),
-// 15, 45, 254 (3.2 TB/s).  One matrix alone is bound by the steps' chain of products: 64 x 14336 takes 75 us, of which
-// 42 are the steps' 17 products of 64 x 64 (4096 cycles of one compute unit's matrix cores each: 29 us).
+// m twice), 16 in the second (it, m, master twice, param).  112 adapters of rank 16 (10
+// million elements) take 86 us: 26 in the first pass (3.9 TB/s), 6 + 7 in the sum and the
+// steps, 35 in the second pass (4.6 TB/s), 7 for the descriptors.  Of rank 64 (50 million, 452 us): 147 (3.4 TB/s),
+// 15, 45, 254 (3.2 TB/s).  One matrix alone is bound by the steps' chain of products: 64 x 14336
+// takes 75 us, of which 42 are the steps' 17 products of 64 x 64 (4096 cycles of one
+// compute unit's matrix cores each: 29 us).
 #include <type_traits>
 
 #include "block_kernels.hpp"
