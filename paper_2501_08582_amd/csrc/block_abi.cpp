@@ -240,15 +240,14 @@ lors_status_t lors_gated_backward(const lors_problem_t* p, int32_t activation, c
     second.dY = dU;
     a.split_ws = ws.split ? static_cast<uint8_t*>(dU) + ws.grad : nullptr;
     hipError_t e = hipSuccess;
-    // the bf16 dX launch clears dB and dA of both projections for the atomics of the
-    // adapters' gradients
-    a.clear_grads = bf16 && dX != nullptr && L != 0;
-    if (!a.clear_grads) {
+    if (L == 0) {
         e = lors::launch_zero2_f32(dB_gate, R * r, dA_gate, r * C, s);
         if (e == hipSuccess) e = lors::launch_zero2_f32(dB_up, R * r, dA_up, r * C, s);
+        return from_hip(e);
     }
-    if (e != hipSuccess || L == 0) return from_hip(e);
-    e = lors::launch_gated_split(dH, G, U, dG, dU, L * R, second.gelu, bf16, s);
+    // which also clears dB and dA for the atomics of the adapters' gradients
+    const lors::Clear clear{{dB_gate, dA_gate, dB_up, dA_up}, {R * r, r * C, R * r, r * C}};
+    e = lors::launch_gated_split(dH, G, U, dG, dU, L * R, second.gelu, bf16, clear, s);
     if (bf16) {
         if ((p->flags & LORS_FLAG_REUSE_MASK_T) == 0u) {
             if (e == hipSuccess) e = lors::launch_mask_transpose(a.M, R, C, a.two_four, const_cast<uint32_t*>(a.Mt), s);

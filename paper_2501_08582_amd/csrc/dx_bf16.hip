@@ -156,10 +156,6 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
         for (int64_t t = (int64_t)blockIdx.x * NT + tid; t < nz0 + nz1; t += stride) {
             if (t < nz0) z0[t] = 0.f;
             else z1[t - nz0] = 0.f;
-#ifdef LORS_GATED
-            if (t < nz0) pair.dB[t] = 0.f;
-            else pair.dA[t - nz0] = 0.f;
-#endif
         }
     }
 

@@ -348,7 +348,7 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
     // up to rank 16 and 8 tokens, 16 features a workgroup whatever their count (11008 x 4096,
     // 1 / 4 / 16 tokens: 59.9 / 62.7 / 74.1 us against 65.9 / 66.6 / 70.5 with the larger
     // blocks, which win at rank 64 too)
-    if (a.L <= 8 && RK == 1) return launch<16, RK, 1>(a, st);
+    if (a.L <= 8 && RK == 1 && g16 < 1 << 22) return launch<16, RK, 1>(a, st);  // (a grid's threads: 32 bits)
 #endif
     if (a.L <= 16 && g16 <= cus) return launch<16, RK, 1>(a, st);
     if (a.L <= 32 && g16 <= cus) return launch<16, RK, 2>(a, st);

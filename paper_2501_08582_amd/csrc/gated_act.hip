@@ -10,6 +10,8 @@
 #include "gated.hpp"
 #include "train_common.hpp"
 
+#include <algorithm>
+
 namespace lors {
 namespace {
 
@@ -32,8 +34,12 @@ __global__ __launch_bounds__(NT) void join_kernel(const T* __restrict__ G, const
 template <typename T>
 __global__ __launch_bounds__(NT) void split_kernel(const T* __restrict__ dH, const T* __restrict__ G,
                                                    const T* __restrict__ U, T* __restrict__ dG, T* __restrict__ dU,
-                                                   int64_t n, int gelu) {
+                                                   int64_t n, int gelu, Clear clear) {
     constexpr int N = train::kUnit<T>;
+    // the adapters' gradients, which the kernels after this one add to
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        for (int64_t e = (int64_t)blockIdx.x * NT + threadIdx.x; e < clear.n[k]; e += (int64_t)gridDim.x * NT) clear.p[k][e] = 0.f;
     const int64_t step = (int64_t)gridDim.x * NT * N;
     for (int64_t e = ((int64_t)blockIdx.x * NT + threadIdx.x) * N; e < n; e += step) {
         const train::F<N> d = train::widen<T, N>(train::load_whole<T, N>(dH + e));
@@ -71,14 +77,17 @@ hipError_t launch_gated_join(const void* G, const void* U, void* H, int64_t n, b
 }
 
 hipError_t launch_gated_split(const void* dH, const void* G, const void* U, void* dG, void* dU, int64_t n, bool gelu,
-                              bool bf16, hipStream_t s) {
+                              bool bf16, const Clear& clear, hipStream_t s) {
     if (n == 0) return hipSuccess;
+    // few rows of wide projections have more to clear than to split
+    const int64_t zeros = clear.n[0] + clear.n[1] + clear.n[2] + clear.n[3];
+    const dim3 grid = grid_for(std::max(n, zeros), bf16 ? 8 : 4);
     if (bf16)
-        hipLaunchKernelGGL(split_kernel<uint16_t>, grid_for(n, 8), dim3(NT), 0, s, (const uint16_t*)dH, (const uint16_t*)G,
-                           (const uint16_t*)U, (uint16_t*)dG, (uint16_t*)dU, n, (int)gelu);
+        hipLaunchKernelGGL(split_kernel<uint16_t>, grid, dim3(NT), 0, s, (const uint16_t*)dH, (const uint16_t*)G,
+                           (const uint16_t*)U, (uint16_t*)dG, (uint16_t*)dU, n, (int)gelu, clear);
     else
-        hipLaunchKernelGGL(split_kernel<float>, grid_for(n, 4), dim3(NT), 0, s, (const float*)dH, (const float*)G,
-                           (const float*)U, (float*)dG, (float*)dU, n, (int)gelu);
+        hipLaunchKernelGGL(split_kernel<float>, grid, dim3(NT), 0, s, (const float*)dH, (const float*)G,
+                           (const float*)U, (float*)dG, (float*)dU, n, (int)gelu, clear);
     return hipGetLastError();
 }
 

@@ -170,8 +170,13 @@ hipError_t launch_gated_dx_thin_bf16(const LayerArgs& a, hipStream_t s, int ra, 
 hipError_t launch_gated_g_bf16(const LayerArgs& a, hipStream_t s);
 // H = act(G) U, and dG = dH U act'(G), dU = dH act(G): n elements
 hipError_t launch_gated_join(const void* G, const void* U, void* H, int64_t n, bool gelu, bool bf16, hipStream_t s);
+// (and zeros to four arrays)
+struct Clear {
+    float* p[4];
+    int64_t n[4];
+};
 hipError_t launch_gated_split(const void* dH, const void* G, const void* U, void* dG, void* dU, int64_t n, bool gelu,
-                              bool bf16, hipStream_t s);
+                              bool bf16, const Clear& clear, hipStream_t s);
 
 // fp32 path
 hipError_t launch_fwd_f32(const LayerArgs& a, hipStream_t s);
