@@ -135,3 +135,61 @@ def test_the_gated_model_s_gradients():
 def test_unknown_rule_is_refused():
     with pytest.raises(ValueError):
         finetune.Trainer(small(update="other"))
+
+
+def test_calls_on_several_streams_at_once():
+    """Each operator on a stream of its own, all in flight together, against one after the other."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+
+    def randn(*shape):
+        return torch.randn(shape, generator=g, device="cuda")
+
+    cfg = small(width=256, hidden=520)
+    gate, up = (finetune.Projection(cfg.hidden, cfg.width, cfg, g) for _ in range(2))
+    with torch.no_grad():
+        for q in (gate, up):
+            q.B.copy_(0.1 * randn(*q.B.shape))
+    pair = [tuple(t.detach() for t in q.parts()) for q in (gate, up)]
+    X, Xb = randn(3, 256).bfloat16(), randn(700, 256).bfloat16()
+    H, G, U = ops.gated_forward(Xb, *pair, cfg.scale, cfg.mask)
+    dH = randn(*H.shape).bfloat16()
+    grads = [randn(16, 3000), randn(900, 100), randn(60, 60)]
+    logits, u = 3 * randn(9, 40000), torch.rand(9, generator=g, device="cuda")
+    calls = [lambda: ops.gated_forward(X, *pair, cfg.scale, cfg.mask, save=False)[:1],
+             lambda: ops.gated_forward(Xb, *pair, cfg.scale, cfg.mask),
+             lambda: ops.gated_backward(dH, Xb, *pair, G, U, cfg.scale, cfg.mask)[:1],
+             lambda: train.orthogonalize(grads),
+             lambda: train.sample(logits, u, 0.9, 50, 0.95),
+             lambda: train.sample(logits.bfloat16(), u, 0.9, 0, 0.95, 0.01)]
+    want = [call() for call in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        got = []
+        for call, stream in zip(calls, streams):
+            with torch.cuda.stream(stream):
+                got.append(call())
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert all(torch.equal(x, y) for x, y in zip(a, b)), i
+
+
+def test_one_projection_in_both_places():
+    """H = act(G) G; its adapters' gradients are the sums of both places'."""
+    cfg = small()
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q = finetune.Projection(cfg.hidden, cfg.width, cfg, g)
+    with torch.no_grad():
+        q.B.copy_(0.1 * torch.randn(q.B.shape, generator=g, device="cuda"))
+    X = torch.randn((40, cfg.width), generator=g, device="cuda").bfloat16()
+    H = ops.lors_gated(X, q.parts(), q.parts(), cfg.scale, cfg.mask)
+    dH = torch.randn(H.shape, generator=g, device="cuda").bfloat16()
+    dB, dA = torch.autograd.grad(H, [q.B, q.A], dH)
+    args = tuple(t.detach() for t in q.parts())
+    H2, G, U = ops.gated_forward(X, args, args, cfg.scale, cfg.mask)
+    assert torch.equal(H, H2) and torch.equal(G, U)
+    _, first, second = ops.gated_backward(dH, X, args, args, G, U, cfg.scale, cfg.mask, grad_dtype=torch.float32)
+    for got, a, b in ((dB, first[0], second[0]), (dA, first[1], second[1])):
+        # each place's gradient is rounded to bf16, and their sum
+        bound = 2.0**-8 * (a.abs() + b.abs() + (a + b).abs()) * (1 + 2.0**-7) + 2.0**-20 * (a.abs().max() + b.abs().max())
+        assert ((got.float() - (a + b)).abs() <= bound).all()

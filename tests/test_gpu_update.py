@@ -60,9 +60,10 @@ def test_direction(shape, dtype):
 @pytest.mark.parametrize("steps,abc", [(1, ABC), (2, ABC), (10, ABC), (7, (1.5, -0.5, 0.0)), (30, (1.5, -0.5, 0.0)), (3, (2.0, -1.5, 0.5))])
 def test_steps_and_coefficients(steps, abc):
     rng = np.random.default_rng(steps)
-    x = matrix(rng, 24, 333, "f32")
-    # ten steps of slope 2 to 3 around their cycle raise 2^-53 to 2^-37 at most
-    close("direction", train.orthogonalize(x, steps=steps, coefficients=abc), ob.direction(f64(x), steps, *abc, 1e-7))
+    for shape in ((24, 333), (300, 40), (100, 333), (200, 90)):
+        x = matrix(rng, *shape, "f32")
+        # ten steps of slope 2 to 3 around their cycle raise 2^-53 to 2^-37 at most
+        close("direction", train.orthogonalize(x, steps=steps, coefficients=abc), ob.direction(f64(x), steps, *abc, 1e-7))
 
 
 def test_singular_values_come_near_one():
@@ -72,7 +73,7 @@ def test_singular_values_come_near_one():
     assert s.min() > 0.6 and s.max() < 1.3
 
 
-@pytest.mark.parametrize("shape", [(16, 300), (300, 64)])
+@pytest.mark.parametrize("shape", [(16, 300), (300, 64), (90, 300), (300, 128)])
 def test_rank_deficient_and_zero(shape):
     rng = np.random.default_rng(1)
     x = matrix(rng, *shape, "f32", rank=3)
@@ -172,7 +173,7 @@ def test_momenta_start_at_zero_and_lr_changes():
     assert torch.equal(masters[0], w1)
 
 
-@pytest.mark.parametrize("shape", [(16, 333), (333, 37), (64, 515)])
+@pytest.mark.parametrize("shape", [(16, 333), (333, 37), (64, 515), (100, 515), (333, 90)])
 def test_nothing_is_written_past_the_end(shape):
     """Every array at an odd place between others; the workspace to its last byte."""
     rows, cols = shape
