@@ -27,7 +27,7 @@
 // million elements) take 86 us: 26 in the first pass (3.9 TB/s), 6 + 7 in the sum and the
 // steps, 35 in the second pass (4.6 TB/s), 7 for the descriptors.  Of rank 64 (50 million, 452 us): 147 (3.4 TB/s),
 // 15, 45, 254 (3.2 TB/s).  One matrix alone is bound by the steps' chain of products: 64 x 14336
-// takes 75 us, of which 42 are the steps' 17 products of 64 x 64 (4096 cycles of one
+// takes 70 us, of which 42 are the steps' 17 products of 64 x 64 (4096 cycles of one
 // compute unit's matrix cores each: 29 us).
 #include <type_traits>
 
@@ -44,6 +44,7 @@ constexpr int NT = 256;
 constexpr int kBatch = 48;        // matrices whose descriptors are kernel arguments
 constexpr int kPiece = 256;       // least columns (along the long side) of a workgroup
 constexpr int kMostPieces = 256;
+constexpr int kNarrow = 96;       // at most as many pieces of the second pass in a launch take a quarter of their columns a turn
 
 struct Batch {
     int count;
@@ -513,22 +514,22 @@ __global__ __launch_bounds__(NT) void steps_kernel(Source src, double eps, doubl
 // the direction and the update
 // ---------------------------------------------------------------------------
 
-// 64 columns from jb on: lane l holds, of the rows p = 4c + l / 16 of every block, the
-// columns 4 (l % 16) + e (wide) or 16 e + l % 16 (tall).  Results come out where the
+// 16 EC columns from jb on: lane l holds, of the rows p = 4c + l / 16 of every block, the
+// columns EC (l % 16) + e (wide) or 16 e + l % 16 (tall).  Results come out where the
 // operands lay.  FULL as above; where there are registers for them (AHEAD), the
 // master's values are on their way during the products.
-template <int DT, bool WIDE, bool FULL>
+template <int DT, bool WIDE, bool FULL, int EC>
 __device__ __forceinline__ void apply_turn(const Matrix& x, const Rule& rule, int64_t jb, int64_t j1, const double* L) {
     const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 4;
-    float v[DT][4][4];  // [block][c][e]
+    float v[DT][4][EC];  // [block][c][e]
     // runs of E consecutive elements: (block k, c) over e, or column e = k over c and the block
-    constexpr int K = WIDE ? 4 * DT : 4, E = WIDE ? 4 : 4 * DT;
+    constexpr int K = WIDE ? 4 * DT : EC, E = WIDE ? EC : 4 * DT;
     auto run = [&](int k, int& n) -> Place {
         if constexpr (WIDE) {
             const int i0 = 16 * (k >> 2) + 4 * (k & 3), i = i0 + h;
-            const int64_t j = jb + 4 * p;
-            n = i < x.d ? (FULL ? 4 : most(j1 - j, 4)) : 0;
-            if (FULL) return {(i0 < x.d ? i0 * x.n : 0) + jb, (uint32_t)(h * x.n) + 4 * p};
+            const int64_t j = jb + EC * p;
+            n = i < x.d ? (FULL ? EC : most(j1 - j, EC)) : 0;
+            if (FULL) return {(i0 < x.d ? i0 * x.n : 0) + jb, (uint32_t)(h * x.n) + EC * p};
             return {n ? (int64_t)i * x.n + j : 0, 0};
         } else {
             const int64_t j = jb + 16 * k + p;
@@ -576,9 +577,9 @@ __device__ __forceinline__ void apply_turn(const Matrix& x, const Rule& rule, in
                 const Place at = run(k, n);
                 read_whole<float, E>(at_place(x.master, at), true, old[k]);
             }
-    constexpr int EG = DT >= 6 ? 1 : DT >= 3 ? 2 : 4;  // sets of columns at a time, for the registers
+    constexpr int EG = EC == 1 || DT >= 6 ? 1 : DT >= 3 ? 2 : 4;  // sets of columns at a time, for the registers
 #pragma unroll
-    for (int e0 = 0; e0 < 4; e0 += EG) {
+    for (int e0 = 0; e0 < EC; e0 += EG) {
         f64x4 o[EG][DT];
 #pragma unroll
         for (int e = 0; e < EG; ++e)
@@ -611,7 +612,7 @@ __device__ __forceinline__ void apply_turn(const Matrix& x, const Rule& rule, in
 #pragma unroll
         for (int e = 0; e < E; ++e) value(k, e) *= x.rate;
     if (x.master != nullptr) {
-        constexpr int RUNS = WIDE ? 4 : DT >= 6 ? 1 : 2;  // runs of the master in flight
+        constexpr int RUNS = WIDE ? 4 : EC == 1 || DT >= 6 ? 1 : 2;  // runs of the master in flight
 #pragma unroll
         for (int k0 = 0; k0 < K; k0 += RUNS) {
             float before[RUNS][E];
@@ -666,7 +667,7 @@ __host__ __device__ inline bool whole_rows(bool wide, int64_t d, int64_t n, int 
     return wide ? d % 4 == 0 && n < (int64_t)1 << 26 : d % (4 * dt) == 0;
 }
 
-template <int DT, bool WIDE, bool FULL>
+template <int DT, bool WIDE, bool FULL, int EC>
 __global__ __launch_bounds__(NT, DT >= 6 ? 1 : 2) void apply_kernel(Source src, Rule rule, int64_t cols, const uint8_t* __restrict__ ws) {
     constexpr int D = Square<DT>::D, PITCH = Square<DT>::PITCH;
     __shared__ __attribute__((aligned(16))) double L[D * PITCH];
@@ -682,8 +683,8 @@ __global__ __launch_bounds__(NT, DT >= 6 ? 1 : 2) void apply_kernel(Source src, 
     __syncthreads();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll 1
-    for (int64_t jb = j0 + 64 * wave; jb < j1; jb += 64 * (NT / 64))
-        apply_turn<DT, WIDE, FULL>(x, rule, jb, j1, L);
+    for (int64_t jb = j0 + 16 * EC * wave; jb < j1; jb += 16 * EC * (NT / 64))
+        apply_turn<DT, WIDE, FULL, EC>(x, rule, jb, j1, L);
 }
 
 int blocks_of(int64_t d) { return d <= 16 ? 1 : d <= 32 ? 2 : d <= 48 ? 3 : d <= 64 ? 4 : d <= 96 ? 6 : 8; }
@@ -692,7 +693,7 @@ int blocks_of(int64_t d) { return d <= 16 ? 1 : d <= 32 ? 2 : d <= 48 ? 3 : d <=
 // them a launch in which a wave takes a tile of the result, and the matrices in the
 // workspace.  P is a left operand alone and kept transposed, S in both forms, so that every
 // operand is read in rows of 16 doubles.  14 launches of 6 us in place of one of 333 for the five
-// steps; 128 x 4096 takes 160 us in place of 414.
+// steps; 128 x 4096 takes 141 us in place of 395.
 template <int DT>
 struct Wide {
     static constexpr int D = 16 * DT;
@@ -877,9 +878,16 @@ hipError_t launch_size(const UpdateArgs& a, const Matrix* matrices, int64_t coun
     }
     if (total == 0) return hipSuccess;
     // Columns of a workgroup of the second pass: its copy of Q is worth several turns of them where
-    // there are workgroups enough.
+    // there are workgroups enough; where they are few, a quarter of the columns a lane, since
+    // a turn's products are 7 us at side 64 (64 x 14336: 11.2 us against 16.5).
     Plan plan{};
+    bool narrow[kLaunches] = {};
     for (int l = 1; l < kLaunches; ++l) {
+        narrow[l] = turns[l] <= kNarrow;
+        if (narrow[l]) {
+            plan.cols[l] = kPiece / 4;
+            continue;
+        }
         int64_t each = turns[l] / 512;
         each = each < 1 ? 1 : each > 8 ? 8 : each;
         while (turns[l] / each + count > (int64_t)1 << 23) each *= 2;  // (a grid's threads are counted in 32 bits)
@@ -918,8 +926,11 @@ hipError_t launch_size(const UpdateArgs& a, const Matrix* matrices, int64_t coun
     launch_steps<DT>(a, src[0], s);
     auto apply = [&](int l, auto wide_tag, auto full_tag) {
         constexpr bool WIDE = decltype(wide_tag)::value, FULL = decltype(full_tag)::value;
-        if (blocks[l] > 0)
-            hipLaunchKernelGGL((apply_kernel<DT, WIDE, FULL>), dim3(blocks[l]), dim3(NT), 0, s, src[l], rule, plan.cols[l],
+        if (blocks[l] > 0 && narrow[l])
+            hipLaunchKernelGGL((apply_kernel<DT, WIDE, FULL, 1>), dim3(blocks[l]), dim3(NT), 0, s, src[l], rule, plan.cols[l],
+                               (const uint8_t*)a.workspace);
+        else if (blocks[l] > 0)
+            hipLaunchKernelGGL((apply_kernel<DT, WIDE, FULL, 4>), dim3(blocks[l]), dim3(NT), 0, s, src[l], rule, plan.cols[l],
                                (const uint8_t*)a.workspace);
     };
     apply(1, std::true_type{}, std::true_type{});
