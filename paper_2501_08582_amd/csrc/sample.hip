@@ -241,11 +241,11 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
             }
             return (int)((hi - q) >> shift);
         };
-        uint64_t total = 0;  // of what the filter before kept
         for (int filter = k != 0 ? 0 : 1; filter < (by_mass ? 2 : 1); ++filter) {
             // the border: of the entries in their order, the first k, or those before which
-            // less than `goal` lies.  The second filter needs no counts: bins of no
-            // weight hold nothing that it keeps.
+            // less than `goal` lies.  The first filter needs no weights (a 64-bit exp an entry: the
+            // second takes those of what the first kept), the second no counts: bins of
+            // no weight hold nothing that it keeps.
             const bool counts = filter == 0;
             const uint64_t from = last;
             lo = 0;
@@ -271,7 +271,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
                     if (!some || q < lo || q > hi || q < from) return;
                     const int b = bin_of(z, q, shift);
                     if (counts) atomicAdd(&s.count[b], 1u);
-                    if (by_mass) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)fixed(z));
+                    else atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)fixed(z));
                 });
                 __syncthreads();
                 const uint32_t c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1];
@@ -279,13 +279,11 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
                 uint64_t c = (uint64_t)c0 + c1, m = m0 + m1;
                 scan2(c, m, s);
                 if (filter == 1 && shift < 0) {  // the whole of what is kept so far
-                    if (k == 0) {
-                        __syncthreads();
-                        if (tid == NT - 1) s.found[2] = m;
-                        __syncthreads();
-                        total = s.found[2];
-                    }
-                    goal = p0 * (double)total;
+                    __syncthreads();
+                    if (tid == NT - 1) s.found[2] = m;
+                    __syncthreads();
+                    goal = p0 * (double)s.found[2];
+                    __syncthreads();
                 }
                 // the border's bin: the last that is not empty and in front of which too little lies
                 const uint64_t cb[2] = {count0 + c - c0 - c1, count0 + c - c1}, mb[2] = {mass0 + m - m0 - m1, mass0 + m - m1};
@@ -388,7 +386,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
             sort_list(s, listed);
             const uint64_t q = s.list[tid];
             const bool some = tid < (int)listed;
-            uint64_t c = some ? 1 : 0, m = some && by_mass ? fixed(logit_of((uint32_t)(q >> 32))) : 0;
+            uint64_t c = some ? 1 : 0, m = some && !counts ? fixed(logit_of((uint32_t)(q >> 32))) : 0;
             const uint64_t own = m;
             scan2(c, m, s);
             const bool in = some && (counts ? count0 + c - 1 < k : (double)(mass0 + m - own) < goal || mass0 + m - own == 0);
@@ -396,13 +394,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
             __syncthreads();
             if (in) atomicMax(&s.bin, tid);
             __syncthreads();
-            if (s.bin == tid) {
-                s.found[0] = q;
-                s.found[1] = mass0 + m;
-            }
+            if (s.bin == tid) s.found[0] = q;
             __syncthreads();
             last = s.found[0];
-            total = s.found[1];
             __syncthreads();
         }
     }
