@@ -26,12 +26,10 @@
 #ifdef LORS_GATED
 #define LORS_PAIR Gated
 #define LORS_PAIR_OF pair_of
-#define LORS_WIDE(FT, RK) (FT == 16 && RK > 1)
 #define LORS_FWD_FEW launch_gated_fwd_few_bf16
 #else
 #define LORS_PAIR Alone
 #define LORS_PAIR_OF alone_of
-#define LORS_WIDE(FT, RK) (FT == 16)
 #define LORS_FWD_FEW launch_fwd_few_bf16
 #endif
 
@@ -66,12 +64,10 @@ struct Cfg {
     // and a third block where it fits; FT = 32 two blocks, so that with NB = 1 two
     // workgroups share a CU where the registers allow (14336 x 4096, 32 tokens:
     // 44 us, against 49 with three blocks in flight and one workgroup).
-    // A gated block up to rank 16 takes 8 waves with FT = 16 as well: three blocks in
-    // flight, two workgroups to a CU.
     static constexpr bool XA = FT == 16 && MB <= 2;  // X is fetched ahead too (else inside its block: it is in L2)
     static constexpr int BLOCK = NB * (4 * WV + 2) + 8 * RK + (XA ? 4 * WV * MB : 0);
     static constexpr int OTHER = 56 + 4 * RC * NB + 2 * RK + NV * (MB * NB + 1) + (XA ? 0 : 4 * WV * MB);
-    static constexpr int NW = LORS_WIDE(FT, RK) && 2 * BLOCK + OTHER <= 128 ? 16 : 2 * BLOCK + OTHER <= 256 ? 8 : 4;
+    static constexpr int NW = FT == 16 && 2 * BLOCK + OTHER <= 128 ? 16 : 2 * BLOCK + OTHER <= 256 ? 8 : 4;
     static constexpr int SLOTS = FT == 16 && 3 * BLOCK + OTHER <= 2048 / NW ? 3 : 2;
     static constexpr int EU = FT == 32 && RK == 1 && MB == 1 && NB == 1 ? 4 : NW / 4;  // waves per SIMD
     static constexpr int RED = NW * NB * MB * NV * 64 * 4;    // the waves' partial sums (after the loop)
@@ -344,12 +340,6 @@ hipError_t launch_rk(const LayerArgs& a, hipStream_t st) {
     // 16 features per workgroup while that leaves at most one per CU, with
     // the smallest token block that takes all tokens
     const int64_t g16 = (a.R + 15) / 16, cus = device_cus();
-#ifdef LORS_GATED
-    // up to rank 16 and 8 tokens, 16 features a workgroup whatever their count (11008 x 4096,
-    // 1 / 4 / 16 tokens: 59.9 / 62.7 / 74.1 us against 65.9 / 66.6 / 70.5 with the larger
-    // blocks, which win at rank 64 too)
-    if (a.L <= 8 && RK == 1 && g16 < 1 << 22) return launch<16, RK, 1>(a, st);  // (a grid's threads: 32 bits)
-#endif
     if (a.L <= 16 && g16 <= cus) return launch<16, RK, 1>(a, st);
     if (a.L <= 32 && g16 <= cus) return launch<16, RK, 2>(a, st);
     if (g16 * ((a.L + 63) / 64) <= cus) return launch<16, RK, 4>(a, st);

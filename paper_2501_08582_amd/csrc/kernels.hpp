@@ -160,6 +160,20 @@ hipError_t launch_dbias_bf16(const LayerArgs& a, hipStream_t s);
 
 // Gated block (a.second): a.Y is H, a.dY the gradient of G.  dX is the sum over both
 // projections; dB and dA are cleared by the dX launch (a.clear_grads) or the caller.
+// Whether the gated block's forward takes the kernel for few tokens: where one projection's does
+// (above), but up to rank 48 its tiles, which hold both projections, are ahead sooner.  Thin
+// tiles take about 0.75 us a K-step whatever R is while their workgroups, of 64 columns of H
+// each, fit the CUs.  Few against tiles, 4096 columns, rank 16 (us): up to 32 tokens 8192 rows
+// 38 to 46 against 49, 11008 rows 63 to 77 against 56, 14336 rows 72 to 80 against 61; 64 tokens, 4096
+// rows 47 against 47, 8192 rows 66 against 51; 128 tokens, 2048 x 2048 26 against 27, 4096 rows 55
+// against 47, 2744 x 1032 15 against 21.
+inline bool gated_few_tokens(int64_t L, int64_t R, int64_t C, int64_t r) {
+    if (!fwd_few_tokens(L, R, C)) return false;
+    if (r > 48) return true;
+    const int64_t cus = device_cus(), wgs = (R + 63) / 64, rounds = (wgs + cus - 1) / cus;
+    if (L <= 32) return C <= 2048 || 16 * wgs <= 9 * cus * rounds;
+    return 4 * ((R + 31) / 32) * ((L + 63) / 64) <= 3 * cus;
+}
 hipError_t launch_gated_fwd_bf16(const LayerArgs& a, hipStream_t s);
 hipError_t launch_gated_fwd_thin_bf16(const LayerArgs& a, hipStream_t s, int first, int tail, int tm);
 hipError_t launch_gated_pair_fwd_bf16(const LayerArgs& a, hipStream_t s);  // ranks up to 48

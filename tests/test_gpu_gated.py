@@ -77,11 +77,11 @@ def near(what, got, ref, tol):
 
 
 # few tokens: odd counts, one feature group, several token blocks, ranks that fill no
-# matrix instruction.  Tiles: below one tile of everything, whole tiles and edges,
+# matrix instruction, and widths from which such a batch takes tiles.  Tiles: below one tile of everything, whole tiles and edges,
 # one short wave of thin tiles, half-feature tiles (ranks above 64), the whole-tile kernels
 # (more than half of a wave of 256), and whole waves followed by thin tiles.
 FEW = [(1, 8, 8, 1), (3, 136, 104, 5), (5, 72, 40, 3), (16, 4104, 72, 16), (32, 264, 136, 24), (32, 8264, 64, 40),
-       (33, 520, 192, 17), (100, 520, 72, 64), (200, 264, 200, 100), (7, 1032, 520, 128), (64, 2048, 128, 33)]
+       (33, 520, 192, 17), (4, 10000, 2056, 16), (32, 9280, 2112, 40), (64, 8192, 136, 16), (129, 3000, 72, 48), (100, 520, 72, 64), (200, 264, 200, 100), (7, 1032, 520, 128), (64, 2048, 128, 33)]
 TILES = [(576, 1024, 136, 24), (577, 1032, 200, 64), (768, 1024, 128, 16), (600, 1032, 192, 100), (1030, 520, 72, 128),
          (3328, 2560, 64, 16), (3328, 2560, 128, 64), (3300, 2552, 72, 33), (3299, 2560, 64, 48), (4352, 4096, 64, 31)]
 
