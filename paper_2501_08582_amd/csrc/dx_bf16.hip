@@ -175,11 +175,16 @@ __global__ __launch_bounds__(NT, 1) void dx_kernel(
         n0 = tn * BN;
     } else {
         int u;
-        thin_coords(blockIdx.x, tiles_m, tiles_n, GROUP_M, n_full, split, (SPAN / TM) * (2 / NF), tm, tn, u);
+#ifdef LORS_GATED
+        const int parts = token_parts(L, TM);
+#else
+        constexpr int parts = SPAN / TM;
+#endif
+        thin_coords(blockIdx.x, tiles_m, tiles_n, GROUP_M, n_full, split, parts * (2 / NF), tm, tn, u);
         kbeg = 0;
         nk = LORS_TERMS * ((R + BK - 1) / BK);
-        m0 = (int64_t)tm * SPAN + (int64_t)(u % (SPAN / TM)) * TM;
-        n0 = tn * BN + (u / (SPAN / TM)) * Lay::FT;
+        m0 = (int64_t)tm * SPAN + (int64_t)(u % parts) * TM;
+        n0 = tn * BN + (u / parts) * Lay::FT;
         if (m0 >= L || n0 >= C) return;  // a part of an edge tile that holds no output
     }
     // last row of the dY slab, last column chunk and last column that exist
@@ -747,7 +752,12 @@ hipError_t launch_thin_tm(const LayerArgs& a, hipStream_t st, int ra, int first,
     float* z0 = clear ? a.dB : nullptr;
     float* z1 = clear ? a.dA : nullptr;
     const int64_t nz0 = clear ? a.R * a.r_grad : 0, nz1 = clear ? a.r_grad * a.C : 0;
-    launch_tm<RK, KRAG, FOLD, TM, 1>(a, st, ra, tail * (2 * thin_span(TM) / TM), tiles_m, tiles_n, first, tail, nullptr,
+#ifdef LORS_GATED
+    const int parts = token_parts(a.L, TM);
+#else
+    const int parts = thin_span(TM) / TM;
+#endif
+    launch_tm<RK, KRAG, FOLD, TM, 1>(a, st, ra, tail * 2 * parts, tiles_m, tiles_n, first, tail, nullptr,
                                           z0, nz0, z1, nz1);
     return hipGetLastError();
 }

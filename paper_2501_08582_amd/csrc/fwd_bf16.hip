@@ -118,17 +118,6 @@ struct Layout {
 
 #define SLOT_END() __builtin_amdgcn_sched_barrier(0)
 
-#ifdef LORS_GATED
-// Token parts that a logical tile of a thin grid is cut into: of a batch below one tile only
-// those that hold tokens.  (Empty workgroups between those with work leave the latter on a part of
-// the CUs, to which they are dealt in turn: 64 tokens, 11008 x 4096, rank 16, 149 us
-// against 59.)
-__host__ __device__ inline int token_parts(int64_t L, int tm) {
-    const int64_t most = thin_span(tm) / tm, parts = (L + tm - 1) / tm;
-    return (int)(parts < most ? parts : most);
-}
-#endif
-
 // A^T slab (rank rows j of 64 k) in the tr64 layout: chunk c of row j is
 // stored at chunk c ^ tr64_swz(j), because the merge reads it with transposed
 // 4-row fragments (the X/W slabs' row-pair XOR would leave those reads 2-way

@@ -38,6 +38,15 @@ static inline GatedGrad grad_pair_of(const LayerArgs& a) {
     return {(const uint16_t*)q.dY, (const uint16_t*)q.W, q.Mt, (const uint16_t*)q.B, (const uint16_t*)q.A, q.dB, q.dA};
 }
 
+// Token parts that a logical tile of a thin grid is cut into: of a batch below one tile only
+// those that hold tokens.  (Empty workgroups between those with work leave the latter on a part of
+// the CUs, to which they are dealt in turn: 64 tokens, 11008 x 4096, rank 16, 149 us
+// against 59.)
+__host__ __device__ static inline int token_parts(int64_t L, int tm) {
+    const int64_t most = thin_span(tm) / tm, parts = (L + tm - 1) / tm;
+    return (int)(parts < most ? parts : most);
+}
+
 // tanh of the GELU's argument and that argument's slope.  tanh(x) = sign(x) (1 - e) / (1 + e)
 // with e = exp(-2|x|) <= 1: no overflow, and full relative accuracy where 1 - e has
 // it; below |x| = 1/16 the series x - x^3/3 + 2x^5/15 (the next term is 4e-8 of x)

@@ -105,7 +105,9 @@ BACK = [(1, 8, 8, 1), (5, 72, 40, 3), (64, 264, 136, 16), (65, 520, 200, 12), (2
         (4352, 64, 4096, 30), (130, 2560, 2560, 17),
         # dX's last wave cut over both projections' K-steps: three pieces a tile, the middle one
         # with steps of both (ragged, and whole tiles); six pieces behind a wave of whole tiles
-        (260, 1032, 10000, 5), (512, 1088, 10240, 64), (2100, 1032, 8200, 33)]
+        (260, 1032, 10000, 5), (512, 1088, 10240, 64), (2100, 1032, 8200, 33),
+        # thin tiles of a batch below one tile
+        (40, 1032, 520, 128), (64, 520, 3080, 16), (150, 264, 2056, 70)]
 
 
 @pytest.mark.parametrize("i,shape", list(enumerate(BACK)))
