@@ -486,19 +486,23 @@ def _update(momentum, nesterov, coefficients, steps, eps, grad, param) -> _lib.U
     return _lib.Update(momentum, eps, a, b, c, steps, int(bool(nesterov)), _dt(grad), _dt(param), 0)
 
 
-def _matrices(what: str, ts: Sequence[torch.Tensor], like: Optional[Sequence[torch.Tensor]] = None,
+def _matrices(what: str, ts: Sequence[torch.Tensor], shapes: Optional[Sequence[torch.Size]] = None,
               dtype: Optional[torch.dtype] = None) -> None:
-    """Contiguous matrices of one device and type, of the shapes of ``like``."""
-    if like is not None and len(ts) != len(like):
-        raise ValueError(f"{what}: expected {len(like)} matrices, got {len(ts)}")
+    """Contiguous matrices of one device and type, of the given shapes."""
+    if shapes is not None and len(ts) != len(shapes):
+        raise ValueError(f"{what}: expected {len(shapes)} matrices, got {len(ts)}")
     dtype = dtype or ts[0].dtype
-    index = (like or ts)[0].get_device()
+    index = ts[0].get_device()
     for i, t in enumerate(ts):
-        if t.dim() != 2 or t.dtype != dtype or (like is not None and t.shape != like[i].shape):
-            shape = tuple(like[i].shape) if like is not None else "a matrix"
+        if t.dim() != 2 or t.dtype != dtype or (shapes is not None and t.shape != shapes[i]):
+            shape = tuple(shapes[i]) if shapes is not None else "a matrix"
             raise ValueError(f"{what} {i}: expected {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
         if t.get_device() != index or index < 0 or not t.is_contiguous():
-            _dev((like or ts)[0], t)  # which says what is wrong
+            _dev(ts[0], t)  # which says what is wrong
+
+
+def _addresses(ts: Sequence[torch.Tensor]) -> List[int]:
+    return list(map(torch.Tensor.data_ptr, ts))
 
 
 def _run_update(p: _lib.Update, items, count: int, ws: Optional[torch.Tensor], dev: torch.device) -> None:
@@ -539,10 +543,13 @@ class OrthogonalUpdate:
 
     with the direction of ``orthogonalize``.  ``masters`` and ``momenta`` are fp32 (momenta: zeros if
     not given) and changed in place; ``params``, of one type, receive the masters' values and may be
-    left out, or be the masters themselves where they are fp32.  A step is one call, whatever the count: its launches are a few for each size of the
-    short side (up to 16, 32, 48, 64, 96, 128).  ``step`` may be captured into a graph, with the lr of
-    that call; its scratch memory belongs to the object, which the graph must not outlive, and steps of one
-    object must not overlap."""
+    left out, or be the masters themselves where they are fp32.  The three lists are the object's to read and
+    the caller's to change: a step works on the tensors that they hold then, wherever those
+    stand by then (a restored momentum, ``p.data = ...``), of the shapes and types of the first.
+    A step is one call, whatever the count: its launches are a few for each size of the
+    short side (up to 16, 32, 48, 64, 96, 128).  ``step`` may be captured into a graph, with the lr and the
+    tensors of that call; its scratch memory belongs to the object, which the graph must not outlive, and steps of
+    one object must not overlap."""
 
     def __init__(self, masters: Sequence[torch.Tensor], params: Optional[Sequence[torch.Tensor]] = None,
                  momenta: Optional[Sequence[torch.Tensor]] = None, momentum: float = 0.95, nesterov: bool = True,
@@ -551,27 +558,47 @@ class OrthogonalUpdate:
         self.masters: List[torch.Tensor] = list(masters)
         if not self.masters:
             raise ValueError("no matrices")
-        _matrices("master", self.masters, dtype=torch.float32)
         self.momenta = [torch.zeros_like(t) for t in self.masters] if momenta is None else list(momenta)
-        _matrices("momentum", self.momenta, self.masters, torch.float32)
         self.params = None if params is None else list(params)
-        if self.params is not None:
-            _matrices("param", self.params, self.masters)
         self.weight_decay = float(weight_decay)
-        self._device = _dev(self.masters[0])
         self._rule = (momentum, nesterov, coefficients, steps, eps)
-        kept = [0] * len(self.masters)
-        if self.params is not None:  # an fp32 parameter may be its own master
-            own = self.params[0].dtype == torch.float32
-            kept = [0 if own and q.data_ptr() == w.data_ptr() else q.data_ptr() for q, w in zip(self.params, self.masters)]
-        self._items = (_lib.UpdateItem * len(self.masters))(*(
-            (*w.shape, w.data_ptr(), m.data_ptr(), w.data_ptr(), q or None, 0.0, 0.0)
-            for w, m, q in zip(self.masters, self.momenta, kept)))
-        self._shape_rate = [math.sqrt(max(1.0, w.shape[0] / w.shape[1])) if w.numel() else 1.0 for w in self.masters]
-        self._lr: Optional[float] = None
+        _matrices("master", self.masters, dtype=torch.float32)
+        self._shapes = [t.shape for t in self.masters]
+        self._device = _dev(self.masters[0])
+        self._param_dtype = torch.float32 if not self.params else self.params[0].dtype
+        self._items = (_lib.UpdateItem * len(self.masters))()
+        self._bind()
         p = self._descriptor(self.masters[0])
         self._ws = _workspace(_lib.orthogonal_workspace_bytes(p, self._items, len(self.masters)), self._device)
         self._stream = _raw_stream(self._device.index)  # whose memory the workspace is
+        self._shape_rate = [math.sqrt(max(1.0, rows / cols)) for rows, cols in self._shapes]
+        self._lr: Optional[float] = None
+
+    def _kept(self) -> List[torch.Tensor]:
+        return [*self.masters, *self.momenta, *(self.params or ())]
+
+    def _bind(self) -> None:
+        """Takes the addresses of the tensors that the lists hold now."""
+        _matrices("master", self.masters, self._shapes, torch.float32)
+        _matrices("momentum", self.momenta, self._shapes, torch.float32)
+        if self.params is not None:
+            _matrices("param", self.params, self._shapes, self._param_dtype)
+        kept, n = self._kept(), len(self.masters)
+        at = _addresses(kept)
+        for t, where in zip(kept, at):
+            if t.device != self._device:
+                raise ValueError("all tensors must be on the same device")
+            if where == 0 and t.numel():
+                raise ValueError("a tensor's storage has been released")
+        for i, (item, (rows, cols), w, m) in enumerate(zip(self._items, self._shapes, at, at[n:])):
+            q = at[2 * n + i] if self.params is not None else 0
+            if q == w and self._param_dtype == torch.float32:  # an fp32 parameter may be its own master
+                q = 0
+            item.rows, item.cols, item.m, item.master, item.param = rows, cols, m, w, q or None
+            item.grad = w  # (of the workspace query; step sets it)
+        # what stands at these addresses stays there until others are taken, so that an address that
+        # is still the same is the same memory
+        self._held, self._at = [t.detach() for t in kept], at
 
     def _descriptor(self, grad: torch.Tensor) -> _lib.Update:
         return _update(*self._rule, grad, self.masters[0] if self.params is None else self.params[0])
@@ -579,7 +606,11 @@ class OrthogonalUpdate:
     def step(self, grads: Sequence[torch.Tensor], lr: float) -> None:
         """One step along the gradients (of the masters' shapes; all bf16 or all fp32)."""
         grads = list(grads)
-        _matrices("gradient", grads, self.masters)
+        _matrices("gradient", grads, self._shapes)
+        if grads[0].device != self._device:
+            raise ValueError("all tensors must be on the same device")
+        if _addresses(self._kept()) != self._at:
+            self._bind()
         items = self._items
         if lr != self._lr:
             decay = lr * self.weight_decay
