@@ -572,7 +572,7 @@ class OrthogonalUpdate:
         self._ws = _workspace(_lib.orthogonal_workspace_bytes(p, self._items, len(self.masters)), self._device)
         self._stream = _raw_stream(self._device.index)  # whose memory the workspace is
         self._shape_rate = [math.sqrt(max(1.0, rows / cols)) for rows, cols in self._shapes]
-        self._lr: Optional[float] = None
+        self._rates: Optional[Tuple[float, float]] = None  # the lr and weight decay that the items hold
 
     def _kept(self) -> List[torch.Tensor]:
         return [*self.masters, *self.momenta, *(self.params or ())]
@@ -604,7 +604,8 @@ class OrthogonalUpdate:
         return _update(*self._rule, grad, self.masters[0] if self.params is None else self.params[0])
 
     def step(self, grads: Sequence[torch.Tensor], lr: float) -> None:
-        """One step along the gradients (of the masters' shapes; all bf16 or all fp32)."""
+        """One step along the gradients (of the masters' shapes; all bf16 or all fp32), at the lr and the
+        ``weight_decay`` of the moment."""
         grads = list(grads)
         _matrices("gradient", grads, self._shapes)
         if grads[0].device != self._device:
@@ -612,11 +613,12 @@ class OrthogonalUpdate:
         if _addresses(self._kept()) != self._at:
             self._bind()
         items = self._items
-        if lr != self._lr:
-            decay = lr * self.weight_decay
+        rates = (float(lr), float(self.weight_decay))
+        if rates != self._rates:
+            lr, decay = rates[0], rates[0] * rates[1]
             for item, rate in zip(items, self._shape_rate):
                 item.rate, item.decay = lr * rate, decay
-            self._lr = lr
+            self._rates = rates
         for item, g in zip(items, grads):
             item.grad = g.data_ptr()
         if _raw_stream(self._device.index) != self._stream and not torch.cuda.is_current_stream_capturing():

@@ -1,6 +1,7 @@
 """What a step of the orthogonalised updates hands to the library, on the CPU: the call
 itself is replaced by one that records its descriptors, and tensors of host memory take the
 device's place."""
+import numpy as np
 import pytest
 import torch
 
@@ -95,3 +96,29 @@ def test_memory_at_an_address_that_a_step_uses_is_not_handed_out_again(calls):
     assert opt.momenta[0].data_ptr() != was
     opt.step(grads, 0.1)
     assert calls[-1][0]["m"] == opt.momenta[0].data_ptr()
+
+
+def rates(seen):
+    return [(item["rate"], item["decay"]) for item in seen[-1]]
+
+
+def test_the_weight_decay_may_change_at_one_lr(calls):
+    opt, grads = made()
+    opt.step(grads, 0.5)
+    tall = (50 / 3) ** 0.5
+    assert rates(calls) == [(0.5, 0.0), (0.5 * tall, 0.0)]
+    opt.weight_decay = 0.25
+    opt.step(grads, 0.5)
+    assert rates(calls) == [(0.5, 0.125), (0.5 * tall, 0.125)]
+
+
+@pytest.mark.parametrize("lr", [torch.tensor(0.5), np.array(0.5)])
+def test_a_learning_rate_changed_in_place(calls, lr):
+    opt, grads = made()
+    opt.weight_decay = 1.0
+    opt.step(grads, lr)
+    lr *= 0.5
+    opt.step(grads, lr)
+    assert rates(calls)[0] == (0.25, 0.25)
+    opt.step(grads, 0.25)
+    assert rates(calls)[0] == (0.25, 0.25)
