@@ -542,7 +542,7 @@ class OrthogonalUpdate:
         param   = master in the parameter's type
 
     with the direction of ``orthogonalize``.  ``masters`` and ``momenta`` are fp32 (momenta: zeros if
-    not given) and changed in place; ``params``, of one type, receive the masters' values and may be
+    not given) and changed in place, for autograd too; ``params``, of one type, receive the masters' values and may be
     left out, or be the masters themselves where they are fp32.  The three lists are the object's to read and
     the caller's to change: a step works on the tensors that they hold then, wherever those
     stand by then (a restored momentum, ``p.data = ...``), of the shapes and types of the first.
@@ -624,6 +624,8 @@ class OrthogonalUpdate:
         if _raw_stream(self._device.index) != self._stream and not torch.cuda.is_current_stream_capturing():
             self._ws.record_stream(torch.cuda.current_stream(self._device))
         _run_update(self._descriptor(grads[0]), items, len(grads), self._ws, self._device)
+        # autograd has to know: a graph that saved one of them must not be passed again
+        torch.autograd.graph.increment_version(self._kept())
 
 
 # ---------------------------------------------------------------------------

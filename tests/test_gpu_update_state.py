@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2501_08582_amd import train
+from paper_2501_08582_amd import ops, train
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,19 @@ def test_replaced_tensors_take_the_step_and_the_old_ones_keep_their_values():
     for got, want in zip((opt.masters, opt.params, opt.momenta), twins):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert all(torch.equal(a, b) for a, b in zip(old, kept))
+
+
+def test_a_graph_from_before_a_step_is_refused_after_it():
+    """The layer saves its adapters; their step must not give its second backward other ones."""
+    W = torch.randn(64, 32, device="cuda").bfloat16()
+    M = ops.mask_pack(torch.ones(64, 32, dtype=torch.bool, device="cuda"))
+    B, A = (torch.randn(s, device="cuda").bfloat16().requires_grad_(True) for s in ((64, 4), (4, 32)))
+    X = torch.randn(8, 32, device="cuda").bfloat16()
+    opt = train.OrthogonalUpdate([t.detach().float() for t in (B, A)], [t.detach() for t in (B, A)])
+    for call in (lambda: ops.lors_linear(X, W, M, B, A, 2.0), lambda: ops.lors_gated(X, (W, M, B, A), (W, M, B, A), 2.0)):
+        out = call().float().sum()
+        grads = torch.autograd.grad(out, [B, A], retain_graph=True)
+        opt.step(grads, 0.02)
+        with pytest.raises(RuntimeError, match="inplace operation"):
+            torch.autograd.grad(out, [B, A])
+        torch.autograd.grad(call().float().sum(), [B, A])  # a new pass is fine

@@ -122,3 +122,20 @@ def test_a_learning_rate_changed_in_place(calls, lr):
     assert rates(calls)[0] == (0.25, 0.25)
     opt.step(grads, 0.25)
     assert rates(calls)[0] == (0.25, 0.25)
+
+
+def test_a_step_counts_as_a_change_in_place(calls):
+    """A graph that saved a parameter before the step refuses its backward after it, as after any change
+    in place; detached views share the count."""
+    opt, grads = made(((4, 30), (30, 5)), torch.float32)
+    leaf = opt.params[0].detach().requires_grad_(True)
+    opt.params[0] = leaf.detach()
+    y = (leaf * leaf).sum()
+    held = [*opt.masters, *opt.momenta, *opt.params]
+    before = [t._version for t in held]
+    opt.step(grads, 0.1)
+    assert all(t._version > v for t, v in zip(held, before))
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        y.backward()
+    with torch.inference_mode():
+        made(own=True)[0].step(grads[:1] + [torch.randn(50, 3)], 0.1)  # (such tensors have no count)
