@@ -9,9 +9,10 @@
 // Every filter keeps a run of one order (logit, then index), so what is kept is
 // what stands no later in it than one entry: a 64-bit number each, the ordered bits of
 // the logit above the inverted index.  Equal logits need no case of their own.
-// Bins hold fixed-point sums, whose order of addition does not matter; the sums of pass 4
-// are fp64 in a fixed order.  A bin of more entries than are sorted at a time is cut again,
-// by those numbers.
+// Bins hold fixed-point sums, whose order of addition does not matter, each in a unit of
+// its own weights' size, so that a far tail counts as exactly as the head; the sums over bins and
+// those of pass 4 are fp64 in a fixed order.  A bin of more entries than are sorted at a time is cut
+// again, by those numbers.
 // Rows of bf16 (sample_values) need no sort: 11777 values hold every logit but those below
 // 2^-30 and from 2^16 on (rows with such take the passes above), so that
 //   A  counts each value's entries in LDS; from the counts, a weight per value (one exp each,
@@ -54,19 +55,20 @@ struct Shared {
     uint64_t list[kSorted];
     double runs[kRuns];
     uint64_t wave64[2 * kWaves];
-    uint64_t found[4];
+    uint64_t found[3];
+    double whole, before;
     uint32_t listed;
     int bin;
 };
 
 // Inclusive sums over the workgroup's threads of a and b.
-template <class A>
-__device__ __forceinline__ void scan2(A& a, uint64_t& b, Shared& s) {
+template <class A, class B>
+__device__ __forceinline__ void scan2(A& a, B& b, Shared& s) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const A x = __shfl_up(a, o);
-        const uint64_t y = __shfl_up(b, o);
+        const B y = __shfl_up(b, o);
         if (lane >= o) {
             a += x;
             b += y;
@@ -74,14 +76,15 @@ __device__ __forceinline__ void scan2(A& a, uint64_t& b, Shared& s) {
     }
     __syncthreads();
     A* wa = (A*)s.wave64;
+    B* wb = (B*)(s.wave64 + kWaves);
     if (lane == 63) {
         wa[wave] = a;
-        s.wave64[kWaves + wave] = b;
+        wb[wave] = b;
     }
     __syncthreads();
     for (int w = 0; w < wave; ++w) {
         a += wa[w];
-        b += s.wave64[kWaves + w];
+        b += wb[w];
     }
 }
 
@@ -107,8 +110,8 @@ __device__ __forceinline__ void sort_list(Shared& s, uint32_t n) {
 
 // 2^t for t <= 0, to 2^-46 of its value: 2^f on |f| <= 1/2 by its Taylor series (the next
 // term is 2^-47).  A weight takes this many 64-bit operations, 14, of about 45 that a
-// division and the library's exp take.
-__device__ __forceinline__ double power_of_two(double t) {
+// division and the library's exp take.  Times 2^more.
+__device__ __forceinline__ double power_of_two(double t, int more = 0) {
     if (!(t > -1000.)) return 0.;
     const double n = rint(t), x = (t - n) * 0.693147180559945309417;
     double y = 1. / 39916800.;
@@ -123,7 +126,7 @@ __device__ __forceinline__ double power_of_two(double t) {
     y = fma(y, x, 0.5);
     y = fma(y, x, 1.);
     y = fma(y, x, 1.);
-    return ldexp(y, (int)n);
+    return ldexp(y, (int)n + more);
 }
 
 template <typename T>
@@ -228,15 +231,22 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
     const uint64_t k = k0 > 0 && k0 < (int64_t)row.V ? (uint64_t)k0 : 0;
     const bool by_mass = p0 < 1.;
     if (k != 0 || by_mass) {
-        const int bits = 62 - (32 - __clz((int)row.V));  // of a fixed-point weight: their sum stays below 2^62
-        const double unit = ldexp(1., bits);
-        auto fixed = [&](float z) { return z > -INFINITY ? (uint64_t)(weight(z) * unit + 0.5) : 0ull; };
-        const float per = (float)(kBinsPerNat / T0);
+        // A weight of bin b is below 2^-raise(b) (by 2^-16 of it at most above), and the integers of
+        // a bin are its weights times 2^(bits + raise(b)): their sum stays below 2^63, and an
+        // entry's rounding is 2^-bits of it.  The last bin's entries may be smaller: those that
+        // round to nothing are 2^-78 or less (at temperatures above 2^-120, below which `per` is cut).
+        const int bits = 62 - (32 - __clz((int)row.V));
+        auto raise = [](int b) { return b * 1477 >> 16; };  // b / kBinsPerNat nats in powers of two, rounded down
+        auto fixed = [&](float z, int up) {
+            return z > -INFINITY ? (uint64_t)(power_of_two(((double)z - topd) * rate, bits + up) + 0.5) : 0ull;
+        };
+        // (halves: no difference of them overflows; finite: the largest logit's bin is 0)
+        const float per = fminf((float)(2. * kBinsPerNat / T0), 3e38f);
         // the entries in [lo, hi] by a level of bins; the first level goes by the logits
         uint64_t lo = 0, hi = ~0ull;
         auto bin_of = [&](float z, uint64_t q, int shift) {
             if (shift < 0) {
-                const float y = (top - z) * per;  // no later for larger logits
+                const float y = (0.5f * top - 0.5f * z) * per;  // no later for larger logits
                 return y < (float)(kBins - 1) ? (int)y : kBins - 1;
             }
             return (int)((hi - q) >> shift);
@@ -250,9 +260,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
             const uint64_t from = last;
             lo = 0;
             hi = ~0ull;
-            int shift = -1;
-            uint64_t count0 = 0, mass0 = 0;
-            double goal = 0.;
+            int shift = -1, up = 0;  // up: of all entries in [lo, hi], behind the first level
+            uint64_t count0 = 0;
+            double mass0 = 0., goal = 0.;
             uint32_t listed = 0;
             for (;;) {
                 for (int b = tid; b < kBins; b += NT) {
@@ -271,30 +281,33 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
                     if (!some || q < lo || q > hi || q < from) return;
                     const int b = bin_of(z, q, shift);
                     if (counts) atomicAdd(&s.count[b], 1u);
-                    else atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)fixed(z));
+                    else atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)fixed(z, shift < 0 ? raise(b) : up));
                 });
                 __syncthreads();
                 const uint32_t c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1];
-                const uint64_t m0 = s.mass[2 * tid], m1 = s.mass[2 * tid + 1];
-                uint64_t c = (uint64_t)c0 + c1, m = m0 + m1;
+                auto mass_of = [&](int b) { return ldexp((double)s.mass[b], -bits - (shift < 0 ? raise(b) : up)); };
+                const double m0 = counts ? 0. : mass_of(2 * tid), m1 = counts ? 0. : mass_of(2 * tid + 1), both = m0 + m1;
+                uint64_t c = (uint64_t)c0 + c1;
+                double m = both;
                 scan2(c, m, s);
                 if (filter == 1 && shift < 0) {  // the whole of what is kept so far
                     __syncthreads();
-                    if (tid == NT - 1) s.found[2] = m;
+                    if (tid == NT - 1) s.whole = m;
                     __syncthreads();
-                    goal = p0 * (double)s.found[2];
+                    goal = p0 * s.whole;
                     __syncthreads();
                 }
                 // the border's bin: the last that is not empty and in front of which too little lies
-                const uint64_t cb[2] = {count0 + c - c0 - c1, count0 + c - c1}, mb[2] = {mass0 + m - m0 - m1, mass0 + m - m1};
-                const bool in0 = counts ? c0 != 0 && cb[0] < k : m0 != 0 && ((double)mb[0] < goal || mb[0] == 0);
-                const bool in1 = counts ? c1 != 0 && cb[1] < k : m1 != 0 && ((double)mb[1] < goal || mb[1] == 0);
+                const uint64_t cb[2] = {count0 + c - c0 - c1, count0 + c - c1};
+                const double mb0 = mass0 + (m - both), mb[2] = {mb0, mb0 + m0};
+                const bool in0 = counts ? c0 != 0 && cb[0] < k : m0 != 0. && (mb[0] < goal || mb[0] == 0.);
+                const bool in1 = counts ? c1 != 0 && cb[1] < k : m1 != 0. && (mb[1] < goal || mb[1] == 0.);
                 if (in0 || in1) atomicMax(&s.bin, 2 * tid + (in1 ? 1 : 0));
                 __syncthreads();
                 const int bin = s.bin;
                 if (2 * tid == (bin & ~1)) {
                     s.found[2] = cb[bin & 1];
-                    s.found[3] = mb[bin & 1];
+                    s.before = mb[bin & 1];
                 }
                 __syncthreads();
                 const uint64_t inside = counts ? s.count[bin] : 0;
@@ -318,14 +331,14 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
                     const float z = logit_of((uint32_t)(q >> 32));
                     const bool first_k = tid < (int)listed && (uint64_t)tid < k && z > -INFINITY;
                     const double w = first_k ? weight(z) : 0.;
-                    uint64_t sum = first_k && by_mass ? fixed(z) : 0, rank = first_k ? 1 : 0;
-                    const uint64_t own = sum;
-                    scan2(rank, sum, s);
+                    double sum = w;
+                    uint64_t nothing = 0;
+                    scan2(nothing, sum, s);
                     __syncthreads();
-                    if (tid == NT - 1) s.found[2] = sum;
+                    if (tid == NT - 1) s.whole = sum;
                     __syncthreads();
-                    const double limit = p0 * (double)s.found[2];
-                    const bool in = first_k && w >= low && (!by_mass || (double)(sum - own) < limit || tid == 0);
+                    const double limit = p0 * s.whole;
+                    const bool in = first_k && w >= low && (!by_mass || sum - w < limit || tid == 0);
                     if (tid == 0) s.bin = NT;
                     __syncthreads();
                     if (!in) atomicMin(&s.bin, tid);
@@ -340,7 +353,6 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
                     const bool some = tid < kept_n;
                     const double mine = some ? s.runs[(uint32_t)e] : 0.;
                     double upto = mine;
-                    uint64_t nothing = 0;
                     scan2(upto, nothing, s);
                     __syncthreads();
                     if (tid == NT - 1) s.runs[0] = upto;
@@ -363,7 +375,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
                     return;
                 }
                 count0 = s.found[2];
-                mass0 = s.found[3];
+                mass0 = s.before;
+                if (shift < 0) up = raise(bin);
                 if (listed <= kSorted) break;
                 // too many: their range, and another level
                 uint64_t least = ~0ull, most = 0;
@@ -386,10 +399,13 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t n, Share
             sort_list(s, listed);
             const uint64_t q = s.list[tid];
             const bool some = tid < (int)listed;
-            uint64_t c = some ? 1 : 0, m = some && !counts ? fixed(logit_of((uint32_t)(q >> 32))) : 0;
-            const uint64_t own = m;
+            const float z = logit_of((uint32_t)(q >> 32));
+            const double own = some && !counts && z > -INFINITY ? weight(z) : 0.;
+            uint64_t c = some ? 1 : 0;
+            double m = own;
             scan2(c, m, s);
-            const bool in = some && (counts ? count0 + c - 1 < k : (double)(mass0 + m - own) < goal || mass0 + m - own == 0);
+            const double ahead = mass0 + (m - own);
+            const bool in = some && (counts ? count0 + c - 1 < k : ahead < goal || ahead == 0.);
             if (tid == 0) s.bin = -1;
             __syncthreads();
             if (in) atomicMax(&s.bin, tid);
