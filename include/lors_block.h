@@ -185,7 +185,8 @@ size_t lors_sample_workspace_bytes(const lors_sample_t* p);
  * positive weight if none does.  logp[n] (may be NULL): log of that entry's weight over
  * the sum.  Weights and sums are in 64 bits: a weight is off by at most 2^-46 + 2^-52 .
  * |log2 w| of its value, the sums that top_p's border is found by are off by vocab . 2^-60 of
- * theirs and by 2^-46 of the largest weight.
+ * theirs and by 2^-46 of the largest weight.  Below 2^-1022 weights have fewer bits, below 2^-1075
+ * none.
  * temperature, top_k, top_p, min_p: NULL, or device arrays of `rows` that take the
  * place of the scalars; there, a temperature that is not above 0 counts as 0, and a
  * top_p or min_p that is NaN as none.

@@ -112,7 +112,7 @@ __device__ __forceinline__ void sort_list(Shared& s, uint32_t n) {
 // term is 2^-47).  A weight takes this many 64-bit operations, 14, of about 45 that a
 // division and the library's exp take.  Times 2^more.
 __device__ __forceinline__ double power_of_two(double t, int more = 0) {
-    if (!(t > -1000.)) return 0.;
+    if (!(t > -1080.)) return 0.;  // (below every number: half of the least is 2^-1075)
     const double n = rint(t), x = (t - n) * 0.693147180559945309417;
     double y = 1. / 39916800.;
     y = fma(y, x, 1. / 3628800.);

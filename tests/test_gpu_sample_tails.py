@@ -93,3 +93,22 @@ def test_tails_of_several_depths(dtype):
         for u in (0.0, 0.3, 0.8, BELOW_ONE):
             check(row, u, top_p=p)
             check(row, u, top_p=p, top_k=300001)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_weights_at_the_end_of_the_range(dtype):
+    """The least weights that 64 bits hold count: u = 0 takes the first, and the next below it is none."""
+    for depth, first in ((1001, True), (1022, True), (1074, True), (1076, False), (2000, False)):
+        z = np.full(40, -np.inf)
+        z[[3, 5, 30]] = -2000.0
+        z[7] = -depth if dtype == torch.float32 else -1000.0
+        z[9] = 0.0
+        # bf16 has not all these numbers: -1000, by the temperature
+        temperature = T if dtype == torch.float32 else T * 1000.0 / depth
+        t = torch.from_numpy(z.astype(np.float32)).to(dtype).cuda().unsqueeze(0)
+        token, logp = train.sample(t, torch.zeros(1, device="cuda"), temperature)
+        assert int(token) == (7 if first else 9), depth
+        # (of 2^-1074 and what rounds to it the logarithm is that number's)
+        assert abs(float(logp) + (depth * math.log(2.0) if first else 0.0)) <= 2.0**-24 * 745
+        token, _ = train.sample(t, torch.ones(1, device="cuda"), temperature)
+        assert int(token) == 9  # nothing behind it has a weight
