@@ -707,7 +707,6 @@ struct Wide {
         w = pt + D * D;
         inv = w + D * D;
     }
-    static constexpr int64_t kDoubles = 6 * D * D + 2;
 };
 
 // S_0 out of the pieces' sum (tiles (t, u), t <= u, of 16 x 16 each).
@@ -944,8 +943,8 @@ hipError_t launch_size(const UpdateArgs& a, const Matrix* matrices, int64_t coun
 
 int64_t update_scratch(int64_t d, int64_t n) {
     const int64_t dt = blocks_of(d);
-    // (the steps of the wide sides keep six matrices and |v| there)
-    return 8 * (pieces_of(n) * (dt * (dt + 1) / 2 * 256) + (dt > 4 ? 6 * 256 * dt * dt + 2 : 256 * dt * dt));
+    // (the steps of the wide sides keep six matrices and |v| there, in 256 bytes of its own)
+    return 8 * (pieces_of(n) * (dt * (dt + 1) / 2 * 256) + (dt > 4 ? 6 * 256 * dt * dt + 32 : 256 * dt * dt));
 }
 
 int64_t update_table(int64_t count) { return count > kBatch ? count * (int64_t)(sizeof(Matrix) + kLaunches * sizeof(int)) : 0; }
