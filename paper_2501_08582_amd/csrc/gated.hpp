@@ -47,26 +47,25 @@ __host__ __device__ static inline int token_parts(int64_t L, int tm) {
     return (int)(parts < most ? parts : most);
 }
 
-// tanh of the GELU's argument and that argument's slope.  tanh(x) = sign(x) (1 - e) / (1 + e)
-// with e = exp(-2|x|) <= 1: no overflow, and full relative accuracy where 1 - e has
-// it; below |x| = 1/16 the series x - x^3/3 + 2x^5/15 (the next term is 4e-8 of x)
-// stands for the difference that cancels.
-__device__ __forceinline__ float gelu_tanh(float g, float& slope) {
+// GELU's (1 + tanh(x)) / 2 = 1 / (1 + exp(-2x)) for x = k (g + 0.044715 g^3), without the difference that
+// cancels below zero (1 + tanh(x) is 2^-24 at g = -5, a rounding of tanh): `s`, and 1 - s in
+// `rest`, both of full relative accuracy, and x's slope.
+__device__ __forceinline__ float gelu_gate(float g, float& rest, float& slope) {
     constexpr float k = 0.797884560802865356f;  // sqrt(2 / pi)
     const float g2 = g * g;
     const float x = k * g * (1.f + 0.044715f * g2);
     slope = k * (1.f + 0.134145f * g2);
-    const float e = __expf(-2.f * fabsf(x)), x2 = x * x;
-    const float far = copysignf((1.f - e) / (1.f + e), x);
-    return fabsf(x) < 0.0625f ? x * (1.f + x2 * (-0.333333333f + 0.133333333f * x2)) : far;
+    const float e = __expf(-2.f * fabsf(x)), big = 1.f / (1.f + e), small = e * big;  // no overflow
+    rest = x < 0.f ? big : small;
+    return x < 0.f ? small : big;
 }
 
 // SiLU g / (1 + exp(-g)), or GELU g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  Where exp(-g)
 // overflows (g below -88) SiLU is -0, as its limit is.
 __device__ __forceinline__ float activate(float g, int gelu) {
     if (gelu) {
-        float slope;
-        return 0.5f * g * (1.f + gelu_tanh(g, slope));
+        float rest, slope;
+        return g * gelu_gate(g, rest, slope);
     }
     return g / (1.f + __expf(-g));
 }
@@ -74,10 +73,10 @@ __device__ __forceinline__ float activate(float g, int gelu) {
 // act(g), and its derivative in `d`
 __device__ __forceinline__ float activate_grad(float g, int gelu, float& d) {
     if (gelu) {
-        float slope;
-        const float t = gelu_tanh(g, slope);
-        d = 0.5f * (1.f + t) + 0.5f * g * (1.f - t * t) * slope;
-        return 0.5f * g * (1.f + t);
+        float rest, slope;
+        const float s = gelu_gate(g, rest, slope), bend = s * rest;
+        d = s + (bend != 0.f ? 2.f * g * bend * slope : 0.f);  // (the slope may have overflown where the bend is 0)
+        return g * s;
     }
     const float y = 1.f / (1.f + __expf(-g));
     d = y * (1.f + g * (1.f - y));
