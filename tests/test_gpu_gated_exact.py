@@ -1,0 +1,67 @@
+"""The gated block's forward where every sum is exact: H held to its one rounding, element by element.
+
+Inputs are small multiples of powers of two.  W' has at most 8 bits, every sum of products fits
+24, so that G and U are exact in fp32 whatever the order, and stored they are their one rounding,
+bit for bit.  H = act(G) U out of the unrounded sums is off by the fp32 steps of act (below 2^-15 of it,
+where |G| < 8) and by its rounding, 2^-8 of itself; in tiles of ranks above 48 act(G) is rounded to bf16 on
+the way as well.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block as ob
+from paper_2501_08582_amd import ops
+from tests.gpu_helpers import dev_to_f64
+
+pytestmark = pytest.mark.gpu
+
+U8 = 2.0**-8
+
+# few tokens; thin tiles of few tokens of a wide projection; whole tiles and edges, thin tiles behind them, ragged K; half-feature tiles
+FEW = [(3, 136, 104, 5), (16, 4104, 72, 16), (33, 520, 192, 17), (7, 1032, 520, 128), (100, 520, 72, 64)]
+THIN = [(4, 10000, 264, 16), (32, 9280, 136, 40), (200, 2560, 200, 48)]
+TILES = [(577, 1032, 200, 31), (768, 1024, 128, 16), (3328, 2560, 128, 48), (3299, 2560, 72, 33)]
+WIDE_RANKS = [(577, 1032, 200, 64), (600, 1032, 192, 100), (3328, 2560, 64, 64), (1030, 520, 72, 128)]
+
+
+def case(L, R, C, r, fmt):
+    """X, and both projections' device tensors and W' of multiples of 2^-5, below 4: |G| below 8."""
+    g = torch.Generator(device="cuda").manual_seed(L + R + C + r)
+
+    def whole(least, most, *shape):
+        return torch.randint(least, most + 1, shape, generator=g, device="cuda").double()
+
+    X = whole(-4, 4, L, C) * 2.0**(-4 if C < 300 else -5)
+    pair, merged = [], []
+    for _ in range(2):
+        if fmt == "2:4":
+            place = torch.rand((R, C // 4, 4), generator=g, device="cuda").topk(2, dim=2).indices
+            keep = torch.zeros((R, C // 4, 4), dtype=torch.bool, device="cuda").scatter_(2, place, True).view(R, C)
+        else:
+            keep = torch.rand((R, C), generator=g, device="cuda") < 0.5
+        W = whole(-31, 31, R, C) * 2.0**-5 * keep
+        B, A = whole(-1, 1, R, r) * 0.25, whole(-1, 1, r, C) * (torch.rand((r, C), generator=g, device="cuda") < 32 / (32 + r))
+        low = B @ A * 0.5
+        assert float(low.abs().max()) <= 96 * 2.0**-5
+        merged.append((W + low) * keep)
+        pair.append((W.bfloat16(), ops.mask_pack(keep, fmt), B.bfloat16(), A.bfloat16()))
+        assert all(torch.equal(t.double(), s) for t, s in zip((pair[-1][0], *pair[-1][2:], merged[-1].bfloat16()), (W, B, A, merged[-1])))
+    return X, pair, merged
+
+
+@pytest.mark.parametrize("i,shape,roundings", [(i, s, n) for n, part in ((1, FEW + THIN + TILES), (2, WIDE_RANKS)) for i, s in enumerate(part)])
+def test_forward(i, shape, roundings):
+    L, R, C, r = shape
+    fmt, act = ("bitmap", "2:4")[i % 2], ("silu", "gelu")[i // 2 % 2]
+    X, pair, merged = case(L, R, C, r, fmt)
+    H, G, U = ops.gated_forward(X.bfloat16(), *pair, 0.5, fmt, act)
+    G64, U64 = (X @ W.T for W in merged)
+    assert torch.equal(G64.float().double(), G64) and float(G64.abs().max()) < 8
+    assert torch.equal(G, G64.float().bfloat16()) and torch.equal(U, U64.float().bfloat16())
+    want = ob.act(dev_to_f64(G64), act)[0] * dev_to_f64(U64)
+    err = np.abs(dev_to_f64(H) - want)
+    # GELU: exp(-2t), |2t| <= 50, is off by 5.5 |2t| 2^-24 and its other steps by 8 . 2^-24
+    bound = ((1 + U8) ** roundings - 1 + 2.0**-14) * np.abs(want)
+    assert (err <= bound).all(), (float((err / np.maximum(np.abs(want), 1e-300)).max()), int((err > bound).sum()))
+    assert torch.equal(ops.gated_forward(X.bfloat16(), *pair, 0.5, fmt, act, save=False)[0], H)
