@@ -65,3 +65,32 @@ def test_forward(i, shape, roundings):
     bound = ((1 + U8) ** roundings - 1 + 2.0**-14) * np.abs(want)
     assert (err <= bound).all(), (float((err / np.maximum(np.abs(want), 1e-300)).max()), int((err > bound).sum()))
     assert torch.equal(ops.gated_forward(X.bfloat16(), *pair, 0.5, fmt, act, save=False)[0], H)
+
+
+BACK = [(1, 8, 8, 1), (5, 72, 40, 3), (65, 520, 200, 12), (200, 264, 512, 64), (577, 1032, 200, 100), (333, 72, 1032, 128),
+        (3328, 64, 2560, 16), (3328, 128, 2560, 64), (3300, 72, 2552, 33), (260, 1032, 10000, 5), (512, 1088, 10240, 64),
+        (2100, 1032, 8200, 33), (40, 1032, 520, 128), (150, 264, 2056, 70)]
+
+
+@pytest.mark.parametrize("i,shape", list(enumerate(BACK)))
+def test_backward(i, shape):
+    """At G = 32 both activations are G and their derivatives 1, so that dG = dH U and dU = 32 dH are exact in
+    bf16; so are D = d^T X (whole numbers of at most 8 bits, 32 times those of U) and all sums: dX is its one
+    rounding and the adapters' gradients are exact, bit for bit, whatever the order of their sums."""
+    L, R, C, r = shape
+    fmt, act = ("2:4", "bitmap")[i % 2], ("silu", "gelu")[i // 2 % 2]
+    _, pair, merged = case(L, R, C, r, fmt)
+    g = torch.Generator(device="cuda").manual_seed(i)
+
+    def signs(*shape):
+        return torch.randint(-1, 2, shape, generator=g, device="cuda").double()
+
+    X, dH, G = signs(L, C), signs(L, R), torch.full((L, R), 32.0, device="cuda").double()
+    U = torch.where(torch.rand((L, R), generator=g, device="cuda") < 0.5, 1.0, -1.0).double()
+    dX, gate, up = ops.gated_backward(*(t.bfloat16() for t in (dH, X)), *pair, G.bfloat16(), U.bfloat16(), 0.5, fmt, act)
+    dG, dU = dH * U, dH * G
+    assert torch.equal(dX, (dG @ merged[0] + dU @ merged[1]).float().bfloat16())
+    for (dB, dA), d, (_, M, B, A) in zip((gate, up), (dG, dU), pair):
+        D = (d.T @ X) * ops.mask_unpack(M, R, C, fmt).bool()
+        assert torch.equal(D.bfloat16().double(), D)
+        assert torch.equal(dB, (0.5 * D @ A.double().T).float()) and torch.equal(dA, (0.5 * B.double().T @ D).float())
