@@ -161,18 +161,24 @@ hipError_t launch_dbias_bf16(const LayerArgs& a, hipStream_t s);
 // Gated block (a.second): a.Y is H, a.dY the gradient of G.  dX is the sum over both
 // projections; dB and dA are cleared by the dX launch (a.clear_grads) or the caller.
 // Whether the gated block's forward takes the kernel for few tokens: where one projection's does
-// (above), but up to rank 48 its tiles, which hold both projections, are ahead sooner.  Thin
-// tiles take about 0.75 us a K-step whatever R is while their workgroups, of 64 columns of H
-// each, fit the CUs.  Few against tiles, 4096 columns, rank 16 (us): up to 32 tokens 8192 rows
-// 38 to 46 against 49, 11008 rows 63 to 77 against 56, 14336 rows 72 to 80 against 61; 64 tokens, 4096
-// rows 47 against 47, 8192 rows 66 against 51; 128 tokens, 2048 x 2048 26 against 27, 4096 rows 55
-// against 47, 2744 x 1032 15 against 21.
+// (above), but up to rank 48 its tiles, which hold both projections, are ahead sooner: they take
+// the same time whatever the rows are while their workgroups, of 64 columns of H each, fit the CUs.  So
+// up to 32 tokens the kernel has the rows that its workgroups of 32 features pass over at once,
+// above them half of those; narrow projections end sooner than the tiles' pipeline starts.  Few against
+// tiles (us), ranks 16 and 48:
+//   4 tokens of C = 4096: R = 8192 38 / 51 and 48 / 57, 8224 63 / 51 and 84 / 56, 14336 70 / 62 and 91 / 67
+//   32 tokens: C = 4096, R = 8192 48 / 53 and 56 / 58, 9216 74 / 54 and 104 / 60; C = 1024, R = 8192 15 / 19 and
+//     17 / 21, 11008 22 / 19 and 31 / 21; C = 512, R = 9216 12.6 / 12.8 and 18.0 / 14.4 (rank 32 13.5 / 13.7)
+//   64 tokens: C = 4096, R = 4096 49 / 51 and 56 / 57, 4352 68 / 52 and 73 / 58; C = 2048, R = 4096 27 / 30 and 30 / 33,
+//     4352 35 / 30 and 39 / 33; C = 1024, R = 4352 19.0 / 18.6 and 20.9 / 20.5, 8192 19.7 / 19.2 and 21.7 / 21.0;
+//     C = 520, R = 8192 11.8 / 16.2 and 12.8 / 17.8
+//   128 tokens: C = 2048, R = 2048 26 / 28 (rank 16)
 inline bool gated_few_tokens(int64_t L, int64_t R, int64_t C, int64_t r) {
     if (!fwd_few_tokens(L, R, C)) return false;
     if (r > 48) return true;
-    const int64_t cus = device_cus(), wgs = (R + 63) / 64, rounds = (wgs + cus - 1) / cus;
-    if (L <= 32) return C <= 2048 || 16 * wgs <= 9 * cus * rounds;
-    return 4 * ((R + 31) / 32) * ((L + 63) / 64) <= 3 * cus;
+    const int64_t cus = device_cus(), wgs = (R + 31) / 32 * ((L + 63) / 64);
+    if (L <= 32) return wgs <= cus || (C <= 512 && r <= 32);
+    return 2 * wgs <= cus || C <= 1024;
 }
 hipError_t launch_gated_fwd_bf16(const LayerArgs& a, hipStream_t s);
 hipError_t launch_gated_fwd_thin_bf16(const LayerArgs& a, hipStream_t s, int first, int tail, int tm);

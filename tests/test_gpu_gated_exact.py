@@ -18,9 +18,10 @@ pytestmark = pytest.mark.gpu
 
 U8 = 2.0**-8
 
-# few tokens; thin tiles of few tokens of a wide projection; whole tiles and edges, thin tiles behind them, ragged K; half-feature tiles
+# few tokens; such of wide projections, on both sides of what is left to thin tiles; whole tiles and edges, thin tiles behind them, ragged K; half-feature tiles
 FEW = [(3, 136, 104, 5), (16, 4104, 72, 16), (33, 520, 192, 17), (7, 1032, 520, 128), (100, 520, 72, 64)]
-THIN = [(4, 10000, 264, 16), (32, 9280, 136, 40), (200, 2560, 200, 48)]
+THIN = [(4, 10000, 264, 16), (16, 8224, 1032, 48), (32, 8192, 520, 40), (20, 9216, 512, 40), (64, 4352, 1032, 32),
+        (40, 8192, 264, 24), (32, 9280, 136, 40), (200, 2560, 200, 48)]
 TILES = [(577, 1032, 200, 31), (768, 1024, 128, 16), (3328, 2560, 128, 48), (3299, 2560, 72, 33)]
 WIDE_RANKS = [(577, 1032, 200, 64), (600, 1032, 192, 100), (3328, 2560, 64, 64), (1030, 520, 72, 128)]
 
