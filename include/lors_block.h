@@ -78,7 +78,8 @@ lors_status_t lors_gated_forward(const lors_problem_t* p, int32_t activation, co
  *   dG = dH . U . act'(G), dU = dH . act(G)   (rounded to the dtype, in the workspace)
  *   dX = dG . Wg' + dU . Wu'                  (skipped if dX is NULL; rounded once)
  *   dB, dA of each projection as lors_backward's, from dG and dU: fp32,
- *   overwritten, their sums' order not fixed.
+ *   overwritten, their sums' order not fixed; bf16: the weight's gradient takes part in them
+ *   to 2^-16 of itself (lors_backward: to 2^-8).
  * p->flags: 0 or LORS_FLAG_REUSE_MASK_T (the workspace still holds the transposed
  * masks of an earlier call with the same R, C, r, L and masks), otherwise
  * LORS_ERR_UNSUPPORTED.

@@ -17,6 +17,12 @@
 // in the accumulator's own row order); dB reads G^T back from LDS.  Per-tile
 // partial sums are added into dB and dA with fp32 atomics, so dB and dA must
 // be zero on entry.
+//
+// A gated block's dY (dG, dU) is itself rounded on the way, so its G is not rounded once more:
+// it stands in both products as two bf16 numbers, its rounding and what that leaves (2^-16 of
+// G is lost).  Relative errors of the gradients rounded to bf16, 4096 tokens of 13824 x 5120, rank 64: 2.3e-3, with
+// one number 2.9e-3 (an exact result's rounding alone: 1.7e-3).  The second one takes 29 of 2370 us of
+// that backward, 10 of 211 of 128 tokens of 11008 x 4096, rank 16.
 #include "gemm_common.hpp"
 #include "kernels.hpp"
 #include "gated.hpp"
@@ -57,7 +63,8 @@ constexpr int EP_LUT = 8192;                       // select LUT: 4 KiB
 constexpr int EP_B = 12288;                        // B block [i][32*JB] bf16: 16 KiB per 32 ranks
                                                    // (then the dA exchange, see the kernel)
 constexpr int EP_A = SMEM;                         // A block [32 j'][256 j]: 16 KiB
-constexpr int SMEM_ALL = SMEM + 32 * kRowBytes;
+constexpr int EP_A_BYTES = 32 * kRowBytes;
+constexpr int SMEM_ALL = SMEM + EP_A_BYTES;
 
 // Copies use uniform bases plus fixed per-lane offsets.  Columns past R or C
 // are not read: their lanes copy the last chunk that exists, and the G entries
@@ -82,11 +89,12 @@ __global__ __launch_bounds__(NT, 1) void g_kernel(
     constexpr int JB = (RK + 1) / 2;  // 32-wide blocks of the rank
     // dA exchange: JBC rank blocks per round, one 4 KiB slot [v/4][lane][4]
     // per (wj, column block b, rank block of the round), right after the B block
-    constexpr int JBC = JB <= 2 ? JB : 1;
+    // (a gated block's: one, for the registers that the second numbers take)
+    constexpr int JBC = JB <= 2 && !kGated ? JB : 1;
     constexpr int EP_X = EP_B + BM * 32 * JB * 2;
     static_assert(GT_BYTES <= SMEM, "G^T tile fits");
     static_assert(EP_X + 2 * 4 * JBC * 16 * kWave * 4 <= SMEM, "B block and dA exchange fit");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[SMEM_ALL];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[SMEM_ALL + (kGated && JB > 1 ? EP_A_BYTES : 0)];
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -341,6 +349,7 @@ __global__ __launch_bounds__(NT, 1) void g_kernel(
     // accumulator elements 8c .. 8c+7 of block (a, b): rows 16c + 4h + {0..3}
     // and 16c + 8 + 4h + {0..3} of column j = l32.
     u32x4 gb[4][4][2];
+    u32x4 rest[kGated ? 4 : 1][kGated ? 4 : 1][2];  // a gated block: what the rounding leaves, in bf16
 #pragma unroll
     for (int a = 0; a < 4; ++a)
 #pragma unroll
@@ -354,6 +363,15 @@ __global__ __launch_bounds__(NT, 1) void g_kernel(
 #pragma unroll
                 for (int p = 0; p < 4; ++p)
                     gb[a][b][c][p] = pack_bf16x2(acc[a][b][8 * c + 2 * p], acc[a][b][8 * c + 2 * p + 1]) & sel[p];
+                if constexpr (kGated) {
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const float x = acc[a][b][8 * c + 2 * p] - __uint_as_float(gb[a][b][c][p] << 16);
+                        const float y = acc[a][b][8 * c + 2 * p + 1] - __uint_as_float(gb[a][b][c][p] & 0xFFFF0000u);
+                        // (where that is not a number, beside an Inf or NaN, some number)
+                        rest[a][b][c][p] = pack_bf16x2(__builtin_amdgcn_fmed3f(x, -2e36f, 2e36f), __builtin_amdgcn_fmed3f(y, -2e36f, 2e36f)) & sel[p];
+                    }
+                }
             }
         }
 
@@ -392,6 +410,9 @@ __global__ __launch_bounds__(NT, 1) void g_kernel(
                                                        lds_tr_read(smem + EP_B + 2 * ((row + 8) * 32 * JB + col)));
 #pragma unroll
                         for (int b = 0; b < 4; ++b) part[b][jl] = mfma_32x32x16(bt, as_bf16x8(gb[a][b][c]), part[b][jl]);
+                        if constexpr (kGated)
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) part[b][jl] = mfma_32x32x16(bt, as_bf16x8(rest[a][b][c]), part[b][jl]);
                     }
             }
 #pragma unroll
@@ -438,6 +459,91 @@ __global__ __launch_bounds__(NT, 1) void g_kernel(
     auto gt_off = [](int j, int i) {
         return j * GT_PITCH + (((i >> 3) ^ ((j & 7) << 2)) << 4) + ((i & 7) << 1);
     };
+    if constexpr (kGated) {
+        // Both numbers of a gated block's G, one after the other in LDS, for the same sums; epilogues 4
+        // and 5 as below, which keep their own loops (the layer's code is then the same instructions
+        // with or without these).  Written twice, G^T has a swizzle of its own: the chunk XORed with
+        // j % 16, bits 0 and 1 above bits 2 and 3, so that the 16-byte writes of 32 consecutive j fall
+        // on all banks (on a quarter of them below), and reads of 4 consecutive j as below.
+        auto gt_own = [](int j, int i) {
+            return j * GT_PITCH + (((i >> 3) ^ ((j & 3) << 2 | (j >> 2 & 3))) << 4) + ((i & 7) << 1);
+        };
+        auto put_gt = [&](const u32x4 (&gt)[4][4][2]) {
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int jl = wj * 128 + 32 * b + l32;
+#pragma unroll
+                    for (int v4 = 0; v4 < 4; ++v4) {
+                        const int il = wi * 128 + 32 * a + 8 * v4 + 4 * h;
+                        const u32x4& gv = gt[a][b][v4 >> 1];
+                        u32x2 o;
+                        o[0] = gv[2 * (v4 & 1)];
+                        o[1] = gv[2 * (v4 & 1) + 1];
+                        *(u32x2*)(smem + gt_own(jl, il)) = o;
+                    }
+                }
+        };
+        auto copy_a = [&](int jb) {  // copy_a_block, into place jb % 2
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int blk = 4 * wave + q, row = 2 * blk + h;
+                const int jr = 32 * jb + row, gj = j0 + 8 * swz_chunk(row, lane & 31);
+                copy16_to_lds((jr < r && gj < C) ? (const void*)(Am + (int64_t)jr * C + gj) : (const void*)zsrc,
+                              lds0 + EP_A + EP_A_BYTES * (jb & 1) + 1024 * blk);
+            }
+        };
+        auto form_db = [&](f32x16 (&db)[2], int jb) {
+            const int g = lane >> 4, jj = lane & 15;
+#pragma unroll 4
+            for (int kc = 0; kc < BN / 16; ++kc) {
+                const int jr0 = 16 * kc + 8 * (g >> 1) + (jj >> 2);
+                const bf16x8 av = *(const bf16x8*)(smem + EP_A + EP_A_BYTES * (jb & 1) + tile_off(l32, 16 * kc + 8 * h));
+#pragma unroll
+                for (int ib = 0; ib < 2; ++ib) {
+                    const int ic = 64 * wave + 32 * ib + 16 * (g & 1) + 4 * (jj & 3);
+                    const bf16x8 ga = frag_from_tr(lds_tr_read(smem + gt_own(jr0, ic)), lds_tr_read(smem + gt_own(jr0 + 4, ic)));
+                    db[ib] = mfma_32x32x16(ga, av, db[ib]);
+                }
+            }
+        };
+        // rank blocks up and down again; A's next one is on its way while one works, unless it is in its place
+        f32x16 db[JB][2];
+        int in_place[2] = {0, -1};
+#pragma unroll
+        for (int n = 0; n < 2 * JB; ++n) {
+            auto block_of = [](int n) { return n < JB ? n : 2 * JB - 1 - n; };
+            const int jb = block_of(n), next = block_of(n + 1);
+            if (n % JB == 0) put_gt(n == 0 ? gb : rest);
+            if (n < JB)
+#pragma unroll
+                for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) db[jb][ib][v] = 0.f;
+            stage_barrier<0>();  // A block landed; G^T complete
+            if (n + 1 < 2 * JB && in_place[next & 1] != next) {
+                copy_a(next);
+                in_place[next & 1] = next;
+            }
+            form_db(db[jb], jb);
+            lds_barrier();  // A block free for the next but one, G^T for the second numbers
+        }
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) {
+            const int jr = 32 * jb + l32;
+            if (jr < r) {
+#pragma unroll
+                for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int gi = i0 + 64 * wave + 32 * ib + 8 * (v >> 2) + 4 * h + (v & 3);
+                        if (gi < R) atomicAdd(dB + (int64_t)gi * r + jr, s * db[jb][ib][v]);
+                    }
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int a = 0; a < 4; ++a)
 #pragma unroll

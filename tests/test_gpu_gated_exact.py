@@ -73,25 +73,48 @@ BACK = [(1, 8, 8, 1), (5, 72, 40, 3), (65, 520, 200, 12), (200, 264, 512, 64), (
         (2100, 1032, 8200, 33), (40, 1032, 520, 128), (150, 264, 2056, 70)]
 
 
+@pytest.mark.parametrize("most", [1, 7])
 @pytest.mark.parametrize("i,shape", list(enumerate(BACK)))
-def test_backward(i, shape):
+def test_backward(i, shape, most):
     """At G = 32 both activations are G and their derivatives 1, so that dG = dH U and dU = 32 dH are exact in
-    bf16; so are D = d^T X (whole numbers of at most 8 bits, 32 times those of U) and all sums: dX is its one
-    rounding and the adapters' gradients are exact, bit for bit, whatever the order of their sums."""
+    bf16, and all sums of products in fp32.  D = d^T X are whole numbers (32 times such), of at most 8 bits where
+    the inputs are at most 1 and of at most 16 where they go up to 7, both of which the adapters'
+    gradients take whole: dX is its one rounding and they are exact, bit for bit, whatever the order of their sums."""
     L, R, C, r = shape
     fmt, act = ("2:4", "bitmap")[i % 2], ("silu", "gelu")[i // 2 % 2]
     _, pair, merged = case(L, R, C, r, fmt)
     g = torch.Generator(device="cuda").manual_seed(i)
 
-    def signs(*shape):
-        return torch.randint(-1, 2, shape, generator=g, device="cuda").double()
+    def whole(*shape):
+        return torch.randint(-most, most + 1, shape, generator=g, device="cuda").double()
 
-    X, dH, G = signs(L, C), signs(L, R), torch.full((L, R), 32.0, device="cuda").double()
+    X, dH, G = whole(L, C), whole(L, R), torch.full((L, R), 32.0, device="cuda").double()
     U = torch.where(torch.rand((L, R), generator=g, device="cuda") < 0.5, 1.0, -1.0).double()
     dX, gate, up = ops.gated_backward(*(t.bfloat16() for t in (dH, X)), *pair, G.bfloat16(), U.bfloat16(), 0.5, fmt, act)
     dG, dU = dH * U, dH * G
     assert torch.equal(dX, (dG @ merged[0] + dU @ merged[1]).float().bfloat16())
     for (dB, dA), d, (_, M, B, A) in zip((gate, up), (dG, dU), pair):
         D = (d.T @ X) * ops.mask_unpack(M, R, C, fmt).bool()
-        assert torch.equal(D.bfloat16().double(), D)
+        first = D.bfloat16().double()
+        assert torch.equal(first + (0.0 if most == 1 else (D - first).bfloat16().double()), D)
         assert torch.equal(dB, (0.5 * D @ A.double().T).float()) and torch.equal(dA, (0.5 * B.double().T @ D).float())
+
+
+@pytest.mark.parametrize("r", [5, 40])
+def test_infinite_gradients_reach_what_they_reach(r):
+    """An Inf of dH makes the sums infinite that hold it with a kept weight, all terms being positive, and
+    no other; in masked places it is nothing."""
+    L, R, C = 70, 72, 136
+    _, pair, _ = case(L, R, C, r, "bitmap")
+    pair = [(W, M, B.abs() + 1, A.abs() + 1) for W, M, B, A in pair]
+    X, dH = torch.ones(L, C, device="cuda").bfloat16(), torch.ones(L, R, device="cuda").bfloat16()
+    dH[64, 7] = float("inf")
+    G, U = torch.full((L, R), 32.0, device="cuda").bfloat16(), torch.ones(L, R, device="cuda").bfloat16()
+    _, gate, up = ops.gated_backward(dH, X, *pair, G, U, 0.5)
+    for (dB, dA), (_, M, _, _) in zip((gate, up), pair):
+        kept = ops.mask_unpack(M, R, C).bool()
+        assert kept[7].any() and not kept[7].all()
+        wantB, wantA = torch.zeros(R, r, dtype=torch.bool, device="cuda"), kept[7].expand(r, C)
+        wantB[7] = True
+        assert torch.equal(dB == float("inf"), wantB) and torch.equal(dA == float("inf"), wantA)
+        assert torch.isfinite(dB[~wantB]).all() and torch.isfinite(dA[~wantA]).all()
