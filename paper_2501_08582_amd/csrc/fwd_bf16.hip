@@ -137,7 +137,8 @@ struct Layout {
 // workgroup computes one after the other; see the epilogue.
 // LORS_GATED 2: a tile holds half as many columns of H, waves 0 and 1 form the gate's
 // features of them and waves 2 and 3 the up projection's: X is read once for both, and the sums
-// meet in LDS, unrounded.  Its stages hold two A slabs, which fit up to rank 48.
+// meet in LDS, unrounded.  Its stages hold two A slabs, which fit beside those of 256 tokens x 256 features up
+// to rank 48 (168192 bytes of 163840 above it).
 template <int RK, bool KRAG, bool FOLD, int TM, int NF>
 __global__ __launch_bounds__(NT, 1) void fwd_kernel(
     const uint16_t* __restrict__ X, const uint16_t* __restrict__ LORS_FIRST(W),

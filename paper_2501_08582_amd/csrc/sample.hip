@@ -23,8 +23,10 @@
 // One workgroup a row, because the passes wait for each other: a second launch or a grid's
 // barrier costs what splitting a row would save.  Bound by that workgroup's own work: 131072
 // entries alone 37 us (about a third each of A, the border, B and the end), 256 such rows, one to a
-// compute unit, 49 (67 MB: 14 at a copy's rate); 37 rows of 50021 fp32 with top-p 59, whose fixed-point
-// sums take a 64-bit exp an entry, 46 with top-k alone.
+// compute unit, 47 (67 MB: 14 at a copy's rate); 37 rows of 50021 fp32 with top-p 59, whose fixed-point
+// sums take a 64-bit exp an entry, 46 with top-k alone.  1024 lanes leave 128 registers each, of which the
+// bf16 kernel, with the passes for other rows in it, spills 36 and the fp32 one 7.  A row of bf16 with
+// one entry outside the table's values takes those passes: 84 us alone, 256 of 131072 entries 206.
 #include "block_kernels.hpp"
 #include "train_common.hpp"
 
