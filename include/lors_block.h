@@ -147,7 +147,8 @@ size_t lors_orthogonal_workspace_bytes(const lors_update_t* p, const lors_update
  * host array, read during the call.  m, master and param may not overlap anything
  * else of the call (the same array in two items: LORS_ERR_ALIAS).  Every result is a
  * function of the inputs alone, bit for bit; where a matrix's gradient holds an Inf
- * or NaN, that matrix's results are NaN, no other's.
+ * or NaN, that matrix's master and param are NaN (m where the gradient is Inf or NaN), no
+ * other's.
  */
 lors_status_t lors_orthogonal_update(const lors_update_t* p, const lors_update_item_t* items, int64_t count,
                                      void* workspace, size_t workspace_bytes, void* stream);
